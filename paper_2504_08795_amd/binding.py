@@ -345,3 +345,189 @@ def daris_probe_cus(p, n_groups=2048, spin=2000):
     out = np.zeros(2 * n_groups, np.uint32)
     _chk(lib().daris_probe_cus(p, n_groups, spin, out.ctypes.data_as(C.POINTER(C.c_uint32))))
     return out.reshape(n_groups, 2)
+
+
+# ---- operators of a generation step (include/daris_ops.h) ------------------------------------------------------------------
+
+STEP_NORM, STEP_APPEND, STEP_ATTEND, STEP_MATVEC = range(4)
+PAGE_TOKENS, SCALE_TOKENS = 64, 16
+
+
+def _struct(name, *fields):
+    return type(name, (C.Structure,), {"_fields_": [(f, t) for t, fs in fields for f in fs.split()]})
+
+
+_P, _L, _I, _F = C.c_void_p, C.c_int64, C.c_int32, C.c_float
+daris_norm = _struct("daris_norm", (_P, "x res weight sum y scale"), (_L, "x_row res_row sum_row y_row"), (_I, "rows width group dtype"), (_F, "eps"))
+daris_cache = _struct("daris_cache", (_P, "k v k_scale v_scale pages before"), (_L, "pages_row"), (_I, "n_pages n_seqs kv_heads dim"))
+daris_append = _struct("daris_append", (daris_cache, "cache"), (_P, "k v q q_out turn row_start"),
+                       (_L, "k_row k_head v_row v_head q_row q_head qo_row qo_head"), (_I, "n_rows q_heads dtype turn_rows rot_dim pairs"))
+daris_attend = _struct("daris_attend", (daris_cache, "cache"), (_P, "q out row_start"), (_L, "q_row q_head out_row out_head"),
+                       (_I, "n_rows q_heads dtype window"), (_F, "scale"))
+daris_matvec = _struct("daris_matvec", (_P, "x x_scale w w_scale y"), (_L, "x_row w_row y_row"), (_I, "rows n k group dtype gate"))
+
+
+class _step(C.Union):
+    _fields_ = [("norm", daris_norm), ("append", daris_append), ("attend", daris_attend), ("matvec", daris_matvec)]
+
+
+class daris_op(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("reserved", C.c_int32), ("u", _step)]
+
+
+_lib_sigs = {"daris_run_ops": (C.c_int32, [C.POINTER(daris_op), C.c_int32, C.c_int32])}
+_SIGS.update(_lib_sigs)
+EXPORTS = sorted(_SIGS)
+
+
+def _need(ok, text):
+    if not ok:
+        raise DarisError(EINVAL, text)
+
+
+def _tensor(name, t, dims, dtypes):
+    """Checks what a descriptor cannot say: a GPU tensor of one of `dtypes` with `dims` dimensions, the last one's elements side by side."""
+    _need(hasattr(t, "data_ptr") and t.is_cuda, f"{name} is no GPU tensor")
+    _need(t.dim() == dims, f"{name} has {t.dim()} dimensions, not {dims}")
+    _need(str(t.dtype)[6:] in dtypes, f"{name} is of {t.dtype}, not {' or '.join(dtypes)}")
+    _need(t.shape[-1] <= 1 or t.stride(-1) == 1, f"{name}'s last dimension is strided")
+    return t
+
+
+def _dense(name, t, shape, dtypes):
+    _tensor(name, t, len(shape), dtypes)
+    _need(tuple(t.shape) == tuple(shape), f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
+    _need(t.is_contiguous(), f"{name} is not contiguous")
+    return t
+
+
+_ACT = ("bfloat16", "float32")
+_F8 = ("float8_e4m3fn",)
+_E8 = ("float8_e8m0fnu", "uint8")
+
+
+def _like(name, t, x):
+    _need(t.dtype == x.dtype, f"{name} is of {t.dtype}, not {x.dtype}")
+    return t
+
+
+def _dtype(t):
+    return BF16 if str(t.dtype) == "torch.bfloat16" else FP32
+
+
+def _at(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _made(kind, value, *keep):
+    op = daris_op(kind, 0)
+    setattr(op.u, ("norm", "append", "attend", "matvec")[kind], value)
+    op.keep = keep      # the buffers live as long as their descriptor
+    return op
+
+
+def make_norm(x, weight, y, eps, res=None, sum=None, scale=None):
+    """y = norm(x + res) * weight for tensors [rows][width] (see daris_norm); y in float8_e4m3fn with scale [rows][width / group]."""
+    _tensor("x", x, 2, _ACT)
+    rows, width = x.shape
+    _like("weight", _dense("weight", weight, (width,), _ACT), x)
+    for name, t in (("res", res), ("sum", sum)):
+        if t is not None:
+            _need(tuple(_like(name, _tensor(name, t, 2, _ACT), x).shape) == (rows, width), f"{name} is {tuple(t.shape)}, not {(rows, width)}")
+    _tensor("y", y, 2, _F8 if scale is not None else _ACT)
+    _need(tuple(y.shape) == (rows, width), f"y is {tuple(y.shape)}, not {(rows, width)}")
+    group = 0
+    if scale is None:
+        _like("y", y, x)
+    else:
+        _tensor("scale", scale, 2, _E8)
+        _need(scale.shape[1] > 0 and width % scale.shape[1] == 0, f"{scale.shape[1]} scales for rows of {width}")
+        group = width // scale.shape[1]
+        _dense("scale", scale, (rows, width // group), _E8)
+    return _made(STEP_NORM, daris_norm(_at(x), _at(res), _at(weight), _at(sum), _at(y), _at(scale), x.stride(0), res.stride(0) if res is not None else 0,
+                                       sum.stride(0) if sum is not None else 0, y.stride(0), rows, width, group, _dtype(x), eps), x, weight, y, res, sum, scale)
+
+
+def make_cache(k, v, k_scale, v_scale, pages, before):
+    """A paged cache (see daris_cache): k [pages][heads][64][dim] and v [pages][heads][dim][64] in float8_e4m3fn, scales [pages][heads][4],
+    pages int32 [sequences][entries], before int32 [sequences]."""
+    _tensor("k", k, 4, _F8)
+    n, h, _, d = k.shape
+    _dense("k", k, (n, h, PAGE_TOKENS, d), _F8)
+    _dense("v", v, (n, h, d, PAGE_TOKENS), _F8)
+    _dense("k_scale", k_scale, (n, h, PAGE_TOKENS // SCALE_TOKENS), _E8)
+    _dense("v_scale", v_scale, (n, h, PAGE_TOKENS // SCALE_TOKENS), _E8)
+    _tensor("pages", pages, 2, ("int32",))
+    _dense("before", before, (pages.shape[0],), ("int32",))
+    _need(pages.shape[0] <= 1 or pages.stride(0) == pages.shape[1], "pages is not contiguous")
+    c = daris_cache(_at(k), _at(v), _at(k_scale), _at(v_scale), _at(pages), _at(before), pages.shape[1], n, pages.shape[0], h, d)
+    c.keep = (k, v, k_scale, v_scale, pages, before)
+    return c
+
+
+def _rows(cache, name, t, row_start, heads=None):
+    _tensor(name, t, 3, _ACT)
+    _need(t.shape[2] == cache.dim, f"{name} has heads of {t.shape[2]}, the cache of {cache.dim}")
+    _need(heads is None or t.shape[1] == heads, f"{name} has {t.shape[1]} heads, not {heads}")
+    if row_start is not None:
+        _dense("row_start", row_start, (cache.n_seqs + 1,), ("int32",))
+    return t
+
+
+def make_append(cache, k, v, row_start=None, q=None, q_out=None, turn=None, rot_dim=0, pairs=False):
+    """Appends rows k, v [rows][heads][dim] to the cache, keys and q -> q_out turned by turn [positions][rot_dim] (see daris_append)."""
+    _rows(cache, "k", k, row_start, cache.kv_heads)
+    _like("v", _rows(cache, "v", v, row_start, cache.kv_heads), k)
+    _need(v.shape[0] == k.shape[0], f"{v.shape[0]} rows of v, {k.shape[0]} of k")
+    _need((q is None) == (q_out is None), "q and q_out go together")
+    for name, t in (("q", q), ("q_out", q_out)):
+        if t is not None:
+            _need(_like(name, _rows(cache, name, t, row_start, q.shape[1]), k).shape[0] == k.shape[0], f"{t.shape[0]} rows of {name}, {k.shape[0]} of k")
+    if turn is not None:
+        _dense("turn", turn, (turn.shape[0], rot_dim), ("float32",))
+    _need(turn is not None or rot_dim == 0, "no table of angles")
+    z = (0, 0, 0)
+    a = daris_append(cache, _at(k), _at(v), _at(q), _at(q_out), _at(turn), _at(row_start), *k.stride()[:2], *v.stride()[:2], *(q.stride() if q is not None else z)[:2],
+                     *(q_out.stride() if q is not None else z)[:2], k.shape[0], q.shape[1] if q is not None else 0, _dtype(k), turn.shape[0] if turn is not None else 0, rot_dim, int(pairs))
+    return _made(STEP_APPEND, a, cache, k, v, q, q_out, turn, row_start)
+
+
+def make_attend(cache, q, out, row_start=None, scale=1.0, window=0):
+    """out = attention of q [rows][heads][dim] over the cache (see daris_attend)."""
+    _rows(cache, "q", q, row_start)
+    _need(_like("out", _rows(cache, "out", out, row_start, q.shape[1]), q).shape[0] == q.shape[0], f"{out.shape[0]} rows of out, {q.shape[0]} of q")
+    a = daris_attend(cache, _at(q), _at(out), _at(row_start), *q.stride()[:2], *out.stride()[:2], q.shape[0], q.shape[1], _dtype(q), window, scale)
+    return _made(STEP_ATTEND, a, cache, q, out, row_start)
+
+
+def make_matvec(x, w, w_scale, y, x_scale=None, gate=False):
+    """y [rows][n] = x [rows][k] times 4-bit weights w [n][k / 2] (uint8) with scales w_scale [n][k / group] (bfloat16); x in float8_e4m3fn with
+    x_scale [rows][k / group]; gate: y [rows][n / 2] (see daris_matvec)."""
+    _tensor("x", x, 2, _F8 if x_scale is not None else _ACT)
+    _tensor("w", w, 2, ("uint8",))
+    rows, k = x.shape
+    n = w.shape[0]
+    _need(k == 2 * w.shape[1], f"x has {k} channels, w {2 * w.shape[1]}")
+    _tensor("w_scale", w_scale, 2, ("bfloat16",))
+    _need(w_scale.shape[1] > 0 and k % w_scale.shape[1] == 0, f"{w_scale.shape[1]} scales for {k} channels")
+    group = k // w_scale.shape[1]
+    _dense("w_scale", w_scale, (n, k // group), ("bfloat16",))
+    if x_scale is not None:
+        _dense("x_scale", x_scale, (rows, k // group), _E8)
+    _tensor("y", y, 2, _ACT)
+    _need(x_scale is not None or y.dtype == x.dtype, f"y is of {y.dtype}, not {x.dtype}")
+    _need(tuple(y.shape) == (rows, n // 2 if gate else n), f"y is {tuple(y.shape)}, not {(rows, n // 2 if gate else n)}")
+    a = daris_matvec(_at(x), _at(x_scale), _at(w), _at(w_scale), _at(y), x.stride(0), w.stride(0), y.stride(0), rows, n, k, group, _dtype(y), int(gate))
+    return _made(STEP_MATVEC, a, x, w, w_scale, y, x_scale)
+
+
+def make_ops(ops):
+    """Operators in the order in which they run, as daris_run_ops takes them; a program keeps it from step to step."""
+    a = (daris_op * len(ops))(*ops)
+    a.keep = tuple(o.keep for o in ops)
+    return a
+
+
+def daris_run_ops(ops, p=0):
+    """Runs what make_ops made on partition p and waits for it."""
+    return _chk(lib().daris_run_ops(ops, len(ops), p))

@@ -12,6 +12,8 @@ DEVICE_SOURCES = {"kernels.hip": "daris_kernels", "taps_kernels.hip": "daris_tap
                   "point_kernels.hip": "daris_point_kernels"}
 # ... of the kernels that compute several layers in a row
 JOINED_SOURCES = {"joined_kernels.hip": "daris_joined_kernels", "tall_kernels.hip": "daris_tall_kernels", "pointwise_kernels.hip": "daris_pointwise_kernels"}
+# ... of the operators of a generation step
+STEP_SOURCES = {"step_kernels.hip": "daris_step_kernels", "attend_kernels.hip": "daris_attend_kernels"}
 HOST_SOURCES = ["aql.cpp", "launch.cpp", "sched_core.cpp", "net_plan.cpp", "net_encode.cpp", "daris_api.cpp"]
 COMMON = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-Wall", "-Wno-unused-function"]
 # no packed fp32 arithmetic in device code (some forms have given wrong results on this hardware)
@@ -40,7 +42,7 @@ def _run(cmd, verbose):
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     asm = ""
-    for src, name in {**DEVICE_SOURCES, **JOINED_SOURCES}.items():
+    for src, name in {**DEVICE_SOURCES, **JOINED_SOURCES, **STEP_SOURCES}.items():
         code_object = os.path.join(CSRC, name + ".co")
         _run([hipcc] + DEVICE_FLAGS + ["-c", os.path.join(CSRC, src), "-o", code_object], verbose)
         asm += BLOB_ASM.format(name=name, path=code_object)

@@ -1,0 +1,556 @@
+// Attention over the paged e4m3 cache with a running maximum and sum: one pass over the pages, scores and weights in registers only.
+//
+// Work. A tile is 16 (narrow) or 128 (wide: 32 a wave) columns; a column is one query head of one row, and all columns of a tile
+// read the same key head, so that every page is fetched once for the whole group.  The tiles of all sequences times their visible
+// pages are cut into units of equal numbers of pages -- the kernel reads the lengths itself, so the cut fits them whatever the table's
+// width and however unequal they are -- and a workgroup takes one.  Units of one tile leave their unnormalised sums in the
+// workspace; the workgroup that arrives last adds them in unit order, so the result does not depend on the order of arrival.
+//
+// Operands. Scores are S^T = K Q^T and outputs O^T = V^T P^T: a lane then holds sixteen scores of ONE column, namely of sixteen
+// neighbouring tokens (the rows of the K tile are permuted so), which are the weights it has to supply to the second product: no
+// exchange between lanes but for the maximum.  Sixteen tokens share a scale, so a lane needs one scale of K and one of V a page.
+// Keys [token][channel] and values [channel][token] are loaded in the operands' own order, 16 bytes a lane, and spread from
+// e4m3 to f16 two at a time (exact).  Queries are divided by a power of two that brings their largest number to 2^14, in one f16 part
+// (bf16) or two (fp32).  The scale of V joins the exponent: w = 2^(s + log2(scale_v) - M + 14), M the running maximum
+// of s + log2(scale_v): w fits f16 whatever the scales are, and the sum of weights takes 1 / scale_v back out.
+//
+// Masks cost nothing on pages that all columns see.  On the others scores are selected away, values that no column sees are cleared, and
+// where a NaN code is left, whose product with a zero weight would spoil other columns, the values' NaNs are counted apart.
+//
+// Narrow tiles are bound by the bytes of the cache, wide ones by the matrix pipe and the exponentials.
+#pragma once
+#include "step_common.h"
+
+namespace daris {
+
+constexpr float kWeightBits = 14.f;
+
+// What a workgroup has to do.
+struct Unit {
+  int s = 0, tile = 0, chunk = 0, chunks = 0, per = 0;  // per: pages of a unit
+  int first = 0;                                        // number of the tile's first unit
+  int row0 = 0, rows = 0, before = 0;
+};
+
+// Pages that any row of sequence s sees: [*lo, return value).
+__device__ __forceinline__ int seen_pages(const AttendArgs& a, int rows, int before, int* lo) {
+  const int end = before + rows;
+  int from = a.window > 0 && before >= a.window ? before - a.window + 1 : 0;
+  from /= kPage;
+  *lo = from;
+  if (end <= 0 || rows == 0) return from;
+  int to = (end + kPage - 1) / kPage;
+  if (to > a.c.pages_row) to = (int)a.c.pages_row;
+  return to < from ? from : to;
+}
+
+// Every wave finds the workgroup's unit by itself, 64 sequences at a time.  False: nothing to do.
+template <int TILE, int MOST>
+__device__ __forceinline__ bool find_unit(const AttendArgs& a, int unit, Unit* u) {
+  const int lane = threadIdx.x & 63, ns = a.c.n_seqs;
+  int row0 = 0, rows = 0, before = 0, tiles = 0, pages = 0;
+  auto look = [&](int s) {
+    row0 = rows = before = tiles = pages = 0;
+    if (s < ns) {
+      row0 = first_row(a.c, s);
+      rows = rows_of(a.c, s);
+      before = tokens_before(a.c, s);
+      tiles = (int)(((int64_t)rows * a.group + TILE - 1) / TILE);
+      int lo;
+      pages = seen_pages(a, rows, before, &lo);
+      pages -= lo;
+    }
+  };
+  float work = 0.f, most = 0.f;
+  for (int s0 = 0; s0 < ns; s0 += 64) {
+    look(s0 + lane);
+    work += wave_sum<64>((float)tiles * (float)pages);
+    most = fmaxf(most, wave_max<64>((float)pages));
+  }
+  // pages of a unit: what makes `target` of them, a little more so that rounding never makes too many; the merge holds MOST of a tile
+  float per = a.target > 0 ? ceilf(work * 1.0001f / (float)a.target) : most;
+  per = fmaxf(per, ceilf(most * (1.f / MOST)));
+  int c = (int)fminf(per, 1.0e9f);
+  c = c < 1 ? 1 : c;
+  c = (c + 3) / 4 * 4;
+  int base = 0;
+  for (int s0 = 0; s0 < ns; s0 += 64) {
+    if (ns > 64) look(s0 + lane);
+    const int chunks = tiles == 0 ? 0 : pages <= c ? 1 : (pages + c - 1) / c;
+    const int mine = tiles * chunks;
+    int upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int o = __shfl_up(upto, d);
+      if (lane >= d) upto += o;
+    }
+    const int start = base + upto - mine;
+    const uint64_t hit = __ballot(unit >= start && unit < start + mine);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      u->s = s0 + l;
+      u->chunks = uniform(__shfl(chunks, l));
+      const int in = unit - uniform(__shfl(start, l));
+      u->tile = in / u->chunks;
+      u->chunk = in - u->tile * u->chunks;
+      u->first = unit - u->chunk;
+      u->per = c;
+      u->row0 = uniform(__shfl(row0, l));
+      u->rows = uniform(__shfl(rows, l));
+      u->before = uniform(__shfl(before, l));
+      return true;
+    }
+    base += uniform(__shfl(upto, 63));
+  }
+  return false;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ bool has_nan_code(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; }
+// 0xff in the bytes that hold the NaN code
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+  const uint32_t top = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  return (top >> 7) * 0xffu;
+}
+
+// One wave's columns, TILE = 16 or 32 of them, and its running sums.
+template <bool BF16, int D, int TILE>
+struct Columns {
+  static constexpr int PARTS = BF16 ? 1 : 2;
+  static constexpr int G = 64 / TILE;            // lanes of a column
+  static constexpr int DEPTH = TILE == 16 ? 32 : 16;  // channels (tokens) of a matrix instruction
+  static constexpr int KT = kPage / TILE;        // score tiles of a page
+  static constexpr int KS = D / DEPTH;           // matrix instructions of a score tile
+  static constexpr int VT = D / TILE;            // output tiles
+  static constexpr int R = TILE * TILE / 64;     // numbers of a tile in a lane
+  static constexpr int KV = D / G / 16;          // 16-byte pieces of a key in a lane
+  static constexpr int HALVES = kPage / (16 * G);  // sixteenths of a page in a lane
+  using Acc = typename std::conditional<TILE == 16, f32x4, f32x16>::type;
+  static __device__ __forceinline__ Acc mma(const f16x8& x, const f16x8& y, const Acc& z) {
+    if constexpr (TILE == 16) return mfma16(x, y, z);
+    else return mfma32(x, y, z);
+  }
+
+  f16x8 q[PARTS][KS];
+  Acc o[VT];
+  float top, sum;   // M; the lane's share of the sum of weights
+  float factor;     // of a score: scale * log2(e) / the queries' power of two
+  int pos;          // position of the column's row
+  int lane, c, g;
+
+  // columns col0 .. of `rows` rows; those behind the last repeat it and are not stored
+  __device__ __forceinline__ void start(const AttendArgs& a, const Unit& u, int head, int col0) {
+    lane = threadIdx.x & 63;
+    c = lane & (TILE - 1);
+    g = lane / TILE;
+    const int cols = u.rows * a.group;
+    const int col = col0 + c < cols ? col0 + c : cols - 1;
+    const int r = col / a.group;
+    pos = u.before + r;
+    const int64_t at = (int64_t)(u.row0 + r) * a.q_row + (int64_t)(head * a.group + (col - r * a.group)) * a.q_head + g * (D / G);
+    float x[KS][8];
+    float most = 0.f;
+#pragma unroll
+    for (int j = 0; j < KS; ++j) {
+      if (a.q_vec) {
+        if (BF16) {
+          unpack<true>(*(const uint4*)((const uint16_t*)a.q + at + 8 * j), x[j]);
+        } else {
+          float lo[4], hi[4];
+          unpack<false>(*(const uint4*)((const float*)a.q + at + 8 * j), lo);
+          unpack<false>(*(const uint4*)((const float*)a.q + at + 8 * j + 4), hi);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[j][e] = lo[e];
+            x[j][e + 4] = hi[e];
+          }
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[j][e] = load_elem<BF16>(a.q, at + 8 * j + e);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < KS; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = fmaxf(most, size_of(x[j][e]));
+#pragma unroll
+    for (int m = TILE; m < 64; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+    int up = 141 - (int)(__float_as_uint(most) >> 23);
+    up = up > 110 ? 110 : up;
+#pragma unroll
+    for (int j = 0; j < KS; ++j) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = __builtin_amdgcn_ldexpf(x[j][e], up);
+        q[0][j][e] = (_Float16)v;
+        if (PARTS == 2) q[PARTS - 1][j][e] = is_finite(v) ? (_Float16)(v - (float)q[0][j][e]) : (_Float16)0.f;
+      }
+    }
+    factor = a.scale * two_to(-up);
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+      for (int i = 0; i < R; ++i) o[t][i] = 0.f;
+    top = -INFINITY;
+    sum = 0.f;
+  }
+
+  // token of a page that row r of score tile t is: a lane's numbers of the tiles are then neighbouring tokens
+  static __device__ __forceinline__ int token_of(int t, int r) {
+    if (TILE == 16) return (r >> 2) * 16 + t * 4 + (r & 3);
+    return t * 32 + ((r >> 2) & 1) * 16 + (r >> 3) * 4 + (r & 3);
+  }
+  // first of the 16 tokens whose scores tile group `half` leaves in this lane, and the sixteenth they are
+  __device__ __forceinline__ int sixteenth(int half) const { return TILE == 16 ? g : half * 2 + g; }
+
+  struct Page {
+    uint4 k[KT][KV];
+    uint4 v[VT][HALVES];
+    uint32_t ks, vs;  // four scale bytes each
+  };
+  __device__ __forceinline__ void fetch(const AttendArgs& a, int head, int page, Page* p) const {
+    const int64_t ph = (int64_t)page * a.c.kv_heads + head;
+    p->ks = *(const uint32_t*)(a.c.k_scale + ph * 4);
+    p->vs = *(const uint32_t*)(a.c.v_scale + ph * 4);
+    const uint8_t* k = a.c.k + ph * (kPage * D) + g * (D / G);
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int i = 0; i < KV; ++i) p->k[t][i] = *(const uint4*)(k + token_of(t, c) * D + i * 16);
+    const uint8_t* v = a.c.v + ph * (kPage * D) + c * kPage;
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) p->v[t][h] = *(const uint4*)(v + t * TILE * kPage + sixteenth(h) * 16);
+  }
+
+  // The page that starts at token t0.  masked: some column does not see all of it; [see_lo, see_hi]: tokens that any column sees.
+  __device__ __forceinline__ void take(const AttendArgs& a, Page& p, int t0, bool masked, int see_lo, int see_hi) {
+    Acc s[KT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) s[t][i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < KS; ++j) {
+        const uint4& w = p.k[t][j >> 1];
+        const f16x8 k = j & 1 ? f16_of_codes(w.z, w.w) : f16_of_codes(w.x, w.y);
+        if (PARTS == 2) s[t] = mma(k, q[PARTS - 1][j], s[t]);
+        s[t] = mma(k, q[0][j], s[t]);
+      }
+    }
+    // scores in powers of two, with the values' scale
+    constexpr int PER = 16 / R;  // score tiles of a sixteenth (16-column tiles: four; 32: one)
+    float big = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      const int part = sixteenth(t / PER);
+      const float f = factor * two_to((int)((p.ks >> (8 * part)) & 0xff) - 127), v = (float)((int)((p.vs >> (8 * part)) & 0xff) - 127);
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        float x = fmaf(s[t][i], f, v);
+        if (masked) {
+          const int token = t0 + part * 16 + (t % PER) * R + i;
+          const bool on = token <= pos && (a.window == 0 || token > pos - a.window);
+          x = on ? x : -INFINITY;
+        }
+        s[t][i] = x;
+        big = fmaxf(big, x);
+      }
+    }
+#pragma unroll
+    for (int m = TILE; m < 64; m *= 2) big = fmaxf(big, __shfl_xor(big, m));
+    const float now = fmaxf(top, big);
+    if (__any(now != top)) {
+      const float shrink = now == top ? 1.f : exp2_fast(top - now);
+#pragma unroll
+      for (int t = 0; t < VT; ++t)
+#pragma unroll
+        for (int i = 0; i < R; ++i) o[t][i] *= shrink;
+      sum *= shrink;
+      top = now;
+    }
+    const float base = (top == -INFINITY ? 0.f : top) - kWeightBits;
+    f16x8 w[PARTS][kPage / (8 * G)];
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+      float add = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int t = h * PER + e / R;
+        const float x = exp2_fast(s[t][e % R] - base);
+        add += x;
+        const _Float16 hi = (_Float16)x;
+        w[0][h * 2 + (e >> 3)][e & 7] = hi;
+        if (PARTS == 2) w[PARTS - 1][h * 2 + (e >> 3)][e & 7] = (_Float16)(x - (float)hi);
+      }
+      sum = fmaf(add, two_to(127 - (int)((p.vs >> (8 * sixteenth(h))) & 0xff)), sum);
+    }
+    bool odd = false;
+    if (masked) {
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) {
+        const int t1 = t0 + sixteenth(h) * 16;
+        uint32_t keep[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          keep[i] = 0u;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) keep[i] |= t1 + 4 * i + b >= see_lo && t1 + 4 * i + b <= see_hi ? 0xffu << (8 * b) : 0u;
+        }
+#pragma unroll
+        for (int t = 0; t < VT; ++t) {
+          uint4& x = p.v[t][h];
+          x.x &= keep[0];
+          x.y &= keep[1];
+          x.z &= keep[2];
+          x.w &= keep[3];
+          odd = odd || has_nan_code(x.x) || has_nan_code(x.y) || has_nan_code(x.z) || has_nan_code(x.w);
+        }
+      }
+      odd = __any(odd);
+    }
+    if (odd) {
+      // NaN codes as numbers 1.0 (0x38), times 1 where the column sees the token: more than 0 makes the output NaN
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) {
+        f16x8 see[2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int token = t0 + sixteenth(h) * 16 + e;
+          see[e >> 3][e & 7] = token <= pos && (a.window == 0 || token > pos - a.window) ? (_Float16)1.f : (_Float16)0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < VT; ++t) {
+          uint4& x = p.v[t][h];
+          const uint4 n = make_uint4(nan_bytes(x.x), nan_bytes(x.y), nan_bytes(x.z), nan_bytes(x.w));
+          Acc count;
+#pragma unroll
+          for (int i = 0; i < R; ++i) count[i] = 0.f;
+          count = mma(f16_of_codes(n.x & 0x38383838u, n.y & 0x38383838u), see[0], count);
+          count = mma(f16_of_codes(n.z & 0x38383838u, n.w & 0x38383838u), see[1], count);
+#pragma unroll
+          for (int i = 0; i < R; ++i) o[t][i] = count[i] > 0.f ? __uint_as_float(0x7fc00000u) : o[t][i];
+          x = make_uint4(x.x & ~n.x, x.y & ~n.y, x.z & ~n.z, x.w & ~n.w);
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) {
+        const f16x8 lo = f16_of_codes(p.v[t][h].x, p.v[t][h].y), hi = f16_of_codes(p.v[t][h].z, p.v[t][h].w);
+        if (PARTS == 2) {
+          o[t] = mma(lo, w[PARTS - 1][h * 2], o[t]);
+          o[t] = mma(hi, w[PARTS - 1][h * 2 + 1], o[t]);
+        }
+        o[t] = mma(lo, w[0][h * 2], o[t]);
+        o[t] = mma(hi, w[0][h * 2 + 1], o[t]);
+      }
+  }
+
+  // Pages [lo, hi) of the sequence, every `stride`-th; the page numbers of 64 of them are read at a time.
+  __device__ __forceinline__ void run(const AttendArgs& a, const Unit& u, int head, int lo, int hi, int stride, int pos_lo, int pos_hi) {
+    const int see_lo = a.window > 0 ? pos_lo - a.window + 1 : 0, see_hi = pos_hi;
+    for (int base = lo; base < hi; base += 64 * stride) {
+      const int at = base + lane * stride;
+      const int mine = at < hi ? page_of(a.c, u.s, at) : -1;
+      const int n = (hi - base + stride - 1) / stride < 64 ? (hi - base + stride - 1) / stride : 64;
+      for (int i = 0; i < n; ++i) {
+        const int page = __builtin_amdgcn_readlane(mine, i);
+        if (page < 0) continue;
+        const int t0 = (base + i * stride) * kPage;
+        Page p;
+        fetch(a, head, page, &p);
+        const bool masked = t0 + kPage - 1 > pos_lo || (a.window > 0 && t0 <= pos_hi - a.window);
+        take(a, p, t0, masked, see_lo, see_hi);
+      }
+    }
+    // the lanes of a column add their shares
+#pragma unroll
+    for (int m = TILE; m < 64; m *= 2) sum += __shfl_xor(sum, m);
+  }
+  // first channel of the four (of neighbouring numbers r .. r + 3) that o[t][r] begins
+  __device__ __forceinline__ int channel(int t, int r) const { return TILE == 16 ? t * 16 + g * 4 : t * 32 + (r >> 2) * 8 + g * 4; }
+};
+
+template <bool BF16>
+__device__ __forceinline__ void put_out(const AttendArgs& a, int64_t at, const float4& v) {
+  if (a.out_vec) {
+    if (BF16) *(uint2*)((uint16_t*)a.out + at) = make_uint2(pack_bf16_rne(v.x, v.y), pack_bf16_rne(v.z, v.w));
+    else *(float4*)((float*)a.out + at) = v;
+  } else {
+    const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (BF16) ((uint16_t*)a.out)[at + i] = (uint16_t)f32_to_bf16_bits(x[i]);
+      else ((float*)a.out)[at + i] = x[i];
+    }
+  }
+}
+
+// Sums of a tile that several units share, in the workspace: [unit][COLS][D] numbers, then [unit][COLS] pairs (M, sum).
+template <int COLS, int D>
+__device__ __forceinline__ float* part_numbers(const AttendArgs& a, int head, int unit) {
+  return a.part + (int64_t)(head * a.units + unit) * (COLS * (D + 2));
+}
+
+// Whether this workgroup is the last of the tile's units (its sums are in the workspace already).
+__device__ __forceinline__ bool arrive(const AttendArgs& a, int head, const Unit& u, int* lds) {
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t* n = a.count + (int64_t)head * a.units + u.first;
+    const uint32_t before = __hip_atomic_fetch_add(n, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    const bool last = before == (uint32_t)u.chunks - 1;
+    if (last) __hip_atomic_store(n, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *lds = last;
+  }
+  __syncthreads();
+  const bool last = *lds != 0;
+  if (last) __threadfence();
+  return last;
+}
+
+template <int COLS, int D, bool BF16>
+__device__ __forceinline__ void merge(const AttendArgs& a, int head, const Unit& u, int col0, float* lds) {
+  // lds [chunks][COLS]: what each unit's sums are multiplied with
+  const int tid = threadIdx.x, cols = u.rows * a.group - col0 < COLS ? u.rows * a.group - col0 : COLS;
+  const float* part = part_numbers<COLS, D>(a, head, u.first);
+  constexpr int STEP = COLS * (D + 2);
+  for (int c = tid; c < cols; c += 256) {
+    float top = -INFINITY, sum = 0.f;
+    for (int k = 0; k < u.chunks; ++k) top = fmaxf(top, part[(int64_t)k * STEP + COLS * D + 2 * c]);
+    const float base = top == -INFINITY ? 0.f : top;
+    for (int k = 0; k < u.chunks; ++k) {
+      const float w = exp2_fast(part[(int64_t)k * STEP + COLS * D + 2 * c] - base);
+      sum = fmaf(w, part[(int64_t)k * STEP + COLS * D + 2 * c + 1], sum);
+      lds[k * COLS + c] = w;
+    }
+    const float back = sum == 0.f ? 0.f : 1.f / sum;
+    for (int k = 0; k < u.chunks; ++k) lds[k * COLS + c] *= back;
+  }
+  __syncthreads();
+  for (int i = tid; i < cols * (D / 4); i += 256) {
+    const int c = i / (D / 4), d = (i - c * (D / 4)) * 4;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int k = 0; k < u.chunks; ++k) {
+      const float w = lds[k * COLS + c];
+      const float4 v = *(const float4*)(part + (int64_t)k * STEP + c * D + d);
+      s.x = fmaf(w, v.x, s.x);
+      s.y = fmaf(w, v.y, s.y);
+      s.z = fmaf(w, v.z, s.z);
+      s.w = fmaf(w, v.w, s.w);
+    }
+    const int col = col0 + c, r = col / a.group;
+    put_out<BF16>(a, (int64_t)(u.row0 + r) * a.out_row + (int64_t)(head * a.group + (col - r * a.group)) * a.out_head + d, s);
+  }
+}
+
+// Four waves on the pages of one 16-column tile, every fourth each.
+template <bool BF16, int D>
+__device__ __forceinline__ void attend_narrow_body(const AttendArgs& a) {
+  constexpr int COLS = 16, MOST = kNarrowUnits, PITCH = D + 4;
+  extern __shared__ float4 smem4[];
+  float* lds = (float*)smem4;  // [4][16][PITCH] sums, [4][16] M, [4][16] sums of weights; later the merge's factors
+  float* tops = lds + 4 * COLS * PITCH;
+  float* sums = tops + 4 * COLS;
+  int* flag = (int*)(sums + 4 * COLS);
+  const int head = blockIdx.x % a.c.kv_heads, tid = threadIdx.x, wave = uniform(tid >> 6);
+  Unit u;
+  if (!find_unit<COLS, MOST>(a, blockIdx.x / a.c.kv_heads, &u)) return;
+  const int col0 = u.tile * COLS, cols = u.rows * a.group - col0 < COLS ? u.rows * a.group - col0 : COLS;
+  const int pos_lo = u.before + col0 / a.group, pos_hi = u.before + (col0 + cols - 1) / a.group;
+  Columns<BF16, D, COLS> w;
+  w.start(a, u, head, col0);
+  int lo, hi = seen_pages(a, u.rows, u.before, &lo);
+  lo += u.chunk * u.per;
+  hi = hi < lo + u.per ? hi : lo + u.per;
+  const int end = pos_hi < 0 ? 0 : pos_hi / kPage + 1;
+  w.run(a, u, head, lo + wave, hi < end ? hi : end, 4, pos_lo, pos_hi);
+  if (w.lane < COLS) {
+    tops[wave * COLS + w.c] = w.top;
+    sums[wave * COLS + w.c] = w.sum;
+  }
+#pragma unroll
+  for (int t = 0; t < D / COLS; ++t) *(float4*)(lds + (wave * COLS + w.c) * PITCH + w.channel(t, 0)) = make_float4(w.o[t][0], w.o[t][1], w.o[t][2], w.o[t][3]);
+  __syncthreads();
+  float* part = part_numbers<COLS, D>(a, head, u.first + u.chunk);
+  for (int i = tid; i < cols * (D / 4); i += 256) {
+    const int c = i / (D / 4), d = (i - c * (D / 4)) * 4;
+    float top = tops[c], sum = 0.f;
+#pragma unroll
+    for (int k = 1; k < 4; ++k) top = fmaxf(top, tops[k * COLS + c]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float f = exp2_fast(tops[k * COLS + c] - base);
+      const float4 v = *(const float4*)(lds + (k * COLS + c) * PITCH + d);
+      sum = fmaf(f, sums[k * COLS + c], sum);
+      s.x = fmaf(f, v.x, s.x);
+      s.y = fmaf(f, v.y, s.y);
+      s.z = fmaf(f, v.z, s.z);
+      s.w = fmaf(f, v.w, s.w);
+    }
+    if (u.chunks == 1) {
+      const float back = sum == 0.f ? 0.f : 1.f / sum;
+      s.x *= back;
+      s.y *= back;
+      s.z *= back;
+      s.w *= back;
+      const int col = col0 + c, r = col / a.group;
+      put_out<BF16>(a, (int64_t)(u.row0 + r) * a.out_row + (int64_t)(head * a.group + (col - r * a.group)) * a.out_head + d, s);
+    } else {
+      *(float4*)(part + c * D + d) = s;
+      if (d == 0) *(float2*)(part + COLS * D + 2 * c) = make_float2(top, sum);
+    }
+  }
+  if (u.chunks > 1 && arrive(a, head, u, flag)) merge<COLS, D, BF16>(a, head, u, col0, lds);
+}
+
+// Four waves side by side on 32 columns each, all on the same pages (which they fetch one after the other from the CU's cache).
+template <bool BF16, int D>
+__device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
+  constexpr int COLS = 128, MOST = kWideUnits;
+  extern __shared__ float4 smem4[];
+  float* lds = (float*)smem4;  // the merge's factors [MOST][128], then a flag
+  int* flag = (int*)(lds + MOST * COLS);
+  const int head = blockIdx.x % a.c.kv_heads, wave = uniform(threadIdx.x >> 6);
+  Unit u;
+  if (!find_unit<COLS, MOST>(a, blockIdx.x / a.c.kv_heads, &u)) return;
+  const int all = u.rows * a.group, col0 = u.tile * COLS + wave * 32;
+  if (col0 < all) {
+    const int cols = all - col0 < 32 ? all - col0 : 32;
+    const int pos_lo = u.before + col0 / a.group, pos_hi = u.before + (col0 + cols - 1) / a.group;
+    Columns<BF16, D, 32> w;
+    w.start(a, u, head, col0);
+    int lo, hi = seen_pages(a, u.rows, u.before, &lo);
+    lo += u.chunk * u.per;
+    hi = hi < lo + u.per ? hi : lo + u.per;
+    const int end = pos_hi < 0 ? 0 : pos_hi / kPage + 1;
+    const int from = a.window > 0 && pos_lo >= a.window ? (pos_lo - a.window + 1) / kPage : 0;
+    w.run(a, u, head, lo > from ? lo : from, hi < end ? hi : end, 1, pos_lo, pos_hi);
+    const bool on = w.c < cols;
+    const int col = col0 + (on ? w.c : 0), r = col / a.group;
+    const int64_t at = (int64_t)(u.row0 + r) * a.out_row + (int64_t)(head * a.group + (col - r * a.group)) * a.out_head;
+    float* part = part_numbers<COLS, D>(a, head, u.first + u.chunk);
+    const float back = u.chunks > 1 ? 1.f : w.sum == 0.f ? 0.f : 1.f / w.sum;
+    if (on) {
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const float4 v = make_float4(w.o[t][i] * back, w.o[t][i + 1] * back, w.o[t][i + 2] * back, w.o[t][i + 3] * back);
+          if (u.chunks == 1) put_out<BF16>(a, at + w.channel(t, i), v);
+          else *(float4*)(part + (wave * 32 + w.c) * D + w.channel(t, i)) = v;
+        }
+      if (u.chunks > 1 && w.g == 0) *(float2*)(part + COLS * D + 2 * (wave * 32 + w.c)) = make_float2(w.top, w.sum);
+    }
+  }
+  if (u.chunks > 1 && arrive(a, head, u, flag)) merge<COLS, D, BF16>(a, head, u, u.tile * COLS, lds);
+}
+
+}  // namespace daris

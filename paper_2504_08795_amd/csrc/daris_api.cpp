@@ -25,12 +25,14 @@
 
 #include "../../include/daris.h"
 #include "../../include/daris_debug.h"
+#include "../../include/daris_ops.h"
 #include "aql.h"
 #include "kernels.h"
 #include "net_encode.h"
 #include "net_plan.h"
 #include "sched_core.h"
 #include "static_scratch.h"
+#include "step_encode.h"
 
 using namespace daris;
 
@@ -51,6 +53,11 @@ extern "C" const char daris_tall_kernels_co[];
 extern "C" const char daris_tall_kernels_co_end[];
 extern "C" const char daris_point_kernels_co[];
 extern "C" const char daris_point_kernels_co_end[];
+// ... and those of the operators of a generation step (step_kernels.hip, attend_kernels.hip)
+extern "C" const char daris_step_kernels_co[];
+extern "C" const char daris_step_kernels_co_end[];
+extern "C" const char daris_attend_kernels_co[];
+extern "C" const char daris_attend_kernels_co_end[];
 
 namespace {
 
@@ -135,6 +142,10 @@ struct PartRt {
   int n_cu = 0, start = 0, n_streams = 1;
   uint32_t mask[8] = {0};
   std::vector<std::shared_ptr<StreamRt>> streams;
+  // workspace of daris_run_ops: partial results, and counters that are zero whenever no operator runs
+  void* step_part = nullptr;
+  uint32_t* step_count = nullptr;
+  size_t step_part_bytes = 0, step_counters = 0;
 };
 
 struct VtEvent {
@@ -209,6 +220,7 @@ bool on_own_device(const void* p) {
 AqlRuntime g_rt;
 KernelTable g_kt;
 JoinedTable g_joined;
+StepTable g_steps;
 int g_rt_device = -1;
 
 bool wave_prio(const TaskRt& T) { return T.prio == DARIS_HP && (G->flags & DARIS_WAVE_PRIORITY); }
@@ -746,10 +758,13 @@ daris_status daris_init(int device, uint64_t seed, int flags) {
                                {daris_joined_kernels_co, (size_t)(daris_joined_kernels_co_end - daris_joined_kernels_co)},
                                {daris_pointwise_kernels_co, (size_t)(daris_pointwise_kernels_co_end - daris_pointwise_kernels_co)},
                                {daris_tall_kernels_co, (size_t)(daris_tall_kernels_co_end - daris_tall_kernels_co)},
-                               {daris_point_kernels_co, (size_t)(daris_point_kernels_co_end - daris_point_kernels_co)}});
+                               {daris_point_kernels_co, (size_t)(daris_point_kernels_co_end - daris_point_kernels_co)},
+                               {daris_step_kernels_co, (size_t)(daris_step_kernels_co_end - daris_step_kernels_co)},
+                               {daris_attend_kernels_co, (size_t)(daris_attend_kernels_co_end - daris_attend_kernels_co)}});
       if (err.empty()) {
         err = g_kt.resolve(g_rt);
         if (err.empty()) err = g_joined.resolve(g_rt);
+        if (err.empty()) err = g_steps.resolve(g_rt);
         if (!err.empty()) err = "kernel " + err;
       }
       if (err.empty()) g_rt_device = device;
@@ -806,6 +821,10 @@ daris_status daris_shutdown(void) {
     }
     (void)hipDeviceSynchronize();
     for (auto& T : G->tasks) free_task(*T);
+    for (PartRt& P : G->parts) {
+      if (P.step_part) (void)hipFree(P.step_part);
+      if (P.step_count) (void)hipFree(P.step_count);
+    }
     for (PartRt& P : G->parts)
       for (auto& S : P.streams) {
         if (S->hw) S->hw->q.destroy();  // destroying a shared queue again is a no-op
@@ -1328,6 +1347,86 @@ daris_status daris_forward_static(daris_task t, const void* d_input, void* d_log
   io.in_elsewhere = !on_own_device(d_input);
   // (a packet that is refused leaves launches queued on the static array: run_direct fails for good then)
   return run_direct(T.static_seq, 0, (int)T.static_seq.launches.size(), io, *G->parts[p].streams[0]);
+}
+
+// The partition's workspace holds `bytes` of partial results and `counters` zeros.
+static daris_status step_workspace(PartRt& P, size_t bytes, size_t counters) {
+  // (no operator runs between calls, so what is freed here is not in use)
+  if (bytes > P.step_part_bytes) {
+    if (P.step_part) (void)hipFree(P.step_part);
+    P.step_part = nullptr;
+    P.step_part_bytes = 0;
+    hipError_t e = hipMalloc(&P.step_part, bytes);
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      P.step_part = nullptr;
+      return fail(DARIS_ENOMEM, "workspace of %zu bytes: %s", bytes, hipGetErrorString(e));
+    }
+    P.step_part_bytes = bytes;
+  }
+  if (counters > P.step_counters) {
+    if (P.step_count) (void)hipFree(P.step_count);
+    P.step_count = nullptr;
+    P.step_counters = 0;
+    hipError_t e = hipMalloc((void**)&P.step_count, counters * sizeof(uint32_t));
+    if (e == hipSuccess) e = hipMemset(P.step_count, 0, counters * sizeof(uint32_t));
+    if (e != hipSuccess) {
+      (void)hipGetLastError();
+      if (P.step_count) (void)hipFree(P.step_count);
+      P.step_count = nullptr;
+      return fail(DARIS_ENOMEM, "workspace of %zu counters: %s", counters, hipGetErrorString(e));
+    }
+    P.step_counters = counters;
+  }
+  return DARIS_OK;
+}
+
+daris_status daris_run_ops(const daris_op* ops, int32_t n, daris_part p) try {
+  daris_status st = check_part(p);
+  if (st != DARIS_OK) return st;
+  if (n < 0 || (n > 0 && !ops)) return fail(DARIS_EINVAL, "%d operators at %p", n, (const void*)ops);
+  for (int i = 0; i < n; ++i) {
+    const std::string err = check_step(ops[i]);
+    if (!err.empty()) return fail(DARIS_EINVAL, "operator %d: %s", i, err.c_str());
+  }
+  if (G->nodev) return fail(DARIS_ESTATE, "no device in DARIS_NO_DEVICE mode");
+  st = make_streams();
+  if (st != DARIS_OK) return st;
+  PartRt& P = G->parts[p];
+  std::vector<StepLaunch> ls(n);
+  size_t bytes = 0, counters = 0;
+  int last = -1;
+  for (int i = 0; i < n; ++i) {
+    const std::string err = encode_step(g_steps, ops[i], P.n_cu, &ls[i]);
+    if (!err.empty()) return fail(DARIS_EINVAL, "operator %d: %s", i, err.c_str());
+    bytes = std::max(bytes, ls[i].part_bytes);
+    counters = std::max(counters, ls[i].counters);
+    if (ls[i].groups) last = i;
+  }
+  st = step_workspace(P, bytes, counters);
+  if (st != DARIS_OK) return st;
+  HIP_TRY(hipDeviceSynchronize());  // the caller's streams may still be writing the buffers (see daris_task_set_io)
+  if (last < 0) return DARIS_OK;
+  // The scheduler lock is not held: tasks go on while the operators run.
+  StreamRt& S = *P.streams[0];
+  bool ok = true;
+  {
+    std::lock_guard<std::mutex> ql(S.hw->mu);
+    for (int i = 0; i <= last && ok; ++i) {
+      if (!ls[i].groups) continue;
+      place_step(&ls[i], P.step_part, P.step_count);
+      ok = S.hw->q.dispatch_copy(ls[i].k, ls[i].groups, ls[i].threads, ls[i].args, ls[i].nbytes, i == last ? G->util_sig : hsa_signal_t{0},
+                                 i == last ? AqlQueue::kReleaseSystem : AqlQueue::kReleaseDevice);
+    }
+  }
+  if (!ok || !aql_wait(G->util_sig, &S.hw->q)) {
+    // launches may still run on the caller's buffers and the workspace
+    std::lock_guard<std::mutex> lk(G->mu);
+    return gpu_wait_failed(S, ok ? "operators" : "packet rejected");
+  }
+  return DARIS_OK;
+} catch (const std::bad_alloc&) {
+  return fail(DARIS_ENOMEM, "host memory");
 }
 
 daris_status daris_read_layer(daris_task t, int layer, float* host_out, int64_t cap_elems) {

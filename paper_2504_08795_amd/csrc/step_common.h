@@ -1,0 +1,86 @@
+// Device helpers that the operators of a generation step share: e4m3 numbers under power-of-two scales, f16 operands of the matrix
+// instructions, and where a step's rows belong.
+#pragma once
+#include "device_common.h"
+#include "step_args.h"
+
+namespace daris {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4v __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x4 mfma16(const f16x8& a, const f16x8& b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mfma32(const f16x8& a, const f16x8& b, const f32x16& c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+
+__device__ __forceinline__ f16x8 halves(f16x2 a, f16x2 b, f16x2 c, f16x2 d) {
+  f16x8 v;
+  v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1]; v[4] = c[0]; v[5] = c[1]; v[6] = d[0]; v[7] = d[1];
+  return v;
+}
+
+// Eight e4m3 codes as f16, which holds every one of them.
+__device__ __forceinline__ f16x8 f16_of_codes(uint32_t lo, uint32_t hi) {
+  return halves(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true),
+                __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
+}
+
+__device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u; }
+// |x| for the largest of a group: what is not finite has no part in it.
+__device__ __forceinline__ float size_of(float x) { return is_finite(x) ? fabsf(x) : 0.f; }
+
+// Exponent byte of the smallest power of two s, 2^-100 at least, with most <= 448 s.  448 = 1.75 * 2^8: a mantissa above .75 carries.
+constexpr int kLeastScale = 27;
+__device__ __forceinline__ int scale_byte(float most) {
+  const int e = (int)((__float_as_uint(most) + 0x1fffffu) >> 23) - 8;
+  return e < kLeastScale ? kLeastScale : e;
+}
+__device__ __forceinline__ float two_to(int e) { return __builtin_amdgcn_ldexpf(1.0f, e); }
+
+// x (already divided by its scale) as e4m3 codes, round to nearest even; what is not finite becomes the NaN code.
+__device__ __forceinline__ float code_input(float x) { return is_finite(x) ? x : __uint_as_float(0x7fc00000u); }
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(code_input(a), code_input(b), 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(code_input(c), code_input(d), r, true);
+}
+
+template <int N>
+__device__ __forceinline__ float wave_max(float v) {  // over N neighbouring lanes
+#pragma unroll
+  for (int m = 1; m < N; m *= 2) v = fmaxf(v, __shfl_xor(v, m));
+  return v;
+}
+template <int N>
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int m = 1; m < N; m *= 2) v += __shfl_xor(v, m);
+  return v;
+}
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// ---- where rows belong ---------------------------------------------------------------------------------------------------
+
+// First row of sequence s (s <= n_seqs); whatever the caller's numbers are, one of the buffers' rows.
+__device__ __forceinline__ int first_row(const CacheArgs& c, int s) {
+  if (!c.row_start) return s < c.n_rows ? s : c.n_rows;
+  const int r = c.row_start[s];
+  return r < 0 ? 0 : r > c.n_rows ? c.n_rows : r;
+}
+__device__ __forceinline__ int rows_of(const CacheArgs& c, int s) {
+  const int n = first_row(c, s + 1) - first_row(c, s);
+  return n < 0 ? 0 : n;
+}
+// Tokens in front of the step's, kept away from what would overflow when rows are added.
+__device__ __forceinline__ int tokens_before(const CacheArgs& c, int s) {
+  const int b = c.before[s];
+  return b < -(1 << 30) ? -(1 << 30) : b > (1 << 30) ? (1 << 30) : b;
+}
+// Page of token t >= 0 of sequence s, or -1.
+__device__ __forceinline__ int page_of(const CacheArgs& c, int s, int page) {
+  if (page >= c.pages_row) return -1;
+  const int p = c.pages[(int64_t)s * c.pages_row + page];
+  return p < 0 || p >= c.n_pages ? -1 : p;
+}
+
+}  // namespace daris
