@@ -396,53 +396,95 @@ __device__ __forceinline__ float* part_numbers(const AttendArgs& a, int head, in
   return a.part + (int64_t)(head * a.units + unit) * (COLS * (D + 2));
 }
 
-// Whether this workgroup is the last of the tile's units (its sums are in the workspace already).
+// Whether this workgroup is the last of the tile's units.  What they leave is written through to where all XCDs see it (put) and read
+// from there (take_back), so neither side needs a fence: a release or an acquire of the device writes back or drops a whole L2, and
+// with one for every workgroup 64 streams took 300 us instead of 88.
 __device__ __forceinline__ bool arrive(const AttendArgs& a, int head, const Unit& u, int* lds) {
-  __threadfence();
+  puts_done();
   __syncthreads();
   if (threadIdx.x == 0) {
     uint32_t* n = a.count + (int64_t)head * a.units + u.first;
-    const uint32_t before = __hip_atomic_fetch_add(n, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    const uint32_t before = __hip_atomic_fetch_add(n, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const bool last = before == (uint32_t)u.chunks - 1;
     if (last) __hip_atomic_store(n, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     *lds = last;
   }
   __syncthreads();
-  const bool last = *lds != 0;
-  if (last) __threadfence();
-  return last;
+  return *lds != 0;
 }
+__device__ __forceinline__ float4 take_back(const float* p) {
+  return __builtin_bit_cast(float4, __builtin_amdgcn_global_load_b128((u32x4 __attribute__((address_space(1)))*)p, "agent"));
+}
+__device__ __forceinline__ float2 take_back2(const float* p) {
+  return __builtin_bit_cast(float2, __hip_atomic_load((const uint64_t __attribute__((address_space(1)))*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+__device__ __forceinline__ void leave2(float* p, float x, float y) { put((void*)p, make_uint2(__float_as_uint(x), __float_as_uint(y))); }
 
 template <int COLS, int D, bool BF16>
 __device__ __forceinline__ void merge(const AttendArgs& a, int head, const Unit& u, int col0, float* lds) {
-  // lds [chunks][COLS]: what each unit's sums are multiplied with
+  // lds [chunks][COLS]: M, then what each unit's numbers are multiplied with; behind it [chunks][COLS]: sums
+  constexpr int STEP = COLS * (D + 2), EACH = 256 / COLS;  // EACH threads share a column
   const int tid = threadIdx.x, cols = u.rows * a.group - col0 < COLS ? u.rows * a.group - col0 : COLS;
   const float* part = part_numbers<COLS, D>(a, head, u.first);
-  constexpr int STEP = COLS * (D + 2);
-  for (int c = tid; c < cols; c += 256) {
+  {
+    const int c = tid / EACH, j = tid % EACH;
+    float* tops = lds + c;
+    float* sums = lds + u.chunks * COLS + c;
     float top = -INFINITY, sum = 0.f;
-    for (int k = 0; k < u.chunks; ++k) top = fmaxf(top, part[(int64_t)k * STEP + COLS * D + 2 * c]);
-    const float base = top == -INFINITY ? 0.f : top;
-    for (int k = 0; k < u.chunks; ++k) {
-      const float w = exp2_fast(part[(int64_t)k * STEP + COLS * D + 2 * c] - base);
-      sum = fmaf(w, part[(int64_t)k * STEP + COLS * D + 2 * c + 1], sum);
-      lds[k * COLS + c] = w;
+    if (c < cols) {
+#pragma unroll 4
+      for (int k = j; k < u.chunks; k += EACH) {
+        const float2 v = take_back2(part + (int64_t)k * STEP + COLS * D + 2 * c);
+        tops[k * COLS] = v.x;
+        sums[k * COLS] = v.y;
+        top = fmaxf(top, v.x);
+      }
     }
+    top = wave_max<EACH>(top);
+    const float base = top == -INFINITY ? 0.f : top;
+    if (c < cols)
+      for (int k = j; k < u.chunks; k += EACH) {
+        const float w = exp2_fast(tops[k * COLS] - base);
+        tops[k * COLS] = w;
+        sum = fmaf(w, sums[k * COLS], sum);
+      }
+    sum = wave_sum<EACH>(sum);
     const float back = sum == 0.f ? 0.f : 1.f / sum;
-    for (int k = 0; k < u.chunks; ++k) lds[k * COLS + c] *= back;
+    if (c < cols)
+      for (int k = j; k < u.chunks; k += EACH) tops[k * COLS] *= back;
   }
   __syncthreads();
   for (int i = tid; i < cols * (D / 4); i += 256) {
     const int c = i / (D / 4), d = (i - c * (D / 4)) * 4;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int k = 0; k < u.chunks; ++k) {
-      const float w = lds[k * COLS + c];
-      const float4 v = *(const float4*)(part + (int64_t)k * STEP + c * D + d);
-      s.x = fmaf(w, v.x, s.x);
-      s.y = fmaf(w, v.y, s.y);
-      s.z = fmaf(w, v.z, s.z);
-      s.w = fmaf(w, v.w, s.w);
+    const float* from = part + c * D + d;
+    int k = 0;
+    for (; k + 16 <= u.chunks; k += 16) {
+      float4 v[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = take_back(from + (int64_t)(k + e) * STEP);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float w = lds[(k + e) * COLS + c];
+        s.x = fmaf(w, v[e].x, s.x);
+        s.y = fmaf(w, v[e].y, s.y);
+        s.z = fmaf(w, v[e].z, s.z);
+        s.w = fmaf(w, v[e].w, s.w);
+      }
+    }
+    for (; k < u.chunks; k += 4) {
+      float4 v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = take_back(from + (int64_t)(k + e < u.chunks ? k + e : k) * STEP);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (k + e >= u.chunks) break;
+        const float w = lds[(k + e) * COLS + c];
+        s.x = fmaf(w, v[e].x, s.x);
+        s.y = fmaf(w, v[e].y, s.y);
+        s.z = fmaf(w, v[e].z, s.z);
+        s.w = fmaf(w, v[e].w, s.w);
+      }
     }
     const int col = col0 + c, r = col / a.group;
     put_out<BF16>(a, (int64_t)(u.row0 + r) * a.out_row + (int64_t)(head * a.group + (col - r * a.group)) * a.out_head + d, s);
@@ -454,8 +496,8 @@ template <bool BF16, int D>
 __device__ __forceinline__ void attend_narrow_body(const AttendArgs& a) {
   constexpr int COLS = 16, MOST = kNarrowUnits, PITCH = D + 4;
   extern __shared__ float4 smem4[];
-  float* lds = (float*)smem4;  // [4][16][PITCH] sums, [4][16] M, [4][16] sums of weights; later the merge's factors
-  float* tops = lds + 4 * COLS * PITCH;
+  float* lds = (float*)smem4;  // [4][16][PITCH] numbers, [4][16] M, [4][16] sums of weights, a flag; the merge takes the numbers' place
+  float* tops = lds + narrow_numbers(D);
   float* sums = tops + 4 * COLS;
   int* flag = (int*)(sums + 4 * COLS);
   const int head = blockIdx.x % a.c.kv_heads, tid = threadIdx.x, wave = uniform(tid >> 6);
@@ -504,8 +546,8 @@ __device__ __forceinline__ void attend_narrow_body(const AttendArgs& a) {
       const int col = col0 + c, r = col / a.group;
       put_out<BF16>(a, (int64_t)(u.row0 + r) * a.out_row + (int64_t)(head * a.group + (col - r * a.group)) * a.out_head + d, s);
     } else {
-      *(float4*)(part + c * D + d) = s;
-      if (d == 0) *(float2*)(part + COLS * D + 2 * c) = make_float2(top, sum);
+      put((void*)(part + c * D + d), s);
+      if (d == 0) leave2(part + COLS * D + 2 * c, top, sum);
     }
   }
   if (u.chunks > 1 && arrive(a, head, u, flag)) merge<COLS, D, BF16>(a, head, u, col0, lds);
@@ -516,8 +558,8 @@ template <bool BF16, int D>
 __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
   constexpr int COLS = 128, MOST = kWideUnits;
   extern __shared__ float4 smem4[];
-  float* lds = (float*)smem4;  // the merge's factors [MOST][128], then a flag
-  int* flag = (int*)(lds + MOST * COLS);
+  float* lds = (float*)smem4;  // for the merge [2][MOST][128], then a flag
+  int* flag = (int*)(lds + 2 * MOST * COLS);
   const int head = blockIdx.x % a.c.kv_heads, wave = uniform(threadIdx.x >> 6);
   Unit u;
   if (!find_unit<COLS, MOST>(a, blockIdx.x / a.c.kv_heads, &u)) return;
@@ -545,9 +587,9 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
         for (int i = 0; i < 16; i += 4) {
           const float4 v = make_float4(w.o[t][i] * back, w.o[t][i + 1] * back, w.o[t][i + 2] * back, w.o[t][i + 3] * back);
           if (u.chunks == 1) put_out<BF16>(a, at + w.channel(t, i), v);
-          else *(float4*)(part + (wave * 32 + w.c) * D + w.channel(t, i)) = v;
+          else put((void*)(part + (wave * 32 + w.c) * D + w.channel(t, i)), v);
         }
-      if (u.chunks > 1 && w.g == 0) *(float2*)(part + COLS * D + 2 * (wave * 32 + w.c)) = make_float2(w.top, w.sum);
+      if (u.chunks > 1 && w.g == 0) leave2(part + COLS * D + 2 * (wave * 32 + w.c), w.top, w.sum);
     }
   }
   if (u.chunks > 1 && arrive(a, head, u, flag)) merge<COLS, D, BF16>(a, head, u, u.tile * COLS, lds);

@@ -62,8 +62,11 @@ struct AttendArgs {
 constexpr int kNarrowColumns = 16, kWideColumns = 128;  // columns (query heads of a row) of a unit
 constexpr int kNarrowUnits = 256, kWideUnits = 16;      // units of a tile, at most
 // bytes of LDS
-constexpr int narrow_lds(int dim) { return (4 * kNarrowColumns * (dim + 4) + 8 * kNarrowColumns + 4) * 4; }
-constexpr int wide_lds() { return (kWideUnits * kWideColumns + 4) * 4; }
+constexpr int narrow_numbers(int dim) {
+  return 4 * kNarrowColumns * (dim + 4) > 2 * kNarrowUnits * kNarrowColumns ? 4 * kNarrowColumns * (dim + 4) : 2 * kNarrowUnits * kNarrowColumns;
+}
+constexpr int narrow_lds(int dim) { return (narrow_numbers(dim) + 8 * kNarrowColumns + 4) * 4; }
+constexpr int wide_lds() { return (2 * kWideUnits * kWideColumns + 4) * 4; }
 // numbers of a unit in AttendArgs::part
 constexpr int64_t unit_floats(int columns, int dim) { return (int64_t)columns * (dim + 2); }
 
