@@ -375,8 +375,12 @@ class daris_op(C.Structure):
     _fields_ = [("kind", C.c_int32), ("reserved", C.c_int32), ("u", _step)]
 
 
-_lib_sigs = {"daris_run_ops": (C.c_int32, [C.POINTER(daris_op), C.c_int32, C.c_int32])}
-_SIGS.update(_lib_sigs)
+_SIGS.update({
+    "daris_run_ops": (C.c_int32, [C.POINTER(daris_op), C.c_int32, C.c_int32]),
+    "daris_plan_ops": (C.c_int32, [C.POINTER(daris_op), C.c_int32, C.c_int32]),
+    "daris_run_plan": (C.c_int32, [C.c_int32]),
+    "daris_free_plan": (C.c_int32, [C.c_int32]),
+})
 EXPORTS = sorted(_SIGS)
 
 
@@ -521,13 +525,46 @@ def make_matvec(x, w, w_scale, y, x_scale=None, gate=False):
     return _made(STEP_MATVEC, a, x, w, w_scale, y, x_scale)
 
 
+class Ops:
+    """Operators in the order in which they run; holds their buffers, and their plan on each partition that has run them."""
+
+    def __init__(self, ops):
+        self.array = (daris_op * len(ops))(*ops)
+        self.keep = tuple(o.keep for o in ops)
+        self.plans = {}
+
+    def __len__(self):
+        return len(self.array)
+
+    def __del__(self):
+        if _lib is not None:
+            for plan in self.plans.values():
+                _lib.daris_free_plan(plan)
+
+
 def make_ops(ops):
     """Operators in the order in which they run, as daris_run_ops takes them; a program keeps it from step to step."""
-    a = (daris_op * len(ops))(*ops)
-    a.keep = tuple(o.keep for o in ops)
-    return a
+    return Ops(ops)
+
+
+def daris_plan_ops(ops, p=0):
+    return _chk(lib().daris_plan_ops(ops.array, len(ops), p))
+
+
+def daris_run_plan(plan):
+    return _chk(lib().daris_run_plan(plan))
+
+
+def daris_free_plan(plan):
+    return _chk(lib().daris_free_plan(plan))
 
 
 def daris_run_ops(ops, p=0):
-    """Runs what make_ops made on partition p and waits for it."""
-    return _chk(lib().daris_run_ops(ops, len(ops), p))
+    """Runs what make_ops made on partition p and waits for it: planned by the first run there (and by the first after a daris_shutdown)."""
+    plan = ops.plans.get(p)
+    if plan is not None:
+        code = lib().daris_run_plan(plan)
+        if code != ERANGE:
+            return _chk(code)
+    ops.plans[p] = plan = daris_plan_ops(ops, p)
+    return daris_run_plan(plan)

@@ -146,6 +146,23 @@ struct PartRt {
   void* step_part = nullptr;
   uint32_t* step_count = nullptr;
   size_t step_part_bytes = 0, step_counters = 0;
+  uint64_t step_moved = 0;  // how often either has moved
+};
+
+// What daris_plan_ops has made of a list of operators.
+struct StepPlan {
+  daris_part p = 0;
+  std::vector<StepLaunch> launches;
+  std::vector<void*> args;  // of the launches, in slots of StepSlots
+  size_t bytes = 0, counters = 0;
+  uint64_t moved = 0;  // the partition's step_moved that the arguments are of
+};
+
+// Places for argument blocks that stay: memory that the host writes through the PCIe aperture (as the queues' rings are).
+struct StepSlots {
+  static constexpr size_t kSlot = 384, kSlab = 1024 * kSlot;
+  std::vector<void*> slabs, free;
+  bool on_device = true;
 };
 
 struct VtEvent {
@@ -194,7 +211,12 @@ struct Global {
   int64_t closed_total_left = -1;  // closed-loop runs: releases left over all tasks, -1 = no common budget
   bool prof = false;                // driver profile: where a stage's wall time goes (host clock and GPU markers)
   int64_t prof_acc[8] = {0};
+  std::mutex plans_mu;              // the two below: a plan may be freed on another thread
+  std::unordered_map<int32_t, std::shared_ptr<StepPlan>> plans;
+  StepSlots slots;
 };
+
+int32_t g_next_plan = 0;  // never the same twice, so that a handle from before a shutdown is none
 
 Global* G = nullptr;
 
@@ -825,6 +847,11 @@ daris_status daris_shutdown(void) {
       if (P.step_part) (void)hipFree(P.step_part);
       if (P.step_count) (void)hipFree(P.step_count);
     }
+    {
+      std::lock_guard<std::mutex> lk(G->plans_mu);
+      G->plans.clear();
+      for (void* m : G->slots.slabs) g_rt.free_mem(m);
+    }
     for (PartRt& P : G->parts)
       for (auto& S : P.streams) {
         if (S->hw) S->hw->q.destroy();  // destroying a shared queue again is a no-op
@@ -1356,6 +1383,7 @@ static daris_status step_workspace(PartRt& P, size_t bytes, size_t counters) {
     if (P.step_part) (void)hipFree(P.step_part);
     P.step_part = nullptr;
     P.step_part_bytes = 0;
+    ++P.step_moved;
     hipError_t e = hipMalloc(&P.step_part, bytes);
     if (e != hipSuccess) {
       (void)hipGetLastError();
@@ -1368,6 +1396,7 @@ static daris_status step_workspace(PartRt& P, size_t bytes, size_t counters) {
     if (P.step_count) (void)hipFree(P.step_count);
     P.step_count = nullptr;
     P.step_counters = 0;
+    ++P.step_moved;
     hipError_t e = hipMalloc((void**)&P.step_count, counters * sizeof(uint32_t));
     if (e == hipSuccess) e = hipMemset(P.step_count, 0, counters * sizeof(uint32_t));
     if (e != hipSuccess) {
@@ -1381,7 +1410,8 @@ static daris_status step_workspace(PartRt& P, size_t bytes, size_t counters) {
   return DARIS_OK;
 }
 
-daris_status daris_run_ops(const daris_op* ops, int32_t n, daris_part p) try {
+// Checks and encodes operators for partition p: the launches that there are.
+static daris_status encode_steps(const daris_op* ops, int32_t n, daris_part p, StepPlan* plan) {
   daris_status st = check_part(p);
   if (st != DARIS_OK) return st;
   if (n < 0 || (n > 0 && !ops)) return fail(DARIS_EINVAL, "%d operators at %p", n, (const void*)ops);
@@ -1390,33 +1420,49 @@ daris_status daris_run_ops(const daris_op* ops, int32_t n, daris_part p) try {
     if (!err.empty()) return fail(DARIS_EINVAL, "operator %d: %s", i, err.c_str());
   }
   if (G->nodev) return fail(DARIS_ESTATE, "no device in DARIS_NO_DEVICE mode");
-  st = make_streams();
-  if (st != DARIS_OK) return st;
-  PartRt& P = G->parts[p];
-  std::vector<StepLaunch> ls(n);
-  size_t bytes = 0, counters = 0;
-  int last = -1;
+  plan->p = p;
   for (int i = 0; i < n; ++i) {
-    const std::string err = encode_step(g_steps, ops[i], P.n_cu, &ls[i]);
+    StepLaunch l;
+    const std::string err = encode_step(g_steps, ops[i], G->parts[p].n_cu, &l);
     if (!err.empty()) return fail(DARIS_EINVAL, "operator %d: %s", i, err.c_str());
-    bytes = std::max(bytes, ls[i].part_bytes);
-    counters = std::max(counters, ls[i].counters);
-    if (ls[i].groups) last = i;
+    if (!l.groups) continue;
+    plan->bytes = std::max(plan->bytes, l.part_bytes);
+    plan->counters = std::max(plan->counters, l.counters);
+    plan->launches.push_back(l);
   }
-  st = step_workspace(P, bytes, counters);
+  return DARIS_OK;
+}
+
+// Runs a plan's launches (with their arguments in the plan's slots, or, without slots, through the queue's ring) and waits.
+static daris_status run_steps(StepPlan& plan) {
+  daris_status st = make_streams();
   if (st != DARIS_OK) return st;
+  PartRt& P = G->parts[plan.p];
+  st = step_workspace(P, plan.bytes, plan.counters);
+  if (st != DARIS_OK) return st;
+  const bool kept = !plan.args.empty();
+  if (!kept || plan.moved != P.step_moved) {
+    for (size_t i = 0; i < plan.launches.size(); ++i) {
+      StepLaunch& l = plan.launches[i];
+      place_step(&l, P.step_part, P.step_count);
+      if (kept) std::memcpy(plan.args[i], l.args, l.nbytes);
+    }
+    if (kept && G->slots.on_device) g_rt.flush_host_writes((char*)plan.args.back() + (plan.launches.back().nbytes - 1) / 4 * 4);
+    plan.moved = P.step_moved;
+  }
   HIP_TRY(hipDeviceSynchronize());  // the caller's streams may still be writing the buffers (see daris_task_set_io)
-  if (last < 0) return DARIS_OK;
+  if (plan.launches.empty()) return DARIS_OK;
   // The scheduler lock is not held: tasks go on while the operators run.
   StreamRt& S = *P.streams[0];
   bool ok = true;
   {
     std::lock_guard<std::mutex> ql(S.hw->mu);
-    for (int i = 0; i <= last && ok; ++i) {
-      if (!ls[i].groups) continue;
-      place_step(&ls[i], P.step_part, P.step_count);
-      ok = S.hw->q.dispatch_copy(ls[i].k, ls[i].groups, ls[i].threads, ls[i].args, ls[i].nbytes, i == last ? G->util_sig : hsa_signal_t{0},
-                                 i == last ? AqlQueue::kReleaseSystem : AqlQueue::kReleaseDevice);
+    for (size_t i = 0; i < plan.launches.size() && ok; ++i) {
+      const StepLaunch& l = plan.launches[i];
+      const bool last = i + 1 == plan.launches.size();
+      const hsa_signal_t done = last ? G->util_sig : hsa_signal_t{0};
+      const unsigned flags = last ? AqlQueue::kReleaseSystem : AqlQueue::kReleaseDevice;
+      ok = kept ? S.hw->q.dispatch(l.k, l.groups, l.threads, plan.args[i], done, flags) : S.hw->q.dispatch_copy(l.k, l.groups, l.threads, l.args, l.nbytes, done, flags);
     }
   }
   if (!ok || !aql_wait(G->util_sig, &S.hw->q)) {
@@ -1425,8 +1471,69 @@ daris_status daris_run_ops(const daris_op* ops, int32_t n, daris_part p) try {
     return gpu_wait_failed(S, ok ? "operators" : "packet rejected");
   }
   return DARIS_OK;
+}
+
+daris_status daris_run_ops(const daris_op* ops, int32_t n, daris_part p) try {
+  StepPlan plan;
+  const daris_status st = encode_steps(ops, n, p, &plan);
+  return st == DARIS_OK ? run_steps(plan) : st;
 } catch (const std::bad_alloc&) {
   return fail(DARIS_ENOMEM, "host memory");
+}
+
+daris_plan daris_plan_ops(const daris_op* ops, int32_t n, daris_part p) try {
+  auto plan = std::make_shared<StepPlan>();
+  const daris_status st = encode_steps(ops, n, p, plan.get());
+  if (st != DARIS_OK) return st;
+  const size_t count = plan->launches.size();
+  std::lock_guard<std::mutex> lk(G->plans_mu);
+  StepSlots& s = G->slots;
+  while (s.free.size() < count) {
+    char* slab = (char*)g_rt.alloc_device_for_host(StepSlots::kSlab);
+    if (!slab) {
+      // (a machine whose host cannot write device memory: all slabs are the host's then, and the kernels read them over the bus)
+      if (!s.slabs.empty() && s.on_device) return fail(DARIS_ENOMEM, "argument blocks of %zu operators", count);
+      s.on_device = false;
+      slab = (char*)g_rt.alloc_host_coherent(StepSlots::kSlab);
+    }
+    if (!slab) return fail(DARIS_ENOMEM, "argument blocks of %zu operators", count);
+    s.slabs.push_back(slab);
+    for (size_t at = 0; at < StepSlots::kSlab; at += StepSlots::kSlot) s.free.push_back(slab + at);
+  }
+  plan->args.assign(s.free.end() - count, s.free.end());
+  s.free.resize(s.free.size() - count);
+  plan->moved = ~0ull;  // its arguments are written by the first run
+  const int32_t handle = g_next_plan++;
+  G->plans[handle] = std::move(plan);
+  return handle;
+} catch (const std::bad_alloc&) {
+  return fail(DARIS_ENOMEM, "host memory");
+}
+
+daris_status daris_run_plan(daris_plan handle) try {
+  if (!G || !G->inited) return fail(DARIS_ESTATE, "library not initialised");
+  if (check_failed() != DARIS_OK) return DARIS_EHIP;
+  std::shared_ptr<StepPlan> plan;
+  {
+    std::lock_guard<std::mutex> lk(G->plans_mu);
+    auto it = G->plans.find(handle);
+    if (it == G->plans.end()) return fail(DARIS_ERANGE, "plan handle %d out of range", handle);
+    plan = it->second;
+  }
+  return run_steps(*plan);
+} catch (const std::bad_alloc&) {
+  return fail(DARIS_ENOMEM, "host memory");
+}
+
+daris_status daris_free_plan(daris_plan handle) {
+  if (!G || !G->inited) return fail(DARIS_ESTATE, "library not initialised");
+  std::lock_guard<std::mutex> lk(G->plans_mu);
+  auto it = G->plans.find(handle);
+  if (it == G->plans.end()) return fail(DARIS_ERANGE, "plan handle %d out of range", handle);
+  // (after a wait that failed its launches may still run: the slots stay as they are until daris_shutdown)
+  if (!G->failed.load()) G->slots.free.insert(G->slots.free.end(), it->second->args.begin(), it->second->args.end());
+  G->plans.erase(it);
+  return DARIS_OK;
 }
 
 daris_status daris_read_layer(daris_task t, int layer, float* host_out, int64_t cap_elems) {

@@ -70,7 +70,12 @@ constexpr int wide_lds() { return (2 * kWideUnits * kWideColumns + 4) * 4; }
 // numbers of a unit in AttendArgs::part
 constexpr int64_t unit_floats(int columns, int dim) { return (int64_t)columns * (dim + 2); }
 
-constexpr int kMatvecWaves = 8;
+// Waves of a workgroup by the blocks of 16 rows; pieces of x (8 channels) and of the weights' scales (8 of them) that a thread stages at
+// a time; the distance of the scales' rows in LDS, an odd number of words.
+constexpr int matvec_waves(int blocks) { return blocks == 1 ? 16 : 8; }
+constexpr int matvec_pieces(int parts) { return parts == 2 ? 4 : 8; }
+constexpr int kScalePieces = 2;
+constexpr int matvec_pitch(int scales) { return (scales + 7) / 8 * 8 + 2; }
 struct MatvecArgs {
   const void* x;
   const uint8_t* x_scale;
@@ -79,10 +84,12 @@ struct MatvecArgs {
   void* y;
   int64_t x_row, w_row, y_row;
   int rows, n, k, gate;
-  int chunk;        // k that a workgroup stages at a time, a multiple of 128
-  int x_vec;        // rows of x are 16-byte vectors
-  int tiles;        // workgroups side by side over n
-  int split;        // tiles of a workgroup side by side: 1, 2, 4 or 8; its other waves split K
+  int x_vec;   // rows of x are 16-byte vectors (8-byte ones of codes)
+  int steps;   // of 128 channels, in a chunk of K that LDS holds
+  int chunk;   // log2 of them, rounded up
+  int across;  // tiles (16 outputs) of a workgroup side by side: a power of two; its other waves share them
+  int groups;  // of so many tiles
+  int wgs;     // workgroups of a block of rows
 };
 
 }  // namespace daris

@@ -245,23 +245,46 @@ inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int 
   a.rows = o.rows; a.n = o.n; a.k = o.k; a.gate = o.gate;
   const int x_bytes = es == 1 ? 8 : 16;
   a.x_vec = aligned_to(o.x, x_bytes) && (o.rows == 1 || (o.x_row * es) % x_bytes == 0);
-  // neighbouring tiles for the waves of a workgroup while there are workgroups for every CU, otherwise shares of K
-  const int64_t tiles = (o.n + 15) / 16;
-  int across = kMatvecWaves;
-  while (across > 1 && (tiles + across - 1) / across * blocks < n_cu) across /= 2;
-  a.split = across;
-  const int64_t side = (tiles + across - 1) / across;
-  a.tiles = (int)side;
-  // x in LDS: as much of K at a time as 60 KiB hold
-  const int rows = o.rows < block ? o.rows : block;
-  const int step_bytes = 128 * 2 * parts * rows + 128 / o.group * block * 4;
-  const int64_t padded = ((int64_t)o.k + 127) / 128;
-  const int64_t steps = padded < 60 * 1024 / step_bytes ? padded : 60 * 1024 / step_bytes;
-  a.chunk = (int)steps * 128;
-  const int staged = (int)steps * step_bytes, reduced = kMatvecWaves * block * 16 * 4;
+  const int rows = o.rows < block ? o.rows : block, steps = (int)(((int64_t)o.k + 127) / 128), waves = matvec_waves(mt);
+  const int64_t tiles = ((int64_t)o.n + 15) / 16, room = n_cu / blocks > 1 ? n_cu / blocks : 1;
+  // x in LDS, of all of K if it fits (with the weights' scales and the waves' sums), else of the largest chunk that fits twice
+  const int per_group = 128 / o.group, step_bytes = 128 * 2 * parts * rows + (type == 1 ? 0 : per_group * block * 4);
+  auto lds = [&](int cs, int across) {
+    const bool again = cs < steps || (tiles + across - 1) / across > room;
+    return (cs < steps ? 2 : 1) * cs * step_bytes + (again ? 2 : 1) * across * 16 * matvec_pitch(cs * per_group) * 2 + waves * block * 16 * 4;
+  };
+  auto log2_up = [](int v) {
+    int log = 0;
+    while ((1 << log) < v) ++log;
+    return log;
+  };
+  auto fits = [&](int cs, int across) {
+    return ((16ll << log2_up(cs)) * rows <= matvec_pieces(parts) * waves * 64) && (cs * per_group + 7) / 8 * across * 16 <= kScalePieces * waves * 64 && lds(cs, across) <= 160 * 1024;
+  };
+  // Tiles side by side in a workgroup: what makes the shortest sequence of steps for a wave, on the most workgroups.  A wave's share of a chunk
+  // counts in fours (its steps travel four at a time), and a barrier as two steps.
+  int64_t best = -1;
+  for (int across = 1; across <= waves; across *= 2) {
+    int cs = steps;
+    if (!fits(cs, across)) {
+      cs = 1 << log2_up(cs);
+      while (cs > 1 && !fits(cs, across)) cs /= 2;
+    }
+    if (!fits(cs, across)) continue;
+    const int64_t groups = (tiles + across - 1) / across, rounds = (groups + room - 1) / room, chunks = (steps + cs - 1) / cs;
+    const int64_t own = ((int64_t)cs * across + waves - 1) / waves, cost = rounds * chunks * ((own + 3) / 4 * 4 + 2);
+    if (best >= 0 && cost >= best) continue;
+    best = cost;
+    a.across = across;
+    a.steps = cs;
+    a.groups = (int)groups;
+    a.wgs = (int)(groups < room ? groups : room);
+  }
+  if (best < 0) return "no chunk of K fits LDS";
+  a.chunk = log2_up(a.steps);
   set_args(l, a);
   const int g = o.group == 32 ? 0 : o.group == 64 ? 1 : 2;
-  return set_grid(l, t.matvec[type][g][many], side * blocks, kMatvecWaves * 64, staged > reduced ? staged : reduced) ? "" : kTooMany;
+  return set_grid(l, t.matvec[type][g][many], (int64_t)a.wgs * blocks, waves * 64, lds(a.steps, a.across)) ? "" : kTooMany;
 }
 
 // What is wrong with an operator, or "".

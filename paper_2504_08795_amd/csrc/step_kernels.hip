@@ -13,7 +13,7 @@ template <bool BF16, int D>
 __global__ __launch_bounds__(256) void step_append(AppendArgs a) { append_body<BF16, D>(a); }
 
 template <int XT, int G, int MT, bool BF16_OUT>
-__global__ __launch_bounds__(kMatvecWaves * 64) void step_matvec(MatvecArgs a) { matvec_body<XT, G, MT, BF16_OUT>(a); }
+__global__ __launch_bounds__(matvec_waves(MT) * 64) void step_matvec(MatvecArgs a) { matvec_body<XT, G, MT, BF16_OUT>(a); }
 
 #define NORM(B, F, A)                                      \
   template __global__ void step_norm<B, F, A, 1, 64>(NormArgs);   \
