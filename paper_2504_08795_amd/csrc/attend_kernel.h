@@ -14,8 +14,8 @@
 // (bf16) or two (fp32).  The scale of V joins the exponent: w = 2^(s + log2(scale_v) - M + 14), M the running maximum
 // of s + log2(scale_v): w fits f16 whatever the scales are, and the sum of weights takes 1 / scale_v back out.
 //
-// Masks cost nothing on pages that all columns see.  On the others scores are selected away, values that no column sees are cleared, and
-// where a NaN code is left, whose product with a zero weight would spoil other columns, the values' NaNs are counted apart.
+// Masks cost nothing on pages that all columns see.  On the others scores are selected away, and values that no column sees, as well as
+// NaN codes, whose product with a zero weight would spoil other columns, are cleared; mark_nans finds the columns that see them.
 //
 // Narrow tiles are bound by the bytes of the cache, wide ones by the matrix pipe and the exponentials.
 #pragma once
@@ -113,6 +113,16 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
   return (top >> 7) * 0xffu;
 }
 
+// The lowest n bytes of a word.
+__device__ __forceinline__ uint32_t bytes_below(int n) { return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
+
+// A channel's codes of tokens t1 .. t1 + 15, those outside [lo, hi] cleared.
+__device__ __forceinline__ uint4 seen(uint4 x, int t1, int lo, int hi) {
+  const int a = lo - t1, b = hi + 1 - t1;
+  return make_uint4(x.x & bytes_below(b) & ~bytes_below(a), x.y & bytes_below(b - 4) & ~bytes_below(a - 4), x.z & bytes_below(b - 8) & ~bytes_below(a - 8),
+                    x.w & bytes_below(b - 12) & ~bytes_below(a - 12));
+}
+
 // One wave's columns, TILE = 16 or 32 of them, and its running sums.
 template <bool BF16, int D, int TILE>
 struct Columns {
@@ -136,6 +146,7 @@ struct Columns {
   float top, sum;   // M; the lane's share of the sum of weights
   float factor;     // of a score: scale * log2(e) / the queries' power of two
   int pos;          // position of the column's row
+  bool nans;        // there were NaN codes among the values of a masked page
   int lane, c, g;
 
   // columns col0 .. of `rows` rows; those behind the last repeat it and are not stored
@@ -182,18 +193,19 @@ struct Columns {
     for (int j = 0; j < KS; ++j) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float v = __builtin_amdgcn_ldexpf(x[j][e], up);
+        const float v = __builtin_amdgcn_ldexpf(a.scale < 0.f ? -x[j][e] : x[j][e], up);
         q[0][j][e] = (_Float16)v;
         if (PARTS == 2) q[PARTS - 1][j][e] = is_finite(v) ? (_Float16)(v - (float)q[0][j][e]) : (_Float16)0.f;
       }
     }
-    factor = a.scale * two_to(-up);
+    factor = fabsf(a.scale) * two_to(-up);
 #pragma unroll
     for (int t = 0; t < VT; ++t)
 #pragma unroll
       for (int i = 0; i < R; ++i) o[t][i] = 0.f;
     top = -INFINITY;
     sum = 0.f;
+    nans = false;
   }
 
   // token of a page that row r of score tile t is: a lane's numbers of the tiles are then neighbouring tokens
@@ -204,10 +216,14 @@ struct Columns {
   // first of the 16 tokens whose scores tile group `half` leaves in this lane, and the sixteenth they are
   __device__ __forceinline__ int sixteenth(int half) const { return TILE == 16 ? g : half * 2 + g; }
 
+  // A page in registers, as its operands are: 16 bytes of a key's channels, of a channel's tokens.
   struct Page {
-    uint4 k[KT][KV];
-    uint4 v[VT][HALVES];
+    static constexpr bool kShared = false;
+    uint4 kr[KT][KV];
+    uint4 vr[VT][HALVES];
     uint32_t ks, vs;  // four scale bytes each
+    __device__ __forceinline__ uint4 k(int t, int i) const { return kr[t][i]; }
+    __device__ __forceinline__ uint4 v(int t, int h) const { return vr[t][h]; }
   };
   __device__ __forceinline__ void fetch(const AttendArgs& a, int head, int page, Page* p) const {
     const int64_t ph = (int64_t)page * a.c.kv_heads + head;
@@ -217,47 +233,65 @@ struct Columns {
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int i = 0; i < KV; ++i) p->k[t][i] = *(const uint4*)(k + token_of(t, c) * D + i * 16);
+      for (int i = 0; i < KV; ++i) p->kr[t][i] = *(const uint4*)(k + token_of(t, c) * D + i * 16);
     const uint8_t* v = a.c.v + ph * (kPage * D) + c * kPage;
 #pragma unroll
     for (int t = 0; t < VT; ++t)
 #pragma unroll
-      for (int h = 0; h < HALVES; ++h) p->v[t][h] = *(const uint4*)(v + t * TILE * kPage + sixteenth(h) * 16);
+      for (int h = 0; h < HALVES; ++h) p->vr[t][h] = *(const uint4*)(v + t * TILE * kPage + sixteenth(h) * 16);
   }
 
   // The page that starts at token t0.  masked: some column does not see all of it; [see_lo, see_hi]: tokens that any column sees.
-  __device__ __forceinline__ void take(const AttendArgs& a, Page& p, int t0, bool masked, int see_lo, int see_hi) {
+  template <typename P>
+  __device__ __forceinline__ void take(const AttendArgs& a, const P& p, int t0, bool masked, int see_lo, int see_hi) {
+    // tokens of its sixteenths that the column sees
+    struct {
+      int from[HALVES], to[HALVES];
+    } sees;
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+      const int t1 = t0 + sixteenth(h) * 16;
+      sees.to[h] = pos + 1 - t1;
+      sees.from[h] = a.window > 0 ? sees.to[h] - a.window : -(1 << 30);
+    }
     Acc s[KT];
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
 #pragma unroll
       for (int i = 0; i < R; ++i) s[t][i] = 0.f;
+      if (P::kShared) __builtin_amdgcn_sched_barrier(0);  // (tile by tile: the operands of all would not fit the registers)
 #pragma unroll
-      for (int j = 0; j < KS; ++j) {
-        const uint4& w = p.k[t][j >> 1];
-        const f16x8 k = j & 1 ? f16_of_codes(w.z, w.w) : f16_of_codes(w.x, w.y);
-        if (PARTS == 2) s[t] = mma(k, q[PARTS - 1][j], s[t]);
-        s[t] = mma(k, q[0][j], s[t]);
+      for (int j = 0; j < KS; j += 2) {
+        const uint4 w = p.k(t, j >> 1);
+        const f16x8 lo = f16_of_codes(w.x, w.y), hi = f16_of_codes(w.z, w.w);
+        if (PARTS == 2) {
+          s[t] = mma(lo, q[PARTS - 1][j], s[t]);
+          s[t] = mma(hi, q[PARTS - 1][j + 1], s[t]);
+        }
+        s[t] = mma(lo, q[0][j], s[t]);
+        s[t] = mma(hi, q[0][j + 1], s[t]);
       }
     }
-    // scores in powers of two, with the values' scale
+    // A score is s * f + v in powers of two, v the values' scale; f > 0 and v are a sixteenth's, so its largest score is that of its largest s.
     constexpr int PER = 16 / R;  // score tiles of a sixteenth (16-column tiles: four; 32: one)
+    float f[HALVES], v[HALVES];
     float big = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
-      const int part = sixteenth(t / PER);
-      const float f = factor * two_to((int)((p.ks >> (8 * part)) & 0xff) - 127), v = (float)((int)((p.vs >> (8 * part)) & 0xff) - 127);
+    for (int h = 0; h < HALVES; ++h) {
+      const int part = sixteenth(h);
+      f[h] = fmaxf(factor * two_to((int)((p.ks >> (8 * part)) & 0xff) - 127), 1.0e-37f);  // (0 would make -inf a NaN)
+      v[h] = (float)((int)((p.vs >> (8 * part)) & 0xff) - 127);
+      float m = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < R; ++i) {
-        float x = fmaf(s[t][i], f, v);
+      for (int e = 0; e < 16; ++e) {
+        float x = s[h * PER + e / R][e % R];
         if (masked) {
-          const int token = t0 + part * 16 + (t % PER) * R + i;
-          const bool on = token <= pos && (a.window == 0 || token > pos - a.window);
-          x = on ? x : -INFINITY;
+          x = e >= sees.from[h] && e < sees.to[h] ? x : -INFINITY;
+          s[h * PER + e / R][e % R] = x;
         }
-        s[t][i] = x;
-        big = fmaxf(big, x);
+        m = fmaxf(m, x);
       }
+      big = fmaxf(big, fmaf(m, f[h], v[h]));
     }
 #pragma unroll
     for (int m = TILE; m < 64; m *= 2) big = fmaxf(big, __shfl_xor(big, m));
@@ -272,14 +306,13 @@ struct Columns {
       top = now;
     }
     const float base = (top == -INFINITY ? 0.f : top) - kWeightBits;
-    f16x8 w[PARTS][kPage / (8 * G)];
+    f16x8 w[PARTS][2 * HALVES];
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) {
       float add = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int t = h * PER + e / R;
-        const float x = exp2_fast(s[t][e % R] - base);
+        const float x = exp2_fast(fmaf(s[h * PER + e / R][e % R], f[h], v[h] - base));
         add += x;
         const _Float16 hi = (_Float16)x;
         w[0][h * 2 + (e >> 3)][e & 7] = hi;
@@ -287,60 +320,19 @@ struct Columns {
       }
       sum = fmaf(add, two_to(127 - (int)((p.vs >> (8 * sixteenth(h))) & 0xff)), sum);
     }
-    bool odd = false;
-    if (masked) {
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      if (P::kShared) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) {
-        const int t1 = t0 + sixteenth(h) * 16;
-        uint32_t keep[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          keep[i] = 0u;
-#pragma unroll
-          for (int b = 0; b < 4; ++b) keep[i] |= t1 + 4 * i + b >= see_lo && t1 + 4 * i + b <= see_hi ? 0xffu << (8 * b) : 0u;
-        }
-#pragma unroll
-        for (int t = 0; t < VT; ++t) {
-          uint4& x = p.v[t][h];
-          x.x &= keep[0];
-          x.y &= keep[1];
-          x.z &= keep[2];
-          x.w &= keep[3];
-          odd = odd || has_nan_code(x.x) || has_nan_code(x.y) || has_nan_code(x.z) || has_nan_code(x.w);
-        }
-      }
-      odd = __any(odd);
-    }
-    if (odd) {
-      // NaN codes as numbers 1.0 (0x38), times 1 where the column sees the token: more than 0 makes the output NaN
-#pragma unroll
-      for (int h = 0; h < HALVES; ++h) {
-        f16x8 see[2];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int token = t0 + sixteenth(h) * 16 + e;
-          see[e >> 3][e & 7] = token <= pos && (a.window == 0 || token > pos - a.window) ? (_Float16)1.f : (_Float16)0.f;
-        }
-#pragma unroll
-        for (int t = 0; t < VT; ++t) {
-          uint4& x = p.v[t][h];
+        uint4 x = p.v(t, h);
+        if (masked) {
+          x = seen(x, t0 + sixteenth(h) * 16, see_lo, see_hi);
           const uint4 n = make_uint4(nan_bytes(x.x), nan_bytes(x.y), nan_bytes(x.z), nan_bytes(x.w));
-          Acc count;
-#pragma unroll
-          for (int i = 0; i < R; ++i) count[i] = 0.f;
-          count = mma(f16_of_codes(n.x & 0x38383838u, n.y & 0x38383838u), see[0], count);
-          count = mma(f16_of_codes(n.z & 0x38383838u, n.w & 0x38383838u), see[1], count);
-#pragma unroll
-          for (int i = 0; i < R; ++i) o[t][i] = count[i] > 0.f ? __uint_as_float(0x7fc00000u) : o[t][i];
+          nans = nans || (n.x | n.y | n.z | n.w) != 0;
           x = make_uint4(x.x & ~n.x, x.y & ~n.y, x.z & ~n.z, x.w & ~n.w);
         }
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < VT; ++t)
-#pragma unroll
-      for (int h = 0; h < HALVES; ++h) {
-        const f16x8 lo = f16_of_codes(p.v[t][h].x, p.v[t][h].y), hi = f16_of_codes(p.v[t][h].z, p.v[t][h].w);
+        const f16x8 lo = f16_of_codes(x.x, x.y), hi = f16_of_codes(x.z, x.w);
         if (PARTS == 2) {
           o[t] = mma(lo, w[PARTS - 1][h * 2], o[t]);
           o[t] = mma(hi, w[PARTS - 1][h * 2 + 1], o[t]);
@@ -348,6 +340,47 @@ struct Columns {
         o[t] = mma(lo, w[0][h * 2], o[t]);
         o[t] = mma(hi, w[0][h * 2 + 1], o[t]);
       }
+    }
+  }
+
+  // NaN codes among the values of a masked page count as 0 above, lest they spoil columns that do not see them.  If there were any, the columns that do
+  // see them are found here, once the pages are through: the codes as numbers 1.0 (0x38) times 1 where the column sees the token are more than 0.
+  __device__ __forceinline__ void mark_nans(const AttendArgs& a, const Unit& u, int head, int lo, int hi, int stride, int pos_lo, int pos_hi) {
+    if (!__any(nans)) return;
+    const int see_lo = a.window > 0 ? pos_lo - a.window + 1 : 0;
+#pragma unroll 1
+    for (int p = lo; p < hi; p += stride) {
+      const int t0 = p * kPage, page = uniform(page_of(a.c, u.s, p));
+      if (page < 0 || !is_masked(a, t0, pos_lo, pos_hi)) continue;
+      const uint8_t* v = a.c.v + ((int64_t)page * a.c.kv_heads + head) * (kPage * D) + c * kPage;
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) {
+        const int t1 = t0 + sixteenth(h) * 16, to = pos + 1 - t1, from = a.window > 0 ? to - a.window : -(1 << 30);
+        f16x8 see[2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) see[e >> 3][e & 7] = e >= from && e < to ? (_Float16)1.f : (_Float16)0.f;
+#pragma unroll
+        for (int t = 0; t < VT; ++t) {
+          const uint4 x = seen(*(const uint4*)(v + t * TILE * kPage + sixteenth(h) * 16), t1, see_lo, pos_hi);
+          Acc count;
+#pragma unroll
+          for (int i = 0; i < R; ++i) count[i] = 0.f;
+          count = mma(f16_of_codes(nan_bytes(x.x) & 0x38383838u, nan_bytes(x.y) & 0x38383838u), see[0], count);
+          count = mma(f16_of_codes(nan_bytes(x.z) & 0x38383838u, nan_bytes(x.w) & 0x38383838u), see[1], count);
+#pragma unroll
+          for (int i = 0; i < R; ++i) o[t][i] = count[i] > 0.f ? __uint_as_float(0x7fc00000u) : o[t][i];
+        }
+      }
+    }
+  }
+
+  // Whether some column does not see all of the page that starts at token t0.
+  static __device__ __forceinline__ bool is_masked(const AttendArgs& a, int t0, int pos_lo, int pos_hi) { return t0 + kPage - 1 > pos_lo || (a.window > 0 && t0 <= pos_hi - a.window); }
+
+  // The lanes of a column add their shares.
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int m = TILE; m < 64; m *= 2) sum += __shfl_xor(sum, m);
   }
 
   // Pages [lo, hi) of the sequence, every `stride`-th; the page numbers of 64 of them are read at a time.
@@ -363,13 +396,11 @@ struct Columns {
         const int t0 = (base + i * stride) * kPage;
         Page p;
         fetch(a, head, page, &p);
-        const bool masked = t0 + kPage - 1 > pos_lo || (a.window > 0 && t0 <= pos_hi - a.window);
-        take(a, p, t0, masked, see_lo, see_hi);
+        take(a, p, t0, is_masked(a, t0, pos_lo, pos_hi), see_lo, see_hi);
       }
     }
-    // the lanes of a column add their shares
-#pragma unroll
-    for (int m = TILE; m < 64; m *= 2) sum += __shfl_xor(sum, m);
+    mark_nans(a, u, head, lo, hi, stride, pos_lo, pos_hi);
+    finish();
   }
   // first channel of the four (of neighbouring numbers r .. r + 3) that o[t][r] begins
   __device__ __forceinline__ int channel(int t, int r) const { return TILE == 16 ? t * 16 + g * 4 : t * 32 + (r >> 2) * 8 + g * 4; }
@@ -553,30 +584,118 @@ __device__ __forceinline__ void attend_narrow_body(const AttendArgs& a) {
   if (u.chunks > 1 && arrive(a, head, u, flag)) merge<COLS, D, BF16>(a, head, u, col0, lds);
 }
 
-// Four waves side by side on 32 columns each, all on the same pages (which they fetch one after the other from the CU's cache).
+// A page in LDS, shared by the waves of a workgroup.  Sixteen neighbouring lanes read sixteen keys (channels) at one place, so the 16-byte
+// pieces of a row are exchanged by what tells these rows apart, and the lanes find them on different banks.
+template <int D>
+struct SharedPage {
+  static constexpr bool kShared = true;
+  static constexpr int PIECES = kPage * D / 16;  // of K; as many of V behind them
+  const uint4* lds;
+  uint32_t ks, vs;
+  int lane;
+  static __device__ __forceinline__ int key_place(int token, int piece) {
+    constexpr int ROW = D / 16;  // pieces of a key
+    return token * ROW + (piece ^ (((token & 7) | ((token >> 1) & 8)) / (16 / ROW)));
+  }
+  static __device__ __forceinline__ int value_place(int channel, int piece) { return PIECES + channel * 4 + (piece ^ ((channel >> 2) & 3)); }
+  __device__ __forceinline__ uint4 k(int t, int i) const {
+    return lds[key_place(Columns<true, D, 32>::token_of(t, lane & 31), (lane >> 5) * (D / 32) + i)];
+  }
+  __device__ __forceinline__ uint4 v(int t, int h) const { return lds[value_place(t * 32 + (lane & 31), h * 2 + (lane >> 5))]; }
+};
+
+// Four waves side by side on 32 columns each.  They share the pages: each fetches a quarter of the next one in whole cache lines while
+// the present one is used from LDS (a wave's operands straight from memory are 32 rows a load, 64 cycles of the CU's address
+// unit: 4096 a page for the four, of 1024 for the matrix instructions).
 template <bool BF16, int D>
 __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
-  constexpr int COLS = 128, MOST = kWideUnits;
-  extern __shared__ float4 smem4[];
-  float* lds = (float*)smem4;  // for the merge [2][MOST][128], then a flag
-  int* flag = (int*)(lds + 2 * MOST * COLS);
-  const int head = blockIdx.x % a.c.kv_heads, wave = uniform(threadIdx.x >> 6);
+  constexpr int COLS = 128, MOST = kWideUnits, PIECES = SharedPage<D>::PIECES, EACH = 2 * PIECES / 256;  // pieces of a page that a thread fetches
+  extern __shared__ uint4 smem_pages[];
+  float* lds = (float*)smem_pages;  // two pages; later for the merge [2][MOST][128]; a flag
+  int* flag = (int*)(lds + wide_numbers(D));
+  const int head = blockIdx.x % a.c.kv_heads, tid = threadIdx.x, wave = uniform(tid >> 6);
   Unit u;
   if (!find_unit<COLS, MOST>(a, blockIdx.x / a.c.kv_heads, &u)) return;
-  const int all = u.rows * a.group, col0 = u.tile * COLS + wave * 32;
-  if (col0 < all) {
-    const int cols = all - col0 < 32 ? all - col0 : 32;
-    const int pos_lo = u.before + col0 / a.group, pos_hi = u.before + (col0 + cols - 1) / a.group;
-    Columns<BF16, D, 32> w;
-    w.start(a, u, head, col0);
-    int lo, hi = seen_pages(a, u.rows, u.before, &lo);
-    lo += u.chunk * u.per;
-    hi = hi < lo + u.per ? hi : lo + u.per;
-    const int end = pos_hi < 0 ? 0 : pos_hi / kPage + 1;
-    const int from = a.window > 0 && pos_lo >= a.window ? (pos_lo - a.window + 1) / kPage : 0;
-    w.run(a, u, head, lo > from ? lo : from, hi < end ? hi : end, 1, pos_lo, pos_hi);
+  const int all = u.rows * a.group, col0 = u.tile * COLS, mine0 = col0 + wave * 32;
+  const int tile_cols = all - col0 < COLS ? all - col0 : COLS, cols = all - mine0 < 32 ? all - mine0 : 32;  // (cols may be none)
+  // pages of the workgroup, and of the wave
+  int lo, hi = seen_pages(a, u.rows, u.before, &lo);
+  lo += u.chunk * u.per;
+  hi = hi < lo + u.per ? hi : lo + u.per;
+  const int tile_lo = u.before + col0 / a.group, tile_hi = u.before + (col0 + tile_cols - 1) / a.group;
+  const int end = tile_hi < 0 ? 0 : tile_hi / kPage + 1, from = a.window > 0 && tile_lo >= a.window ? (tile_lo - a.window + 1) / kPage : 0;
+  hi = hi < end ? hi : end;
+  lo = lo > from ? lo : from;
+  const int pos_lo = u.before + mine0 / a.group, pos_hi = cols > 0 ? u.before + (mine0 + cols - 1) / a.group : -1;
+  const int see_lo = a.window > 0 ? pos_lo - a.window + 1 : 0;
+
+  Columns<BF16, D, 32> w;
+  w.start(a, u, head, cols > 0 ? mine0 : col0);
+
+  u32x4 next[EACH];
+  uint32_t next_ks = 0, next_vs = 0;
+  auto fetch = [&](int page) {
+    const int64_t ph = (int64_t)page * a.c.kv_heads + head;
+    next_ks = *(const uint32_t*)(a.c.k_scale + ph * 4);
+    next_vs = *(const uint32_t*)(a.c.v_scale + ph * 4);
+    const u32x4* k = (const u32x4*)(a.c.k + ph * (kPage * D));
+    const u32x4* v = (const u32x4*)(a.c.v + ph * (kPage * D));
+#pragma unroll
+    for (int i = 0; i < EACH / 2; ++i) {
+      next[i] = k[i * 256 + tid];
+      next[EACH / 2 + i] = v[i * 256 + tid];
+    }
+  };
+  auto store = [&](int buf) {
+    u32x4* to = (u32x4*)smem_pages + buf * 2 * PIECES;
+#pragma unroll
+    for (int i = 0; i < EACH / 2; ++i) {
+      const int n = i * 256 + tid;
+      to[SharedPage<D>::key_place(n / (D / 16), n % (D / 16))] = next[i];
+      to[SharedPage<D>::value_place(n / 4, n % 4)] = next[EACH / 2 + i];
+    }
+  };
+  // page numbers, 64 at a time (a wave has them all: the loop is the same for all four)
+  int ids = -1, ids0 = 0;
+  auto number = [&](int p) {
+    if (p - ids0 >= 64) {
+      ids0 = p;
+      ids = p + w.lane < hi ? page_of(a.c, u.s, p + w.lane) : -1;
+    }
+    return __builtin_amdgcn_readlane(ids, p - ids0);
+  };
+  int page = -1;
+  auto advance = [&](int p) {  // the first page from p on that is there
+    for (; p < hi; ++p)
+      if ((page = number(p)) >= 0) break;
+    return p;
+  };
+  ids0 = lo;
+  ids = lo + w.lane < hi ? page_of(a.c, u.s, lo + w.lane) : -1;
+  int p = advance(lo), buf = 0;
+  if (p < hi) {
+    fetch(page);
+    store(0);
+  }
+  while (p < hi) {
+    __syncthreads();
+    SharedPage<D> now;
+    now.lds = smem_pages + buf * 2 * PIECES;
+    now.ks = next_ks;
+    now.vs = next_vs;
+    now.lane = w.lane;
+    const int after = advance(p + 1), t0 = p * kPage;
+    if (after < hi) fetch(page);
+    if (t0 <= pos_hi && (a.window == 0 || t0 + kPage > see_lo)) w.take(a, now, t0, w.is_masked(a, t0, pos_lo, pos_hi), see_lo, pos_hi);
+    buf ^= 1;
+    if (after < hi) store(buf);
+    p = after;
+  }
+  w.mark_nans(a, u, head, lo, hi, 1, pos_lo, pos_hi);
+  w.finish();
+  if (cols > 0) {
     const bool on = w.c < cols;
-    const int col = col0 + (on ? w.c : 0), r = col / a.group;
+    const int col = mine0 + (on ? w.c : 0), r = col / a.group;
     const int64_t at = (int64_t)(u.row0 + r) * a.out_row + (int64_t)(head * a.group + (col - r * a.group)) * a.out_head;
     float* part = part_numbers<COLS, D>(a, head, u.first + u.chunk);
     const float back = u.chunks > 1 ? 1.f : w.sum == 0.f ? 0.f : 1.f / w.sum;
@@ -592,7 +711,7 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
       if (u.chunks > 1 && w.g == 0) leave2(part + COLS * D + 2 * (wave * 32 + w.c), w.top, w.sum);
     }
   }
-  if (u.chunks > 1 && arrive(a, head, u, flag)) merge<COLS, D, BF16>(a, head, u, u.tile * COLS, lds);
+  if (u.chunks > 1 && arrive(a, head, u, flag)) merge<COLS, D, BF16>(a, head, u, col0, lds);
 }
 
 }  // namespace daris

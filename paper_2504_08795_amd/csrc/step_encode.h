@@ -27,7 +27,7 @@ struct StepTable {
   const AqlKernel* norm[2][2][2][6] = {};  // [bf16][8 bits][aligned][kNormShapes]
   const AqlKernel* append[2][3] = {};      // [bf16][dim 64, 128, 256]
   const AqlKernel* narrow[2][3] = {};
-  const AqlKernel* wide[2][3] = {};        // (none of fp32 and 256)
+  const AqlKernel* wide[2][3] = {};        // (none of 256)
   const AqlKernel* matvec[4][3][2] = {};   // [kMatvecTypes][group 32, 64, 128][16 rows, 64]
   std::string resolve(const AqlRuntime& rt);
 };
@@ -53,7 +53,7 @@ inline std::string StepTable::resolve(const AqlRuntime& rt) {
     for (int d = 0; d < 3; ++d) {
       append[b][d] = find("daris::step_append<%s, %d>", tf[b], 64 << d);
       narrow[b][d] = find("daris::step_attend_narrow<%s, %d>", tf[b], 64 << d);
-      if (b || d < 2) wide[b][d] = find("daris::step_attend_wide<%s, %d>", tf[b], 64 << d);
+      if (d < 2) wide[b][d] = find("daris::step_attend_wide<%s, %d>", tf[b], 64 << d);
     }
   }
   for (int t = 0; t < 4; ++t)
@@ -233,7 +233,7 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   l->counters = a.target ? (size_t)units * o.cache.kv_heads : 0;
   l->part_bytes = a.target ? (size_t)(units * o.cache.kv_heads * unit_floats(cols, o.cache.dim)) * sizeof(float) : 0;
   set_args(l, a);
-  return set_grid(l, wide ? t.wide[bf16][d] : t.narrow[bf16][d], units * o.cache.kv_heads, 256, wide ? wide_lds() : narrow_lds(o.cache.dim)) ? "" : kTooMany;
+  return set_grid(l, wide ? t.wide[bf16][d] : t.narrow[bf16][d], units * o.cache.kv_heads, 256, wide ? wide_lds(o.cache.dim) : narrow_lds(o.cache.dim)) ? "" : kTooMany;
 }
 
 inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int n_cu, StepLaunch* l) {
