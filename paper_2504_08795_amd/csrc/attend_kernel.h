@@ -11,8 +11,8 @@
 // exchange between lanes but for the maximum.  Sixteen tokens share a scale, so a lane needs one scale of K and one of V a page.
 // Keys [token][channel] and values [channel][token] are loaded in the operands' own order, 16 bytes a lane, and spread from
 // e4m3 to f16 two at a time (exact).  Queries are divided by a power of two that brings their largest number to 2^14, in one f16 part
-// (bf16) or two (fp32).  The scale of V joins the exponent: w = 2^(s + log2(scale_v) - M + 14), M the running maximum
-// of s + log2(scale_v): w fits f16 whatever the scales are, and the sum of weights takes 1 / scale_v back out.
+// (bf16) or two (fp32).  The scale of V joins the exponent: w = 2^(s + log2(scale_v) - M + 10), M a running maximum
+// of s + log2(scale_v) (at most 5 behind): w fits f16 whatever the scales are, and the sum of weights takes 1 / scale_v back out.
 //
 // Masks cost nothing on pages that all columns see.  On the others scores are selected away, and values that no column sees, as well as
 // NaN codes, whose product with a zero weight would spoil other columns, are cleared; mark_nans finds the columns that see them.
@@ -23,7 +23,7 @@
 
 namespace daris {
 
-constexpr float kWeightBits = 14.f;
+constexpr float kWeightBits = 10.f, kMaxLag = 5.f;  // a weight is at most 2^15
 
 // What a workgroup has to do.
 struct Unit {
@@ -81,7 +81,7 @@ __device__ __forceinline__ bool find_unit(const AttendArgs& a, int unit, Unit* u
     int upto = mine;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-      const int o = __shfl_up(upto, d);
+      const int o = __builtin_amdgcn_ds_bpermute((lane - d) * 4, upto);
       if (lane >= d) upto += o;
     }
     const int start = base + upto - mine;
@@ -89,18 +89,18 @@ __device__ __forceinline__ bool find_unit(const AttendArgs& a, int unit, Unit* u
     if (hit) {
       const int l = __builtin_ctzll(hit);
       u->s = s0 + l;
-      u->chunks = uniform(__shfl(chunks, l));
-      const int in = unit - uniform(__shfl(start, l));
+      u->chunks = __builtin_amdgcn_readlane(chunks, l);
+      const int in = unit - __builtin_amdgcn_readlane(start, l);
       u->tile = in / u->chunks;
       u->chunk = in - u->tile * u->chunks;
       u->first = unit - u->chunk;
       u->per = c;
-      u->row0 = uniform(__shfl(row0, l));
-      u->rows = uniform(__shfl(rows, l));
-      u->before = uniform(__shfl(before, l));
+      u->row0 = __builtin_amdgcn_readlane(row0, l);
+      u->rows = __builtin_amdgcn_readlane(rows, l);
+      u->before = __builtin_amdgcn_readlane(before, l);
       return true;
     }
-    base += uniform(__shfl(upto, 63));
+    base += __builtin_amdgcn_readlane(upto, 63);
   }
   return false;
 }
@@ -147,53 +147,68 @@ struct Columns {
   float factor;     // of a score: scale * log2(e) / the queries' power of two
   int pos;          // position of the column's row
   bool nans;        // there were NaN codes among the values of a masked page
-  int lane, c, g;
+  int lane;
+  __device__ __forceinline__ int c() const { return lane & (TILE - 1); }  // column of the lane, and which of the column's lanes it is
+  __device__ __forceinline__ int g() const { return lane / TILE; }
 
   // columns col0 .. of `rows` rows; those behind the last repeat it and are not stored
   __device__ __forceinline__ void start(const AttendArgs& a, const Unit& u, int head, int col0) {
     lane = threadIdx.x & 63;
-    c = lane & (TILE - 1);
-    g = lane / TILE;
+    const int c = this->c(), g = this->g();
     const int cols = u.rows * a.group;
     const int col = col0 + c < cols ? col0 + c : cols - 1;
     const int r = col / a.group;
     pos = u.before + r;
     const int64_t at = (int64_t)(u.row0 + r) * a.q_row + (int64_t)(head * a.group + (col - r * a.group)) * a.q_head + g * (D / G);
-    float x[KS][8];
-    float most = 0.f;
-#pragma unroll
-    for (int j = 0; j < KS; ++j) {
-      if (a.q_vec) {
-        if (BF16) {
-          unpack<true>(*(const uint4*)((const uint16_t*)a.q + at + 8 * j), x[j]);
-        } else {
-          float lo[4], hi[4];
-          unpack<false>(*(const uint4*)((const float*)a.q + at + 8 * j), lo);
-          unpack<false>(*(const uint4*)((const float*)a.q + at + 8 * j + 4), hi);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[j][e] = lo[e];
-            x[j][e + 4] = hi[e];
-          }
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[j][e] = load_elem<BF16>(a.q, at + 8 * j + e);
-      }
-    }
+    constexpr int W = BF16 ? 1 : 2;  // 16-byte vectors of eight channels
+    uint4 raw[KS][W];
 #pragma unroll
     for (int j = 0; j < KS; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) most = fmaxf(most, size_of(x[j][e]));
+      for (int i = 0; i < W; ++i) {
+        if (a.q_vec) {
+          raw[j][i] = *(const uint4*)((const char*)a.q + (at + 8 * j) * (BF16 ? 2 : 4) + 16 * i);
+        } else if (BF16) {
+          const uint16_t* x = (const uint16_t*)a.q + at + 8 * j;
+          raw[j][i] = make_uint4(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16, x[4] | (uint32_t)x[5] << 16, x[6] | (uint32_t)x[7] << 16);
+        } else {
+          const uint32_t* x = (const uint32_t*)a.q + at + 8 * j + 4 * i;
+          raw[j][i] = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+      }
+    auto channels = [&](int j, float (&x)[8]) {
+      if constexpr (BF16) {
+        unpack<true>(raw[j][0], x);
+      } else {
+        float lo[4], hi[4];
+        unpack<false>(raw[j][0], lo);
+        unpack<false>(raw[j][W - 1], hi);
 #pragma unroll
-    for (int m = TILE; m < 64; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+        for (int e = 0; e < 4; ++e) {
+          x[e] = lo[e];
+          x[e + 4] = hi[e];
+        }
+      }
+    };
+    float most = 0.f;
+#pragma unroll
+    for (int j = 0; j < KS; ++j) {
+      float x[8];
+      channels(j, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = fmaxf(most, size_of(x[e]));
+    }
+    most = lanes_max<TILE, 64>(most);
     int up = 141 - (int)(__float_as_uint(most) >> 23);
     up = up > 110 ? 110 : up;
 #pragma unroll
     for (int j = 0; j < KS; ++j) {
+      __builtin_amdgcn_sched_barrier(0);
+      float x[8];
+      channels(j, x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float v = __builtin_amdgcn_ldexpf(a.scale < 0.f ? -x[j][e] : x[j][e], up);
+        const float v = __builtin_amdgcn_ldexpf(a.scale < 0.f ? -x[e] : x[e], up);
         q[0][j][e] = (_Float16)v;
         if (PARTS == 2) q[PARTS - 1][j][e] = is_finite(v) ? (_Float16)(v - (float)q[0][j][e]) : (_Float16)0.f;
       }
@@ -214,7 +229,7 @@ struct Columns {
     return t * 32 + ((r >> 2) & 1) * 16 + (r >> 3) * 4 + (r & 3);
   }
   // first of the 16 tokens whose scores tile group `half` leaves in this lane, and the sixteenth they are
-  __device__ __forceinline__ int sixteenth(int half) const { return TILE == 16 ? g : half * 2 + g; }
+  __device__ __forceinline__ int sixteenth(int half) const { return TILE == 16 ? g() : half * 2 + g(); }
 
   // A page in registers, as its operands are: 16 bytes of a key's channels, of a channel's tokens.
   struct Page {
@@ -229,21 +244,21 @@ struct Columns {
     const int64_t ph = (int64_t)page * a.c.kv_heads + head;
     p->ks = *(const uint32_t*)(a.c.k_scale + ph * 4);
     p->vs = *(const uint32_t*)(a.c.v_scale + ph * 4);
-    const uint8_t* k = a.c.k + ph * (kPage * D) + g * (D / G);
+    const uint8_t* k = a.c.k + ph * (kPage * D) + g() * (D / G);
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int i = 0; i < KV; ++i) p->kr[t][i] = *(const uint4*)(k + token_of(t, c) * D + i * 16);
-    const uint8_t* v = a.c.v + ph * (kPage * D) + c * kPage;
+      for (int i = 0; i < KV; ++i) p->kr[t][i] = *(const uint4*)(k + token_of(t, c()) * D + i * 16);
+    const uint8_t* v = a.c.v + ph * (kPage * D) + c() * kPage;
 #pragma unroll
     for (int t = 0; t < VT; ++t)
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) p->vr[t][h] = *(const uint4*)(v + t * TILE * kPage + sixteenth(h) * 16);
   }
 
-  // The page that starts at token t0.  masked: some column does not see all of it; [see_lo, see_hi]: tokens that any column sees.
-  template <typename P>
-  __device__ __forceinline__ void take(const AttendArgs& a, const P& p, int t0, bool masked, int see_lo, int see_hi) {
+  // The page that starts at token t0.  MASKED: some column does not see all of it; [see_lo, see_hi]: tokens that any column sees.
+  template <bool MASKED, typename P>
+  __device__ __forceinline__ void take_page(const AttendArgs& a, const P& p, int t0, int see_lo, int see_hi) {
     // tokens of its sixteenths that the column sees
     struct {
       int from[HALVES], to[HALVES];
@@ -254,14 +269,15 @@ struct Columns {
       sees.to[h] = pos + 1 - t1;
       sees.from[h] = a.window > 0 ? sees.to[h] - a.window : -(1 << 30);
     }
+    uint32_t found = 0;
     Acc s[KT];
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
 #pragma unroll
       for (int i = 0; i < R; ++i) s[t][i] = 0.f;
-      if (P::kShared) __builtin_amdgcn_sched_barrier(0);  // (tile by tile: the operands of all would not fit the registers)
-#pragma unroll
+      #pragma unroll
       for (int j = 0; j < KS; j += 2) {
+        if (P::kShared) __builtin_amdgcn_sched_barrier(0);  // (one after the other: the operands of all would not fit the registers)
         const uint4 w = p.k(t, j >> 1);
         const f16x8 lo = f16_of_codes(w.x, w.y), hi = f16_of_codes(w.z, w.w);
         if (PARTS == 2) {
@@ -285,7 +301,7 @@ struct Columns {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         float x = s[h * PER + e / R][e % R];
-        if (masked) {
+        if (MASKED) {
           x = e >= sees.from[h] && e < sees.to[h] ? x : -INFINITY;
           s[h * PER + e / R][e % R] = x;
         }
@@ -293,10 +309,11 @@ struct Columns {
       }
       big = fmaxf(big, fmaf(m, f[h], v[h]));
     }
-#pragma unroll
-    for (int m = TILE; m < 64; m *= 2) big = fmaxf(big, __shfl_xor(big, m));
-    const float now = fmaxf(top, big);
+    big = lanes_max<TILE, 64>(big);
+    // M follows only when it has been passed by kMaxLag: up to there the weights have room, and most pages then leave the outputs alone
+    const float now = big > top + kMaxLag ? big : top;
     if (__any(now != top)) {
+      asm volatile("");  // (a branch: left to itself the compiler multiplies always)
       const float shrink = now == top ? 1.f : exp2_fast(top - now);
 #pragma unroll
       for (int t = 0; t < VT; ++t)
@@ -326,10 +343,10 @@ struct Columns {
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) {
         uint4 x = p.v(t, h);
-        if (masked) {
+        if (MASKED) {
           x = seen(x, t0 + sixteenth(h) * 16, see_lo, see_hi);
           const uint4 n = make_uint4(nan_bytes(x.x), nan_bytes(x.y), nan_bytes(x.z), nan_bytes(x.w));
-          nans = nans || (n.x | n.y | n.z | n.w) != 0;
+          found |= n.x | n.y | n.z | n.w;
           x = make_uint4(x.x & ~n.x, x.y & ~n.y, x.z & ~n.z, x.w & ~n.w);
         }
         const f16x8 lo = f16_of_codes(x.x, x.y), hi = f16_of_codes(x.z, x.w);
@@ -341,18 +358,19 @@ struct Columns {
         o[t] = mma(hi, w[0][h * 2 + 1], o[t]);
       }
     }
+    if (MASKED && __any(found != 0)) nans = true;
   }
 
   // NaN codes among the values of a masked page count as 0 above, lest they spoil columns that do not see them.  If there were any, the columns that do
   // see them are found here, once the pages are through: the codes as numbers 1.0 (0x38) times 1 where the column sees the token are more than 0.
   __device__ __forceinline__ void mark_nans(const AttendArgs& a, const Unit& u, int head, int lo, int hi, int stride, int pos_lo, int pos_hi) {
-    if (!__any(nans)) return;
+    if (!nans) return;
     const int see_lo = a.window > 0 ? pos_lo - a.window + 1 : 0;
 #pragma unroll 1
     for (int p = lo; p < hi; p += stride) {
       const int t0 = p * kPage, page = uniform(page_of(a.c, u.s, p));
       if (page < 0 || !is_masked(a, t0, pos_lo, pos_hi)) continue;
-      const uint8_t* v = a.c.v + ((int64_t)page * a.c.kv_heads + head) * (kPage * D) + c * kPage;
+      const uint8_t* v = a.c.v + ((int64_t)page * a.c.kv_heads + head) * (kPage * D) + c() * kPage;
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) {
         const int t1 = t0 + sixteenth(h) * 16, to = pos + 1 - t1, from = a.window > 0 ? to - a.window : -(1 << 30);
@@ -361,6 +379,7 @@ struct Columns {
         for (int e = 0; e < 16; ++e) see[e >> 3][e & 7] = e >= from && e < to ? (_Float16)1.f : (_Float16)0.f;
 #pragma unroll
         for (int t = 0; t < VT; ++t) {
+          __builtin_amdgcn_sched_barrier(0);
           const uint4 x = seen(*(const uint4*)(v + t * TILE * kPage + sixteenth(h) * 16), t1, see_lo, pos_hi);
           Acc count;
 #pragma unroll
@@ -374,14 +393,18 @@ struct Columns {
     }
   }
 
+  template <typename P>
+  __device__ __forceinline__ void take(const AttendArgs& a, const P& p, int t0, bool masked, int see_lo, int see_hi) {
+    // (a page in registers has one form: two would hold twice the addresses, and memory has to be waited for anyway)
+    if (!P::kShared || masked) take_page<true>(a, p, t0, see_lo, see_hi);
+    else take_page<false>(a, p, t0, see_lo, see_hi);
+  }
+
   // Whether some column does not see all of the page that starts at token t0.
   static __device__ __forceinline__ bool is_masked(const AttendArgs& a, int t0, int pos_lo, int pos_hi) { return t0 + kPage - 1 > pos_lo || (a.window > 0 && t0 <= pos_hi - a.window); }
 
   // The lanes of a column add their shares.
-  __device__ __forceinline__ void finish() {
-#pragma unroll
-    for (int m = TILE; m < 64; m *= 2) sum += __shfl_xor(sum, m);
-  }
+  __device__ __forceinline__ void finish() { sum = lanes_sum<TILE, 64>(sum); }
 
   // Pages [lo, hi) of the sequence, every `stride`-th; the page numbers of 64 of them are read at a time.
   __device__ __forceinline__ void run(const AttendArgs& a, const Unit& u, int head, int lo, int hi, int stride, int pos_lo, int pos_hi) {
@@ -403,7 +426,7 @@ struct Columns {
     finish();
   }
   // first channel of the four (of neighbouring numbers r .. r + 3) that o[t][r] begins
-  __device__ __forceinline__ int channel(int t, int r) const { return TILE == 16 ? t * 16 + g * 4 : t * 32 + (r >> 2) * 8 + g * 4; }
+  __device__ __forceinline__ int channel(int t, int r) const { return TILE == 16 ? t * 16 + g() * 4 : t * 32 + (r >> 2) * 8 + g() * 4; }
 };
 
 template <bool BF16>
@@ -430,10 +453,10 @@ __device__ __forceinline__ float* part_numbers(const AttendArgs& a, int head, in
 // Whether this workgroup is the last of the tile's units.  What they leave is written through to where all XCDs see it (put) and read
 // from there (take_back), so neither side needs a fence: a release or an acquire of the device writes back or drops a whole L2, and
 // with one for every workgroup 64 streams took 300 us instead of 88.
-__device__ __forceinline__ bool arrive(const AttendArgs& a, int head, const Unit& u, int* lds) {
+__device__ __forceinline__ bool arrive(const AttendArgs& a, int head, const Unit& u, int* lds, int tid) {
   puts_done();
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     uint32_t* n = a.count + (int64_t)head * a.units + u.first;
     const uint32_t before = __hip_atomic_fetch_add(n, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     const bool last = before == (uint32_t)u.chunks - 1;
@@ -452,10 +475,10 @@ __device__ __forceinline__ float2 take_back2(const float* p) {
 __device__ __forceinline__ void leave2(float* p, float x, float y) { put((void*)p, make_uint2(__float_as_uint(x), __float_as_uint(y))); }
 
 template <int COLS, int D, bool BF16>
-__device__ __forceinline__ void merge(const AttendArgs& a, int head, const Unit& u, int col0, float* lds) {
+__device__ __forceinline__ void merge(const AttendArgs& a, int head, const Unit& u, int col0, float* lds, int tid) {
   // lds [chunks][COLS]: M, then what each unit's numbers are multiplied with; behind it [chunks][COLS]: sums
   constexpr int STEP = COLS * (D + 2), EACH = 256 / COLS;  // EACH threads share a column
-  const int tid = threadIdx.x, cols = u.rows * a.group - col0 < COLS ? u.rows * a.group - col0 : COLS;
+  const int cols = u.rows * a.group - col0 < COLS ? u.rows * a.group - col0 : COLS;
   const float* part = part_numbers<COLS, D>(a, head, u.first);
   {
     const int c = tid / EACH, j = tid % EACH;
@@ -544,11 +567,11 @@ __device__ __forceinline__ void attend_narrow_body(const AttendArgs& a) {
   const int end = pos_hi < 0 ? 0 : pos_hi / kPage + 1;
   w.run(a, u, head, lo + wave, hi < end ? hi : end, 4, pos_lo, pos_hi);
   if (w.lane < COLS) {
-    tops[wave * COLS + w.c] = w.top;
-    sums[wave * COLS + w.c] = w.sum;
+    tops[wave * COLS + w.c()] = w.top;
+    sums[wave * COLS + w.c()] = w.sum;
   }
 #pragma unroll
-  for (int t = 0; t < D / COLS; ++t) *(float4*)(lds + (wave * COLS + w.c) * PITCH + w.channel(t, 0)) = make_float4(w.o[t][0], w.o[t][1], w.o[t][2], w.o[t][3]);
+  for (int t = 0; t < D / COLS; ++t) *(float4*)(lds + (wave * COLS + w.c()) * PITCH + w.channel(t, 0)) = make_float4(w.o[t][0], w.o[t][1], w.o[t][2], w.o[t][3]);
   __syncthreads();
   float* part = part_numbers<COLS, D>(a, head, u.first + u.chunk);
   for (int i = tid; i < cols * (D / 4); i += 256) {
@@ -581,7 +604,7 @@ __device__ __forceinline__ void attend_narrow_body(const AttendArgs& a) {
       if (d == 0) leave2(part + COLS * D + 2 * c, top, sum);
     }
   }
-  if (u.chunks > 1 && arrive(a, head, u, flag)) merge<COLS, D, BF16>(a, head, u, col0, lds);
+  if (u.chunks > 1 && arrive(a, head, u, flag, tid)) merge<COLS, D, BF16>(a, head, u, col0, lds, tid);
 }
 
 // A page in LDS, shared by the waves of a workgroup.  Sixteen neighbouring lanes read sixteen keys (channels) at one place, so the 16-byte
@@ -613,7 +636,7 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
   extern __shared__ uint4 smem_pages[];
   float* lds = (float*)smem_pages;  // two pages; later for the merge [2][MOST][128]; a flag
   int* flag = (int*)(lds + wide_numbers(D));
-  const int head = blockIdx.x % a.c.kv_heads, tid = threadIdx.x, wave = uniform(tid >> 6);
+  const int head = blockIdx.x % a.c.kv_heads, wave = uniform(threadIdx.x >> 6);
   Unit u;
   if (!find_unit<COLS, MOST>(a, blockIdx.x / a.c.kv_heads, &u)) return;
   const int all = u.rows * a.group, col0 = u.tile * COLS, mine0 = col0 + wave * 32;
@@ -635,6 +658,7 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
   u32x4 next[EACH];
   uint32_t next_ks = 0, next_vs = 0;
   auto fetch = [&](int page) {
+    const int tid = wave * 64 + w.lane;
     const int64_t ph = (int64_t)page * a.c.kv_heads + head;
     next_ks = *(const uint32_t*)(a.c.k_scale + ph * 4);
     next_vs = *(const uint32_t*)(a.c.v_scale + ph * 4);
@@ -647,6 +671,7 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
     }
   };
   auto store = [&](int buf) {
+    const int tid = wave * 64 + w.lane;
     u32x4* to = (u32x4*)smem_pages + buf * 2 * PIECES;
 #pragma unroll
     for (int i = 0; i < EACH / 2; ++i) {
@@ -694,8 +719,8 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
   w.mark_nans(a, u, head, lo, hi, 1, pos_lo, pos_hi);
   w.finish();
   if (cols > 0) {
-    const bool on = w.c < cols;
-    const int col = mine0 + (on ? w.c : 0), r = col / a.group;
+    const bool on = w.c() < cols;
+    const int col = mine0 + (on ? w.c() : 0), r = col / a.group;
     const int64_t at = (int64_t)(u.row0 + r) * a.out_row + (int64_t)(head * a.group + (col - r * a.group)) * a.out_head;
     float* part = part_numbers<COLS, D>(a, head, u.first + u.chunk);
     const float back = u.chunks > 1 ? 1.f : w.sum == 0.f ? 0.f : 1.f / w.sum;
@@ -706,12 +731,13 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
         for (int i = 0; i < 16; i += 4) {
           const float4 v = make_float4(w.o[t][i] * back, w.o[t][i + 1] * back, w.o[t][i + 2] * back, w.o[t][i + 3] * back);
           if (u.chunks == 1) put_out<BF16>(a, at + w.channel(t, i), v);
-          else put((void*)(part + (wave * 32 + w.c) * D + w.channel(t, i)), v);
+          else put((void*)(part + (wave * 32 + w.c()) * D + w.channel(t, i)), v);
         }
-      if (u.chunks > 1 && w.g == 0) leave2(part + COLS * D + 2 * (wave * 32 + w.c), w.top, w.sum);
+      if (u.chunks > 1 && w.g() == 0) leave2(part + COLS * D + 2 * (wave * 32 + w.c()), w.top, w.sum);
     }
   }
-  if (u.chunks > 1 && arrive(a, head, u, flag)) merge<COLS, D, BF16>(a, head, u, col0, lds);
+  const int tid = wave * 64 + w.lane;
+  if (u.chunks > 1 && arrive(a, head, u, flag, tid)) merge<COLS, D, BF16>(a, head, u, col0, lds, tid);
 }
 
 }  // namespace daris

@@ -261,7 +261,8 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
       bool on = out < a.n;
       if (a.gate) {
         // neighbouring lanes hold a pair: a row of the group is an even number of outputs, so pairs never part
-        const float other = __shfl_xor(s, 1);
+        float other, own;
+        lane_pair<1>(s, &own, &other);
         s = s / (1.f + expf(-s)) * other;
         on = on && !(out & 1);
         out >>= 1;

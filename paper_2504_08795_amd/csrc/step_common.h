@@ -44,18 +44,47 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(code_input(c), code_input(d), r, true);
 }
 
-template <int N>
-__device__ __forceinline__ float wave_max(float v) {  // over N neighbouring lanes
-#pragma unroll
-  for (int m = 1; m < N; m *= 2) v = fmaxf(v, __shfl_xor(v, m));
+// v of this lane and of the lane whose number differs by M (in either order).
+template <int M>
+__device__ __forceinline__ void lane_pair(float v, float* a, float* b) {
+  static_assert(M == 1 || M == 2 || M == 4 || M == 8 || M == 16 || M == 32, "a bit of the lane's number");
+  const int x = __builtin_bit_cast(int, v);
+  if constexpr (M == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    *a = __builtin_bit_cast(float, (int)r[0]);
+    *b = __builtin_bit_cast(float, (int)r[1]);
+  } else if constexpr (M == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    *a = __builtin_bit_cast(float, (int)r[0]);
+    *b = __builtin_bit_cast(float, (int)r[1]);
+  } else {
+    *a = v;
+    *b = __builtin_bit_cast(float, __builtin_amdgcn_ds_swizzle(x, (M << 10) | 0x1f));
+  }
+}
+// ... over lanes whose numbers differ in the bits FROM .. TO / 2: the result in all of them
+template <int FROM, int TO>
+__device__ __forceinline__ float lanes_max(float v) {
+  if constexpr (FROM < TO) {
+    float a, b;
+    lane_pair<FROM>(v, &a, &b);
+    return lanes_max<FROM * 2, TO>(fmaxf(a, b));
+  }
+  return v;
+}
+template <int FROM, int TO>
+__device__ __forceinline__ float lanes_sum(float v) {
+  if constexpr (FROM < TO) {
+    float a, b;
+    lane_pair<FROM>(v, &a, &b);
+    return lanes_sum<FROM * 2, TO>(a + b);
+  }
   return v;
 }
 template <int N>
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int m = 1; m < N; m *= 2) v += __shfl_xor(v, m);
-  return v;
-}
+__device__ __forceinline__ float wave_max(float v) { return lanes_max<1, N>(v); }  // over N neighbouring lanes
+template <int N>
+__device__ __forceinline__ float wave_sum(float v) { return lanes_sum<1, N>(v); }
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
