@@ -97,45 +97,65 @@ __device__ __forceinline__ int afresh(int v) {
 
 template <int XT, int G, int MT, bool BF16_OUT>
 __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
+  // (short: with one row a wave has two or three steps to do, and what it computes around them takes longer than the steps)
   constexpr int PARTS = XT == kRowsF32 ? 2 : 1, GS = 128 / G, ROWS = 16 * MT, WAVES = matvec_waves(MT), T = WAVES * 64;
-  constexpr int PIECES = matvec_pieces(PARTS), RING = 4;
+  constexpr int PIECES = matvec_pieces(PARTS), RING = 4, ES = XT == kRowsF32 ? 4 : XT == kRowsBf16 ? 2 : 1;
   constexpr bool AHEAD = MT > 1;  // a chunk of x travels while the one before is computed (sixteen waves have no registers for that)
   extern __shared__ uint4 smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, c = lane & 15;
-  const int across = a.across, split = WAVES / across;  // tiles side by side, waves on one of them
-  const int mb = blockIdx.x / a.wgs, m0 = mb * ROWS, rows = a.rows - m0 < ROWS ? a.rows - m0 : ROWS;
-  const int own_tile = wave / split, part = wave - own_tile * split;
-  const int groups = a.k / G, steps = (a.k + 127) / 128, cs = a.steps, chunks = (steps + cs - 1) / cs;
-  // LDS: x [PARTS][step][row][instruction, lane group], the last exchanged by the row's number so that rows lie on different banks, and (of scaled rows) their scales [step][group][ROWS], twice if there is more than
-  // one chunk; the weights' scales [across * 16][pitch] twice if there is more to come; sums [WAVES][ROWS][16]
-  const int pieces = cs * 16 * rows, x_size = PARTS * pieces + (XT == kRowsBf16 ? 0 : cs * GS * ROWS / 4), pitch = matvec_pitch(cs * GS);
-  uint16_t* const ws_lds = (uint16_t*)(smem + (chunks > 1 ? 2 : 1) * x_size);
-  const int ws_size = across * 16 * pitch;
-  const bool again = chunks > 1 || a.wgs < a.groups;
-  float* const red = (float*)(ws_lds + (again ? 2 : 1) * ws_size);
+  char* const lds = (char*)smem;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
+  const int split_log = (MT == 1 ? 4 : 3) - a.across;  // tiles side by side: 1 << across; waves on one of them: 1 << split_log
+  const int own_tile = wave >> split_log, part = wave & ((1 << split_log) - 1);
+  int m0 = 0, tg = blockIdx.x;
+  if (a.rows > ROWS) {
+    const int mb = tg / a.wgs;
+    m0 = mb * ROWS;
+    tg -= mb * a.wgs;
+  }
+  const int rows = a.rows - m0 < ROWS ? a.rows - m0 : ROWS;
+  const int cs = a.steps, steps = (a.k + 127) >> 7, chunks = a.chunks;
+  // LDS, in bytes: x [PARTS][step][row][instruction, lane group], the last exchanged by the row's number so that rows lie on different banks, and (of scaled
+  // rows) their scales [step][group][ROWS], twice if there is more than one chunk; the weights' scales [tiles * 16][pitch] twice if there is more to
+  // come; sums [WAVES][ROWS][16]
+  const int part_size = cs * rows * 256, x_size = PARTS * part_size + (XT == kRowsBf16 ? 0 : cs * GS * ROWS * 4), pitch = a.pitch * 2;
+  const int ws_at = (chunks > 1 ? 2 : 1) * x_size, ws_size = (16 << a.across) * pitch;
+  float* const red = (float*)(lds + ws_at + (chunks > 1 || a.wgs < a.groups ? 2 : 1) * ws_size);
 
   // ---- weights: the wave's steps of a chunk are neighbouring ones, so that it reads whole cache lines
-  const int own = (cs + split - 1) / split, first = part * own, turns = (own + RING - 1) / RING * RING;
+  const int own = (cs + (1 << split_log) - 1) >> split_log, first = part * own, turns = (own + RING - 1) & -RING;
+  struct List {  // the wave's steps of a tile in a chunk
+    const uint8_t* w;
+    int n, to_last;  // to_last: the step that ends K comes so many later than the first
+  };
+  auto list = [&](int tg, int ch) {
+    const int n = ((tg << a.across) + own_tile) * 16 + c, st = ch * cs + first;
+    List l;
+    l.n = tg < a.groups ? (cs < steps - ch * cs ? cs : steps - ch * cs) - first : 0;
+    l.n = l.n < own ? l.n : own;
+    l.to_last = steps - 1 - st;
+    l.w = a.w + (int64_t)(n < a.n ? n : a.n - 1) * a.w_row + st * 64 + g * 16;
+    return l;
+  };
+  // Channels past K: their x is 0, so any weights will do -- those of lane group 0.
+  const int past = (a.k & 127) != 0 && g * 32 >= (a.k & 127) ? -g * 16 : 0;
   uint4 ring[RING];
-  auto fetch = [&](int slot, int tg, int ch, int i) {
-    const int st = first + i, k = (ch * cs + st) * 128 + g * 32;
-    const int n = (tg * across + own_tile) * 16 + c;
-    ring[slot] = make_uint4(0u, 0u, 0u, 0u);
-    if (tg < a.groups && i < own && st < cs && k < a.k) ring[slot] = *(const uint4*)(a.w + (int64_t)(n < a.n ? n : a.n - 1) * a.w_row + k / 2);
+  auto fetch = [&](int slot, const List& l, int i) {
+    if (i < l.n) ring[slot] = *(const uint4*)(l.w + i * 64 + (i == l.to_last ? past : 0));
   };
   // ---- and their scales, eight neighbours a thread
-  uint32_t sc[kScalePieces][4];
-  const int eights = (cs * GS + 7) / 8;
+  const int groups = a.k / G;
+  u32x4 sc[kScalePieces];
   auto load_scales = [&](int tg, int ch) {
     const int tid = afresh(threadIdx.x);
 #pragma unroll
     for (int i = 0; i < kScalePieces; ++i) {
-      const int p = i * T + tid, r = p / eights, at = (p - r * eights) * 8, from = ch * cs * GS + at;
-      if (r >= across * 16 || from >= groups) continue;
-      const int n = tg * across * 16 + r;
+      if ((i * T) >> a.eights >= 16 << a.across) break;
+      const int p = i * T + tid, r = p >> a.eights, from = ch * cs * GS + (p & ((1 << a.eights) - 1)) * 8;
+      if (r >= 16 << a.across || from >= groups) continue;
+      const int n = (tg << a.across) * 16 + r;
       const uint16_t* s = a.w_scale + (int64_t)(n < a.n ? n : a.n - 1) * groups + from;
       if (from + 8 <= groups) {
-        __builtin_memcpy(sc[i], s, 16);
+        __builtin_memcpy(&sc[i], s, 16);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
@@ -151,9 +171,10 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
     const int tid = afresh(threadIdx.x);
 #pragma unroll
     for (int i = 0; i < kScalePieces; ++i) {
-      const int p = i * T + tid, r = p / eights, at = (p - r * eights) * 8;
-      if (r >= across * 16) continue;
-      uint32_t* to = (uint32_t*)(ws_lds + buf * ws_size + r * pitch + at);  // (the pitch is an odd number of words)
+      if ((i * T) >> a.eights >= 16 << a.across) break;
+      const int p = i * T + tid, r = p >> a.eights, at = (p & ((1 << a.eights) - 1)) * 16;
+      if (r >= 16 << a.across || at >= pitch - 4) continue;
+      uint32_t* to = (uint32_t*)(lds + ws_at + buf * ws_size + r * pitch + at);  // (the pitch is an odd number of words)
 #pragma unroll
       for (int e = 0; e < 4; ++e) to[e] = sc[i][e];
     }
@@ -161,51 +182,51 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
 
   // ---- rows of x: neighbouring threads take neighbouring pieces of a row
   RowPiece<XT> raw[PIECES];
+  const int row_log = a.chunk + 4, in_chunk = cs * 16;
   auto load = [&](int ch) {
     const int tid = afresh(threadIdx.x);
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int p = i * T + tid, m = p >> (a.chunk + 4), q = p & ((16 << a.chunk) - 1), k = ch * cs * 128 + q * 8;
+      if ((i * T) >> row_log >= rows) break;
+      const int p = i * T + tid, m = p >> row_log, q = p & ((1 << row_log) - 1), k = ch * cs * 128 + q * 8;
 #pragma unroll
       for (int e = 0; e < (XT == kRowsF32 ? 2 : 1); ++e) raw[i].v[e] = make_uint4(0u, 0u, 0u, 0u);
       raw[i].scale = 127;
-      if (m >= rows || q >= cs * 16 || k >= a.k) continue;
-      const int64_t at = (int64_t)(m0 + m) * a.x_row + k;
+      if (m >= rows || q >= in_chunk || k >= a.k) continue;
+      const char* x = (const char*)a.x + ((int64_t)(m0 + m) * a.x_row + k) * ES;
       if (XT == kRowsF8) {
         raw[i].scale = a.x_scale[(int64_t)(m0 + m) * groups + k / G];
-        const uint8_t* x = (const uint8_t*)a.x + at;
         if (a.x_vec) {
           const uint2 v = *(const uint2*)x;
           raw[i].v[0].x = v.x;
           raw[i].v[0].y = v.y;
         } else {
+          const uint8_t* b = (const uint8_t*)x;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            raw[i].v[0].x |= (uint32_t)x[e] << (8 * e);
-            raw[i].v[0].y |= (uint32_t)x[e + 4] << (8 * e);
+            raw[i].v[0].x |= (uint32_t)b[e] << (8 * e);
+            raw[i].v[0].y |= (uint32_t)b[e + 4] << (8 * e);
           }
         }
       } else if (XT == kRowsBf16) {
-        const uint16_t* x = (const uint16_t*)a.x + at;
+        const uint16_t* h = (const uint16_t*)x;
         if (a.x_vec) raw[i].v[0] = *(const uint4*)x;
-        else raw[i].v[0] = make_uint4(x[0] | (uint32_t)x[1] << 16, x[2] | (uint32_t)x[3] << 16, x[4] | (uint32_t)x[5] << 16, x[6] | (uint32_t)x[7] << 16);
+        else raw[i].v[0] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
       } else {
-        const uint32_t* x = (const uint32_t*)a.x + at;
+        const uint32_t* f = (const uint32_t*)x;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) raw[i].v[XT == kRowsF32 ? e : 0] = a.x_vec ? *(const uint4*)(x + 4 * e) : make_uint4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+        for (int e = 0; e < 2; ++e) raw[i].v[XT == kRowsF32 ? e : 0] = a.x_vec ? *(const uint4*)(f + 4 * e) : make_uint4(f[4 * e], f[4 * e + 1], f[4 * e + 2], f[4 * e + 3]);
       }
     }
   };
   auto stage = [&](int buf) {
-    uint4* frag = smem + buf * x_size;
-    float* xs = (float*)(frag + PARTS * pieces);
+    char* const frag = lds + buf * x_size;
     const int tid = afresh(threadIdx.x);
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int p = i * T + tid, m = p >> (a.chunk + 4), q = p & ((16 << a.chunk) - 1), in_step = (q & 15) * 8;
-      if ((i * T) >> (a.chunk + 4) >= rows) break;
+      if ((i * T) >> row_log >= rows) break;
+      const int p = i * T + tid, m = p >> row_log, q = p & ((1 << row_log) - 1), in_step = (q & 15) * 8;
       if (XT == kRowsF32) __builtin_amdgcn_sched_barrier(0);  // (piece by piece, or their parts do not fit the registers)
-      const int to = ((q >> 4) * rows + m) * 16 + (place<G>(in_step) ^ (m & 15));
       uint4 high, low = make_uint4(0u, 0u, 0u, 0u);
       float back = 1.f;
       if (XT == kRowsBf16) {
@@ -238,10 +259,11 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
         high = __builtin_bit_cast(uint4, h);
         low = __builtin_bit_cast(uint4, f16_in_order(rest));
       }
-      if (m < rows && q < cs * 16) {
-        frag[to] = high;
-        if (PARTS == 2) frag[pieces + to] = low;
-        if (XT != kRowsBf16 && (in_step & (G - 1)) == 0) xs[((q >> 4) * GS + in_step / G) * ROWS + m] = back;
+      if (m < rows && q < in_chunk) {
+        char* to = frag + (((q >> 4) * rows + m) * 16 + (place<G>(in_step) ^ (m & 15))) * 16;
+        *(uint4*)to = high;
+        if (PARTS == 2) *(uint4*)(to + part_size) = low;
+        if (XT != kRowsBf16 && (in_step & (G - 1)) == 0) ((float*)(frag + PARTS * part_size))[((q >> 4) * GS + in_step / G) * ROWS + m] = back;
       }
     }
   };
@@ -253,11 +275,14 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
 
   // the outputs of a group of tiles from the waves' sums
   auto write = [&](int tg) {
-    for (int i = afresh(threadIdx.x); i < rows * across * 16; i += T) {
-      const int m = i / (across * 16), o = i - m * across * 16, t = o >> 4, col = o & 15;
+    const int wide = a.across + 4;  // log2 of the outputs side by side
+    for (int i = afresh(threadIdx.x); i < rows << wide; i += T) {
+      const int m = i >> wide, o = i & ((1 << wide) - 1);
+      const float* r = red + (((o >> 4) << split_log) * ROWS + m) * 16 + (o & 15);
       float s = 0.f;
-      for (int p = 0; p < split; ++p) s += red[((t * split + p) * ROWS + m) * 16 + col];
-      int out = tg * across * 16 + o;
+#pragma unroll 4
+      for (int p = 0; p < 1 << split_log; ++p) s += r[p * ROWS * 16];
+      int out = (tg << wide) + o;
       bool on = out < a.n;
       if (a.gate) {
         // neighbouring lanes hold a pair: a row of the group is an even number of outputs, so pairs never part
@@ -274,11 +299,12 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
     }
   };
 
-  int tg = blockIdx.x - mb * a.wgs, ch = 0, buf = 0, last = -1;
+  int ch = 0, buf = 0, last = -1;
+  List now = list(tg, 0);
+#pragma unroll
+  for (int i = 0; i < RING; ++i) fetch(i, now, i);
   load(0);
   load_scales(tg, 0);
-#pragma unroll
-  for (int i = 0; i < RING; ++i) fetch(i, tg, 0, i);
   stage(0);
   stage_scales(0);
   for (;;) {
@@ -287,52 +313,64 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
     const bool over = ch + 1 == chunks;
     const int next_ch = over ? 0 : ch + 1, next = over ? tg + a.wgs : tg;
     const bool more = next < a.groups;
+    List after = now;
+    after.n = 0;
     if (more) {
+      after = list(next, next_ch);
       if (AHEAD && chunks > 1) load(next_ch);
       load_scales(next, next_ch);
     }
-    const uint4* frag = smem + (chunks > 1 ? buf * x_size : 0);
-    const float* xs = (const float*)(frag + PARTS * pieces);
-    const uint16_t* ws = ws_lds + buf * ws_size + (own_tile * 16 + c) * pitch;
+    const int x_at = chunks > 1 ? buf * x_size : 0;
+    int f[MT];  // where the wave's operands of its first step lie
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const int xr = m * 16 + c < rows ? m * 16 + c : rows - 1;
+      f[m] = x_at + ((first * rows + xr) * 16 + (g ^ (xr & 15))) * 16;
+    }
+    const char* xs = lds + x_at + PARTS * part_size + (first * GS * ROWS + g * 4) * 4;
+    const char* ws = lds + ws_at + buf * ws_size + (own_tile * 16 + c) * pitch + first * GS * 2;
 #pragma unroll 1
-    for (int i0 = 0; i0 < turns; i0 += RING) {
+    for (int i0 = 0; i0 < turns; i0 += RING, xs += RING * GS * ROWS * 4, ws += RING * GS * 2) {
 #pragma unroll
       for (int e = 0; e < RING; ++e) {
-        const int i = i0 + e, st = first + i;  // of the chunk
-        const uint4 now = arranged<G>(ring[e]);
-        if (i + RING < turns) fetch(e, tg, ch, i + RING);
-        else fetch(e, next, next_ch, i + RING - turns);
-        if (i >= own || st >= cs || ch * cs + st >= steps) continue;
-        const uint32_t wd[4] = {now.x, now.y, now.z, now.w};
+        const int i = i0 + e;
+        if (i >= now.n) {
+          if (i + RING >= turns) fetch(e, after, i + RING - turns);
+          continue;
+        }
+        const uint4 own_w = arranged<G>(ring[e]);
+        if (i + RING < turns) fetch(e, now, i + RING);
+        else fetch(e, after, i + RING - turns);
+        const uint32_t wd[4] = {own_w.x, own_w.y, own_w.z, own_w.w};
         uint4 b[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) b[j] = XT == kRowsBf16 ? __builtin_bit_cast(uint4, bf16_of_nibbles(wd[j])) : __builtin_bit_cast(uint4, f16_of_nibbles(wd[j]));
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          const int xr = m * 16 + c < rows ? m * 16 + c : rows - 1;
-          const int f = (st * rows + xr) * 16 + (g ^ (xr & 15));
 #pragma unroll
           for (int u = 0; u < GS; ++u) {
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int j = u * (4 / GS); j < (u + 1) * (4 / GS); ++j) {
-              const uint4 x = frag[f ^ (j * 4)];
+              const char* at = lds + (f[m] ^ (j * 64));
+              const uint4 x = *(const uint4*)at;
               if (XT == kRowsBf16) {
                 sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, b[j]), sum, 0, 0, 0);
                 sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), minus, sum, 0, 0, 0);
               } else {
-                if (PARTS == 2) sum = mfma16(__builtin_bit_cast(f16x8, frag[pieces + (f ^ (j * 4))]), __builtin_bit_cast(f16x8, b[j]), sum);
+                if (PARTS == 2) sum = mfma16(__builtin_bit_cast(f16x8, *(const uint4*)(at + part_size)), __builtin_bit_cast(f16x8, b[j]), sum);
                 sum = mfma16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, b[j]), sum);
               }
             }
-            const float by = bf16_bits_to_f32(ws[st * GS + u]);
+            const float by = bf16_bits_to_f32(*(const uint16_t*)(ws + (e * GS + u) * 2));
             float4 x4 = make_float4(1.f, 1.f, 1.f, 1.f);
-            if (XT != kRowsBf16) x4 = *(const float4*)(xs + (st * GS + u) * ROWS + m * 16 + g * 4);
+            if (XT != kRowsBf16) x4 = *(const float4*)(xs + ((e * GS + u) * ROWS + m * 16) * 4);
             total[m][0] = fmaf(sum[0], by * x4.x, total[m][0]);
             total[m][1] = fmaf(sum[1], by * x4.y, total[m][1]);
             total[m][2] = fmaf(sum[2], by * x4.z, total[m][2]);
             total[m][3] = fmaf(sum[3], by * x4.w, total[m][3]);
           }
+          f[m] += rows * 256;
         }
       }
     }
@@ -353,6 +391,7 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
     stage_scales(buf);
     tg = next;
     ch = next_ch;
+    now = after;
   }
   __syncthreads();
   write(last);

@@ -88,9 +88,12 @@ struct MatvecArgs {
   int x_vec;   // rows of x are 16-byte vectors (8-byte ones of codes)
   int steps;   // of 128 channels, in a chunk of K that LDS holds
   int chunk;   // log2 of them, rounded up
-  int across;  // tiles (16 outputs) of a workgroup side by side: a power of two; its other waves share them
+  int chunks;
+  int across;  // log2 of a workgroup's tiles (16 outputs) side by side; its other waves share them
   int groups;  // of so many tiles
   int wgs;     // workgroups of a block of rows
+  int eights;  // log2 of the pieces of scales that a tile's row has in a chunk, rounded up
+  int pitch;   // matvec_pitch of a chunk
 };
 
 }  // namespace daris

@@ -259,7 +259,7 @@ inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int 
     return log;
   };
   auto fits = [&](int cs, int across) {
-    return ((16ll << log2_up(cs)) * rows <= matvec_pieces(parts) * waves * 64) && (cs * per_group + 7) / 8 * across * 16 <= kScalePieces * waves * 64 && lds(cs, across) <= 160 * 1024;
+    return ((16ll << log2_up(cs)) * rows <= matvec_pieces(parts) * waves * 64) && (across * 16 << log2_up((cs * per_group + 7) / 8)) <= kScalePieces * waves * 64 && lds(cs, across) <= 160 * 1024;
   };
   // Tiles side by side in a workgroup: what makes the shortest sequence of steps for a wave, on the most workgroups.  A wave's share of a chunk
   // counts in fours (its steps travel four at a time), and a barrier as two steps.
@@ -275,16 +275,19 @@ inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int 
     const int64_t own = ((int64_t)cs * across + waves - 1) / waves, cost = rounds * chunks * ((own + 3) / 4 * 4 + 2);
     if (best >= 0 && cost >= best) continue;
     best = cost;
-    a.across = across;
+    a.across = log2_up(across);
     a.steps = cs;
+    a.chunks = (int)chunks;
     a.groups = (int)groups;
     a.wgs = (int)(groups < room ? groups : room);
   }
   if (best < 0) return "no chunk of K fits LDS";
   a.chunk = log2_up(a.steps);
+  a.eights = log2_up((a.steps * per_group + 7) / 8);
+  a.pitch = matvec_pitch(a.steps * per_group);
   set_args(l, a);
   const int g = o.group == 32 ? 0 : o.group == 64 ? 1 : 2;
-  return set_grid(l, t.matvec[type][g][many], (int64_t)a.wgs * blocks, waves * 64, lds(a.steps, a.across)) ? "" : kTooMany;
+  return set_grid(l, t.matvec[type][g][many], (int64_t)a.wgs * blocks, waves * 64, lds(a.steps, 1 << a.across)) ? "" : kTooMany;
 }
 
 // What is wrong with an operator, or "".
