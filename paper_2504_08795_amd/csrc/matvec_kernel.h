@@ -3,8 +3,8 @@
 // y^T is computed in tiles of 16 outputs: a wave reads 16 rows of weights, 128 channels (a step) at a time, 16 bytes a lane straight
 // into registers, spreads the nibbles and multiplies them with the rows of x on the matrix instructions.  A group's sum is
 // taken by them alone and multiplied by the weights' scale once, in fp32.  x lies in LDS in the order of the nibbles.
-//   bf16 x: as it is.  0x4300 | c is the bf16 number 128 + c; a second product with the constant -136 takes the rest away in the same
-//     accumulator.  Sums are 17 times as large as the result on the way, which costs four of fp32's 24 bits.
+//   bf16 x: as it is.  0x4300 | c is the bf16 number 128 + c; a second product with the constant -136 takes the rest away.  Both sums are 17 times
+//     as large as the result, which costs four of fp32's 24 bits.
 //   fp32 x: two f16 parts (22 bits), a group of a row divided by a power of two that makes its largest number 2^14 and more, so that
 //     nothing overflows; 0x6400 | c is the f16 number 1024 + c, one packed addition makes it c - 8.
 //   e4m3 x: f16 holds every one of them.
@@ -19,20 +19,27 @@ namespace daris {
 
 enum { kRowsF32 = 0, kRowsBf16 = 1, kRowsF8 = 2 };
 
-// Eight nibbles as f16 in the order 0 4 1 5 2 6 3 7.
-__device__ __forceinline__ f16x8 f16_of_nibbles(uint32_t w) {
-  const f16x2 minus = {(_Float16)-1032.0f, (_Float16)-1032.0f};
-  f16x2 p[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) p[i] = __builtin_bit_cast(f16x2, ((w >> (4 * i)) & 0x000f000fu) | 0x64006400u) + minus;
-  return halves(p[0], p[1], p[2], p[3]);
-}
-
-// ... plus 128 as bf16.
-__device__ __forceinline__ bf16x8 bf16_of_nibbles(uint32_t w) {
-  const uint4 v = make_uint4((w & 0x000f000fu) | 0x43004300u, ((w >> 4) & 0x000f000fu) | 0x43004300u, ((w >> 8) & 0x000f000fu) | 0x43004300u, ((w >> 12) & 0x000f000fu) | 0x43004300u);
-  return __builtin_bit_cast(bf16x8, v);
-}
+// What spreads nibbles: the constants stay in registers (an instruction that takes both as literals does not exist, and two take twice as long).
+template <int XT>
+struct Spread {
+  uint32_t mask = 0x000f000fu, high = XT == kRowsBf16 ? 0x43004300u : 0x64006400u;
+  u32x4 minus = {0xc308c308u, 0xc308c308u, 0xc308c308u, 0xc308c308u};  // -136 as bf16
+  __device__ __forceinline__ Spread() {
+    asm volatile("" : "+s"(mask));
+    asm volatile("" : "+v"(high));
+    if (XT == kRowsBf16) asm volatile("" : "+v"(minus));
+  }
+  // Eight nibbles in the order 0 4 1 5 2 6 3 7: plus 128 as bf16, or minus 8 as f16.
+  __device__ __forceinline__ uint4 operator()(uint32_t w) const {
+    uint4 v = make_uint4((w & mask) | high, ((w >> 4) & mask) | high, ((w >> 8) & mask) | high, ((w >> 12) & mask) | high);
+    if (XT != kRowsBf16) {
+      const f16x2 less = {(_Float16)-1032.0f, (_Float16)-1032.0f};
+      v = make_uint4(__builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v.x) + less), __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v.y) + less),
+                     __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v.z) + less), __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v.w) + less));
+    }
+    return v;
+  }
+};
 
 // Eight channels of x in the nibbles' order.
 __device__ __forceinline__ f16x8 f16_in_order(const float (&v)[8]) {
@@ -102,7 +109,8 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
   constexpr int PIECES = matvec_pieces(PARTS), RING = 4, ES = XT == kRowsF32 ? 4 : XT == kRowsBf16 ? 2 : 1;
   constexpr bool AHEAD = MT > 1;  // a chunk of x travels while the one before is computed (sixteen waves have no registers for that)
   extern __shared__ uint4 smem[];
-  char* const lds = (char*)smem;
+  typedef char __attribute__((address_space(3))) * Lds;
+  const Lds lds = (Lds)smem;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
   const int split_log = (MT == 1 ? 4 : 3) - a.across;  // tiles side by side: 1 << across; waves on one of them: 1 << split_log
   const int own_tile = wave >> split_log, part = wave & ((1 << split_log) - 1);
@@ -119,13 +127,13 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
   // come; sums [WAVES][ROWS][16]
   const int part_size = cs * rows * 256, x_size = PARTS * part_size + (XT == kRowsBf16 ? 0 : cs * GS * ROWS * 4), pitch = a.pitch * 2;
   const int ws_at = (chunks > 1 ? 2 : 1) * x_size, ws_size = (16 << a.across) * pitch;
-  float* const red = (float*)(lds + ws_at + (chunks > 1 || a.wgs < a.groups ? 2 : 1) * ws_size);
+  float __attribute__((address_space(3)))* const red = (float __attribute__((address_space(3)))*)(lds + ws_at + (chunks > 1 || a.wgs < a.groups ? 2 : 1) * ws_size);
 
   // ---- weights: the wave's steps of a chunk are neighbouring ones, so that it reads whole cache lines
   const int own = (cs + (1 << split_log) - 1) >> split_log, first = part * own, turns = (own + RING - 1) & -RING;
-  struct List {  // the wave's steps of a tile in a chunk
+  struct List {  // the wave's steps of a tile in a chunk: where the first is, how many there are, how much later the step comes that ends K
     const uint8_t* w;
-    int n, to_last;  // to_last: the step that ends K comes so many later than the first
+    int n, to_last;
   };
   auto list = [&](int tg, int ch) {
     const int n = ((tg << a.across) + own_tile) * 16 + c, st = ch * cs + first;
@@ -138,9 +146,12 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
   };
   // Channels past K: their x is 0, so any weights will do -- those of lane group 0.
   const int past = (a.k & 127) != 0 && g * 32 >= (a.k & 127) ? -g * 16 : 0;
-  uint4 ring[RING];
+  u32x4 ring[RING];
+  // Steps i .. i + RING - 1 of a list.  A step that is none is fetched too, from one place for all lanes: a load that may or may not have been issued makes
+  // the wave wait for all of them.
   auto fetch = [&](int slot, const List& l, int i) {
-    if (i < l.n) ring[slot] = *(const uint4*)(l.w + i * 64 + (i == l.to_last ? past : 0));
+    const uint8_t* from = i < l.n ? l.w + i * 64 + (i == l.to_last ? past : 0) : a.w;
+    ring[slot] = *(const u32x4*)from;
   };
   // ---- and their scales, eight neighbours a thread
   const int groups = a.k / G;
@@ -174,7 +185,7 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
       if ((i * T) >> a.eights >= 16 << a.across) break;
       const int p = i * T + tid, r = p >> a.eights, at = (p & ((1 << a.eights) - 1)) * 16;
       if (r >= 16 << a.across || at >= pitch - 4) continue;
-      uint32_t* to = (uint32_t*)(lds + ws_at + buf * ws_size + r * pitch + at);  // (the pitch is an odd number of words)
+      uint32_t __attribute__((address_space(3)))* to = (uint32_t __attribute__((address_space(3)))*)(lds + ws_at + buf * ws_size + r * pitch + at);  // (the pitch is an odd number of words)
 #pragma unroll
       for (int e = 0; e < 4; ++e) to[e] = sc[i][e];
     }
@@ -220,7 +231,7 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
     }
   };
   auto stage = [&](int buf) {
-    char* const frag = lds + buf * x_size;
+    const Lds frag = lds + buf * x_size;
     const int tid = afresh(threadIdx.x);
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
@@ -260,10 +271,10 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
         low = __builtin_bit_cast(uint4, f16_in_order(rest));
       }
       if (m < rows && q < in_chunk) {
-        char* to = frag + (((q >> 4) * rows + m) * 16 + (place<G>(in_step) ^ (m & 15))) * 16;
-        *(uint4*)to = high;
-        if (PARTS == 2) *(uint4*)(to + part_size) = low;
-        if (XT != kRowsBf16 && (in_step & (G - 1)) == 0) ((float*)(frag + PARTS * part_size))[((q >> 4) * GS + in_step / G) * ROWS + m] = back;
+        const Lds to = frag + (((q >> 4) * rows + m) * 16 + (place<G>(in_step) ^ (m & 15))) * 16;
+        *(u32x4 __attribute__((address_space(3)))*)to = __builtin_bit_cast(u32x4, high);
+        if (PARTS == 2) *(u32x4 __attribute__((address_space(3)))*)(to + part_size) = __builtin_bit_cast(u32x4, low);
+        if (XT != kRowsBf16 && (in_step & (G - 1)) == 0) ((float __attribute__((address_space(3)))*)(frag + PARTS * part_size))[((q >> 4) * GS + in_step / G) * ROWS + m] = back;
       }
     }
   };
@@ -271,14 +282,14 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
   f32x4 total[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) total[m] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const bf16x8 minus = __builtin_bit_cast(bf16x8, make_uint4(0xc308c308u, 0xc308c308u, 0xc308c308u, 0xc308c308u));  // -136
+  const Spread<XT> spread;
 
   // the outputs of a group of tiles from the waves' sums
   auto write = [&](int tg) {
     const int wide = a.across + 4;  // log2 of the outputs side by side
     for (int i = afresh(threadIdx.x); i < rows << wide; i += T) {
       const int m = i >> wide, o = i & ((1 << wide) - 1);
-      const float* r = red + (((o >> 4) << split_log) * ROWS + m) * 16 + (o & 15);
+      const float __attribute__((address_space(3)))* r = red + (((o >> 4) << split_log) * ROWS + m) * 16 + (o & 15);
       float s = 0.f;
 #pragma unroll 4
       for (int p = 0; p < 1 << split_log; ++p) s += r[p * ROWS * 16];
@@ -327,48 +338,55 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
       const int xr = m * 16 + c < rows ? m * 16 + c : rows - 1;
       f[m] = x_at + ((first * rows + xr) * 16 + (g ^ (xr & 15))) * 16;
     }
-    const char* xs = lds + x_at + PARTS * part_size + (first * GS * ROWS + g * 4) * 4;
-    const char* ws = lds + ws_at + buf * ws_size + (own_tile * 16 + c) * pitch + first * GS * 2;
+    Lds xs = lds + x_at + PARTS * part_size + (first * GS * ROWS + g * 4) * 4;
+    Lds ws = lds + ws_at + buf * ws_size + (own_tile * 16 + c) * pitch + first * GS * 2;
 #pragma unroll 1
     for (int i0 = 0; i0 < turns; i0 += RING, xs += RING * GS * ROWS * 4, ws += RING * GS * 2) {
+      const bool same = i0 + RING < turns;
+      const List ahead = same ? now : after;
+      const int from = same ? i0 + RING : 0;
 #pragma unroll
       for (int e = 0; e < RING; ++e) {
-        const int i = i0 + e;
-        if (i >= now.n) {
-          if (i + RING >= turns) fetch(e, after, i + RING - turns);
-          continue;
-        }
-        const uint4 own_w = arranged<G>(ring[e]);
-        if (i + RING < turns) fetch(e, now, i + RING);
-        else fetch(e, after, i + RING - turns);
-        const uint32_t wd[4] = {own_w.x, own_w.y, own_w.z, own_w.w};
-        uint4 b[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) b[j] = XT == kRowsBf16 ? __builtin_bit_cast(uint4, bf16_of_nibbles(wd[j])) : __builtin_bit_cast(uint4, f16_of_nibbles(wd[j]));
+        const u32x4 mine = ring[e];
+        fetch(e, ahead, from + e);
+        if (i0 + e >= now.n) continue;
+        const uint4 own_w = arranged<G>(__builtin_bit_cast(uint4, mine));
+        const uint4 b[4] = {spread(own_w.x), spread(own_w.y), spread(own_w.z), spread(own_w.w)};
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
+          u32x4 x[PARTS][4];
+          auto operand = [&](int j) {
+            const Lds at = lds + (f[m] ^ (j * 64));
+            x[0][j] = *(const u32x4 __attribute__((address_space(3)))*)at;
+            if (PARTS == 2) x[PARTS - 1][j] = *(const u32x4 __attribute__((address_space(3)))*)(at + part_size);
+          };
+          if (PARTS == 1) {  // (both parts of all four do not fit sixteen waves' registers)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) operand(j);
+          }
 #pragma unroll
           for (int u = 0; u < GS; ++u) {
-            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f}, less = {0.f, 0.f, 0.f, 0.f};  // two chains: an instruction waits for the one it adds to
 #pragma unroll
             for (int j = u * (4 / GS); j < (u + 1) * (4 / GS); ++j) {
-              const char* at = lds + (f[m] ^ (j * 64));
-              const uint4 x = *(const uint4*)at;
+              if (PARTS == 2) operand(j);
               if (XT == kRowsBf16) {
-                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, b[j]), sum, 0, 0, 0);
-                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), minus, sum, 0, 0, 0);
+                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[0][j]), __builtin_bit_cast(bf16x8, b[j]), sum, 0, 0, 0);
+                less = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[0][j]), __builtin_bit_cast(bf16x8, spread.minus), less, 0, 0, 0);
               } else {
-                if (PARTS == 2) sum = mfma16(__builtin_bit_cast(f16x8, *(const uint4*)(at + part_size)), __builtin_bit_cast(f16x8, b[j]), sum);
-                sum = mfma16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, b[j]), sum);
+                sum = mfma16(__builtin_bit_cast(f16x8, x[0][j]), __builtin_bit_cast(f16x8, b[j]), sum);
+                if (PARTS == 2) less = mfma16(__builtin_bit_cast(f16x8, x[PARTS - 1][j]), __builtin_bit_cast(f16x8, b[j]), less);
               }
             }
-            const float by = bf16_bits_to_f32(*(const uint16_t*)(ws + (e * GS + u) * 2));
-            float4 x4 = make_float4(1.f, 1.f, 1.f, 1.f);
-            if (XT != kRowsBf16) x4 = *(const float4*)(xs + ((e * GS + u) * ROWS + m * 16) * 4);
-            total[m][0] = fmaf(sum[0], by * x4.x, total[m][0]);
-            total[m][1] = fmaf(sum[1], by * x4.y, total[m][1]);
-            total[m][2] = fmaf(sum[2], by * x4.z, total[m][2]);
-            total[m][3] = fmaf(sum[3], by * x4.w, total[m][3]);
+            if (XT == kRowsBf16 || PARTS == 2) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q) sum[q] += less[q];
+            }
+            const float by = bf16_bits_to_f32(*(const uint16_t __attribute__((address_space(3)))*)(ws + (e * GS + u) * 2));
+            f32x4 x4 = {1.f, 1.f, 1.f, 1.f};
+            if (XT != kRowsBf16) x4 = *(const f32x4 __attribute__((address_space(3)))*)(xs + ((e * GS + u) * ROWS + m * 16) * 4);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) total[m][q] = fmaf(sum[q], by * x4[q], total[m][q]);
           }
           f[m] += rows * 256;
         }
