@@ -190,6 +190,20 @@ __device__ __forceinline__ void turn_queries(const AppendArgs& a, int row, int h
   }
 }
 
+// The last sequence s whose first_row(s) / DIV + PER s is at most `at` (they grow with s), found by all lanes at once: a search by halves would wait
+// for memory once for every halving.
+template <int DIV, int PER>
+__device__ __forceinline__ int sequence_at(const CacheArgs& c, int at) {
+  int found = 0;
+  for (int s0 = 0; s0 < c.n_seqs; s0 += 64) {
+    const int s = s0 + (threadIdx.x & 63);
+    const int n = __popcll(__ballot(s < c.n_seqs && first_row(c, s < c.n_seqs ? s : 0) / DIV + PER * s <= at));
+    found += n;
+    if (n < 64) break;
+  }
+  return found > 0 ? found - 1 : 0;
+}
+
 // Waves: first a.items sixteenths x key heads, then a.q_items groups of query heads.
 template <bool BF16, int D>
 __device__ __forceinline__ void append_body(const AppendArgs& a) {
@@ -197,16 +211,9 @@ __device__ __forceinline__ void append_body(const AppendArgs& a) {
   if (wave < a.items) {
     const int item = wave / a.c.kv_heads, head = wave - item * a.c.kv_heads;
     // Sequence s has the items from first_row(s) / 16 + 2 s on: n tokens lie in at most n / 16 + 2 sixteenths.
-    int s = item;
-    int base = item;
+    int s = item, base = item;
     if (a.c.row_start) {
-      int lo = 0, hi = a.c.n_seqs - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (first_row(a.c, mid) / kScaleTokens + 2 * mid <= item) lo = mid;
-        else hi = mid - 1;
-      }
-      s = lo;
+      s = sequence_at<kScaleTokens, 2>(a.c, item);
       base = first_row(a.c, s) / kScaleTokens + 2 * s;
     }
     if (s >= a.c.n_seqs) return;
@@ -226,13 +233,7 @@ __device__ __forceinline__ void append_body(const AppendArgs& a) {
     const int i = wave - a.items, row = i / per_row, head = (i - row * per_row) * kTurnHeads;
     int s = row;
     if (a.c.row_start) {
-      int lo = 0, hi = a.c.n_seqs - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (first_row(a.c, mid) <= row) lo = mid;
-        else hi = mid - 1;
-      }
-      s = lo;
+      s = sequence_at<1, 0>(a.c, row);
       if (row < first_row(a.c, s) || row >= first_row(a.c, s + 1)) return;
     }
     turn_queries<BF16, D>(a, row, head, tokens_before(a.c, s) + (row - first_row(a.c, s)));

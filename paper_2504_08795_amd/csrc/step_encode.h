@@ -225,7 +225,7 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   const int cols = wide ? kWideColumns : kNarrowColumns;
   const int64_t tiles = columns / cols + o.cache.n_seqs;  // at most: each sequence's last one may be part of a tile
   // enough workgroups for the CUs to hold several each; wide tiles that are that many by themselves are not cut
-  const int64_t aim = (wide ? 2 : 3) * (int64_t)n_cu / o.cache.kv_heads;
+  const int64_t aim = 2 * (int64_t)n_cu / o.cache.kv_heads;
   a.target = wide && columns / cols >= aim ? 0 : aim < 1 ? 1 : (int)aim;
   const int64_t units = tiles + a.target + 1;
   if (units * o.cache.kv_heads > 0x7fffffll) return kTooMany;
