@@ -116,6 +116,8 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
 // The lowest n bytes of a word.
 __device__ __forceinline__ uint32_t bytes_below(int n) { return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
 
+// The lowest n halves of a word.
+__device__ __forceinline__ uint32_t halves_below(int n) { return n >= 2 ? 0xffffffffu : n <= 0 ? 0u : 0xffffu; }
 // A channel's codes of tokens t1 .. t1 + 15, those outside [lo, hi] cleared.
 __device__ __forceinline__ uint4 seen(uint4 x, int t1, int lo, int hi) {
   const int a = lo - t1, b = hi + 1 - t1;
@@ -237,8 +239,23 @@ struct Columns {
     uint4 kr[KT][KV];
     uint4 vr[VT][HALVES];
     uint32_t ks, vs;  // four scale bytes each
-    __device__ __forceinline__ uint4 k(int t, int i) const { return kr[t][i]; }
-    __device__ __forceinline__ uint4 v(int t, int h) const { return vr[t][h]; }
+    __device__ __forceinline__ f16x8 key(int t, int j) const {
+      const uint4& w = kr[t][j >> 1];
+      return j & 1 ? f16_of_codes(w.z, w.w) : f16_of_codes(w.x, w.y);
+    }
+    // The sixteen values of a channel; MASKED: those of tokens outside [lo, hi] and NaN codes as 0, *found: there were such codes.
+    template <bool MASKED>
+    __device__ __forceinline__ void values(int t, int h, int t1, int lo, int hi, uint32_t* found, f16x8 (&x)[2]) const {
+      uint4 w = vr[t][h];
+      if (MASKED) {
+        w = seen(w, t1, lo, hi);
+        const uint4 n = make_uint4(nan_bytes(w.x), nan_bytes(w.y), nan_bytes(w.z), nan_bytes(w.w));
+        *found |= n.x | n.y | n.z | n.w;
+        w = make_uint4(w.x & ~n.x, w.y & ~n.y, w.z & ~n.z, w.w & ~n.w);
+      }
+      x[0] = f16_of_codes(w.x, w.y);
+      x[1] = f16_of_codes(w.z, w.w);
+    }
   };
   __device__ __forceinline__ void fetch(const AttendArgs& a, int head, int page, Page* p) const {
     const int64_t ph = (int64_t)page * a.c.kv_heads + head;
@@ -278,8 +295,7 @@ struct Columns {
       #pragma unroll
       for (int j = 0; j < KS; j += 2) {
         if (P::kShared) __builtin_amdgcn_sched_barrier(0);  // (one after the other: the operands of all would not fit the registers)
-        const uint4 w = p.k(t, j >> 1);
-        const f16x8 lo = f16_of_codes(w.x, w.y), hi = f16_of_codes(w.z, w.w);
+        const f16x8 lo = p.key(t, j), hi = p.key(t, j + 1);
         if (PARTS == 2) {
           s[t] = mma(lo, q[PARTS - 1][j], s[t]);
           s[t] = mma(hi, q[PARTS - 1][j + 1], s[t]);
@@ -342,14 +358,9 @@ struct Columns {
       if (P::kShared) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) {
-        uint4 x = p.v(t, h);
-        if (MASKED) {
-          x = seen(x, t0 + sixteenth(h) * 16, see_lo, see_hi);
-          const uint4 n = make_uint4(nan_bytes(x.x), nan_bytes(x.y), nan_bytes(x.z), nan_bytes(x.w));
-          found |= n.x | n.y | n.z | n.w;
-          x = make_uint4(x.x & ~n.x, x.y & ~n.y, x.z & ~n.z, x.w & ~n.w);
-        }
-        const f16x8 lo = f16_of_codes(x.x, x.y), hi = f16_of_codes(x.z, x.w);
+        f16x8 x[2];
+        p.template values<MASKED>(t, h, t0 + sixteenth(h) * 16, see_lo, see_hi, &found, x);
+        const f16x8 lo = x[0], hi = x[1];
         if (PARTS == 2) {
           o[t] = mma(lo, w[PARTS - 1][h * 2], o[t]);
           o[t] = mma(hi, w[PARTS - 1][h * 2 + 1], o[t]);
@@ -607,32 +618,51 @@ __device__ __forceinline__ void attend_narrow_body(const AttendArgs& a) {
   if (u.chunks > 1 && arrive(a, head, u, flag, tid)) merge<COLS, D, BF16>(a, head, u, col0, lds, tid);
 }
 
-// A page in LDS, shared by the waves of a workgroup.  Sixteen neighbouring lanes read sixteen keys (channels) at one place, so the 16-byte
-// pieces of a row are exchanged by what tells these rows apart, and the lanes find them on different banks.
+// A page in LDS as f16, shared by the waves of a workgroup.  Sixteen neighbouring lanes read sixteen keys (channels) at one place, so the
+// 16-byte pieces of a row are exchanged by what tells these rows apart, and the lanes find them on different banks.
 template <int D>
 struct SharedPage {
   static constexpr bool kShared = true;
-  static constexpr int PIECES = kPage * D / 16;  // of K; as many of V behind them
-  const uint4* lds;
+  static constexpr int ROW = D / 8;             // pieces of a key (of a channel: eight)
+  static constexpr int PIECES = kPage * ROW;    // of K; as many of V behind them
+  const u32x4* lds;
   uint32_t ks, vs;
   int lane;
   static __device__ __forceinline__ int key_place(int token, int piece) {
-    constexpr int ROW = D / 16;  // pieces of a key
-    return token * ROW + (piece ^ (((token & 7) | ((token >> 1) & 8)) / (16 / ROW)));
+    const int by = (token & 7) | ((token >> 1) & 8);  // what tells the tokens of sixteen lanes apart
+    return token * ROW + (piece ^ (ROW >= 16 ? by : by >> 1));
   }
-  static __device__ __forceinline__ int value_place(int channel, int piece) { return PIECES + channel * 4 + (piece ^ ((channel >> 2) & 3)); }
-  __device__ __forceinline__ uint4 k(int t, int i) const {
-    return lds[key_place(Columns<true, D, 32>::token_of(t, lane & 31), (lane >> 5) * (D / 32) + i)];
+  static __device__ __forceinline__ int value_place(int channel, int piece) { return PIECES + channel * 8 + (piece ^ ((channel >> 1) & 7)); }
+  __device__ __forceinline__ f16x8 key(int t, int j) const {
+    return __builtin_bit_cast(f16x8, lds[key_place(Columns<true, D, 32>::token_of(t, lane & 31), (lane >> 5) * (D / 16) + j)]);
   }
-  __device__ __forceinline__ uint4 v(int t, int h) const { return lds[value_place(t * 32 + (lane & 31), h * 2 + (lane >> 5))]; }
+  template <bool MASKED>
+  __device__ __forceinline__ void values(int t, int h, int t1, int lo, int hi, uint32_t* found, f16x8 (&x)[2]) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      u32x4 w = lds[value_place(t * 32 + (lane & 31), (h * 2 + (lane >> 5)) * 2 + i)];
+      if (MASKED) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int t2 = t1 + i * 8 + e * 2;
+          w[e] &= halves_below(hi + 1 - t2) & ~halves_below(lo - t2);
+          // a NaN has all bits of the exponent, which no finite code has as f16
+          const uint32_t n = ((~(((w[e] & 0x7c007c00u) ^ 0x7c007c00u) + 0x7fff7fffu) & 0x80008000u) >> 15) * 0xffffu;
+          *found |= n;
+          w[e] &= ~n;
+        }
+      }
+      x[i] = __builtin_bit_cast(f16x8, w);
+    }
+  }
 };
 
 // Four waves side by side on 32 columns each.  They share the pages: each fetches a quarter of the next one in whole cache lines while
-// the present one is used from LDS (a wave's operands straight from memory are 32 rows a load, 64 cycles of the CU's address
+// the present one is used from LDS, and spreads it to f16 once for all (a wave's operands straight from memory are 32 rows a load, 64 cycles of the CU's address
 // unit: 4096 a page for the four, of 1024 for the matrix instructions).
 template <bool BF16, int D>
 __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
-  constexpr int COLS = 128, MOST = kWideUnits, PIECES = SharedPage<D>::PIECES, EACH = 2 * PIECES / 256;  // pieces of a page that a thread fetches
+  constexpr int COLS = 128, MOST = kWideUnits, PIECES = SharedPage<D>::PIECES, EACH = kPage * D / 16 / 256 * 2;  // 16-byte pieces of a page that a thread fetches
   extern __shared__ uint4 smem_pages[];
   float* lds = (float*)smem_pages;  // two pages; later for the merge [2][MOST][128]; a flag
   int* flag = (int*)(lds + wide_numbers(D));
@@ -676,8 +706,12 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
 #pragma unroll
     for (int i = 0; i < EACH / 2; ++i) {
       const int n = i * 256 + tid;
-      to[SharedPage<D>::key_place(n / (D / 16), n % (D / 16))] = next[i];
-      to[SharedPage<D>::value_place(n / 4, n % 4)] = next[EACH / 2 + i];
+      const u32x4 k = next[i], v = next[EACH / 2 + i];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        to[SharedPage<D>::key_place(n / (D / 16), n % (D / 16) * 2 + e)] = __builtin_bit_cast(u32x4, f16_of_codes(k[2 * e], k[2 * e + 1]));
+        to[SharedPage<D>::value_place(n / 4, n % 4 * 2 + e)] = __builtin_bit_cast(u32x4, f16_of_codes(v[2 * e], v[2 * e + 1]));
+      }
     }
   };
   // page numbers, 64 at a time (a wave has them all: the loop is the same for all four)
@@ -705,7 +739,7 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
   while (p < hi) {
     __syncthreads();
     SharedPage<D> now;
-    now.lds = smem_pages + buf * 2 * PIECES;
+    now.lds = (const u32x4*)smem_pages + buf * 2 * PIECES;
     now.ks = next_ks;
     now.vs = next_vs;
     now.lane = w.lane;

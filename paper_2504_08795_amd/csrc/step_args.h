@@ -66,7 +66,7 @@ constexpr int narrow_numbers(int dim) {
   return 4 * kNarrowColumns * (dim + 4) > 2 * kNarrowUnits * kNarrowColumns ? 4 * kNarrowColumns * (dim + 4) : 2 * kNarrowUnits * kNarrowColumns;
 }
 constexpr int narrow_lds(int dim) { return (narrow_numbers(dim) + 8 * kNarrowColumns + 4) * 4; }
-constexpr int wide_numbers(int dim) { return 2 * 2 * kPage * dim / 4 > 2 * kWideUnits * kWideColumns ? 2 * 2 * kPage * dim / 4 : 2 * kWideUnits * kWideColumns; }
+constexpr int wide_numbers(int dim) { return 2 * 2 * kPage * dim / 2 > 2 * kWideUnits * kWideColumns ? 2 * 2 * kPage * dim / 2 : 2 * kWideUnits * kWideColumns; }
 constexpr int wide_lds(int dim) { return (wide_numbers(dim) + 4) * 4; }
 // numbers of a unit in AttendArgs::part
 constexpr int64_t unit_floats(int columns, int dim) { return (int64_t)columns * (dim + 2); }
