@@ -289,20 +289,40 @@ struct Columns {
     uint32_t found = 0;
     Acc s[KT];
 #pragma unroll
-    for (int t = 0; t < KT; ++t) {
+    for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int i = 0; i < R; ++i) s[t][i] = 0.f;
-      #pragma unroll
-      for (int j = 0; j < KS; j += 2) {
-        if (P::kShared) __builtin_amdgcn_sched_barrier(0);  // (one after the other: the operands of all would not fit the registers)
-        const f16x8 lo = p.key(t, j), hi = p.key(t, j + 1);
-        if (PARTS == 2) {
-          s[t] = mma(lo, q[PARTS - 1][j], s[t]);
-          s[t] = mma(hi, q[PARTS - 1][j + 1], s[t]);
+    if constexpr (P::kShared) {
+      // one pair of operands ahead of the instructions, in this order: left to itself the compiler reads all of them first, for which
+      // there are no registers, or each when it is needed
+      f16x8 k[KT], next[KT];
+#pragma unroll
+      for (int t = 0; t < KT; ++t) k[t] = p.key(t, 0);
+#pragma unroll
+      for (int j = 0; j < KS; ++j) {
+        if (j + 1 < KS) {
+#pragma unroll
+          for (int t = 0; t < KT; ++t) next[t] = p.key(t, j + 1);
         }
-        s[t] = mma(lo, q[0][j], s[t]);
-        s[t] = mma(hi, q[0][j + 1], s[t]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+          if (PARTS == 2) s[t] = mma(k[t], q[PARTS - 1][j], s[t]);
+          s[t] = mma(k[t], q[0][j], s[t]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < KT; ++t) k[t] = next[t];
       }
+    } else {
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+          const f16x8 k = p.key(t, j);
+          if (PARTS == 2) s[t] = mma(k, q[PARTS - 1][j], s[t]);
+          s[t] = mma(k, q[0][j], s[t]);
+        }
     }
     // A score is s * f + v in powers of two, v the values' scale; f > 0 and v are a sixteenth's, so its largest score is that of its largest s.
     constexpr int PER = 16 / R;  // score tiles of a sixteenth (16-column tiles: four; 32: one)
@@ -353,20 +373,26 @@ struct Columns {
       }
       sum = fmaf(add, two_to(127 - (int)((p.vs >> (8 * sixteenth(h))) & 0xff)), sum);
     }
+    f16x8 x[2], next[2];  // (as above, sixteen values ahead)
+    auto values = [&](int n, f16x8 (&to)[2]) { p.template values<MASKED>(n / HALVES, n % HALVES, t0 + sixteenth(n % HALVES) * 16, see_lo, see_hi, &found, to); };
+    constexpr bool AHEAD = P::kShared && !MASKED;
+    if (P::kShared) __builtin_amdgcn_sched_barrier(0);
+    if (AHEAD) values(0, x);
 #pragma unroll
-    for (int t = 0; t < VT; ++t) {
+    for (int n = 0; n < VT * HALVES; ++n) {
+      const int t = n / HALVES, h = n % HALVES;
+      if (!AHEAD) values(n, x);
+      else if (n + 1 < VT * HALVES) values(n + 1, next);
       if (P::kShared) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int h = 0; h < HALVES; ++h) {
-        f16x8 x[2];
-        p.template values<MASKED>(t, h, t0 + sixteenth(h) * 16, see_lo, see_hi, &found, x);
-        const f16x8 lo = x[0], hi = x[1];
-        if (PARTS == 2) {
-          o[t] = mma(lo, w[PARTS - 1][h * 2], o[t]);
-          o[t] = mma(hi, w[PARTS - 1][h * 2 + 1], o[t]);
-        }
-        o[t] = mma(lo, w[0][h * 2], o[t]);
-        o[t] = mma(hi, w[0][h * 2 + 1], o[t]);
+      for (int i = 0; i < 2; ++i) {
+        if (PARTS == 2) o[t] = mma(x[i], w[PARTS - 1][h * 2 + i], o[t]);
+        o[t] = mma(x[i], w[0][h * 2 + i], o[t]);
+      }
+      if (P::kShared) __builtin_amdgcn_sched_barrier(0);
+      if (AHEAD) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[i] = next[i];
       }
     }
     if (MASKED && __any(found != 0)) nans = true;
