@@ -694,7 +694,15 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
   int* flag = (int*)(lds + wide_numbers(D));
   const int head = blockIdx.x % a.c.kv_heads, wave = uniform(threadIdx.x >> 6);
   Unit u;
-  if (!find_unit<COLS, MOST>(a, blockIdx.x / a.c.kv_heads, &u)) return;
+  int unit = blockIdx.x / a.c.kv_heads;
+  if (a.snake) {
+    // One sequence, a unit a tile: later tiles see more pages.  The longest come first; where two rounds of workgroups are all there are, the second comes
+    // the other way round, so that a CU gets a long one and a short one.
+    const int tiles = (int)(((int64_t)rows_of(a.c, 0) * a.group + COLS - 1) / COLS), half = (tiles + 1) / 2;
+    if (unit < tiles && (a.snake == 1 || unit < half)) unit = tiles - 1 - unit;
+    else if (unit < tiles) unit = unit - half;
+  }
+  if (!find_unit<COLS, MOST>(a, unit, &u)) return;
   const int all = u.rows * a.group, col0 = u.tile * COLS, mine0 = col0 + wave * 32;
   const int tile_cols = all - col0 < COLS ? all - col0 : COLS, cols = all - mine0 < 32 ? all - mine0 : 32;  // (cols may be none)
   // pages of the workgroup, and of the wave

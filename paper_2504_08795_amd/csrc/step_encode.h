@@ -230,6 +230,7 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   const int64_t units = tiles + a.target + 1;
   if (units * o.cache.kv_heads > 0x7fffffll) return kTooMany;
   a.units = (int)units;
+  if (wide && a.target == 0 && o.cache.n_seqs == 1) a.snake = (columns + cols - 1) / cols * o.cache.kv_heads <= 2 * (int64_t)n_cu ? 2 : 1;
   l->counters = a.target ? (size_t)units * o.cache.kv_heads : 0;
   l->part_bytes = a.target ? (size_t)(units * o.cache.kv_heads * unit_floats(cols, o.cache.dim)) * sizeof(float) : 0;
   set_args(l, a);
