@@ -487,30 +487,6 @@ __device__ __forceinline__ float* part_numbers(const AttendArgs& a, int head, in
   return a.part + (int64_t)(head * a.units + unit) * (COLS * (D + 2));
 }
 
-// Whether this workgroup is the last of the tile's units.  What they leave is written through to where all XCDs see it (put) and read
-// from there (take_back), so neither side needs a fence: a release or an acquire of the device writes back or drops a whole L2, and
-// with one for every workgroup 64 streams took 300 us instead of 88.
-__device__ __forceinline__ bool arrive(const AttendArgs& a, int head, const Unit& u, int* lds, int tid) {
-  puts_done();
-  __syncthreads();
-  if (tid == 0) {
-    uint32_t* n = a.count + (int64_t)head * a.units + u.first;
-    const uint32_t before = __hip_atomic_fetch_add(n, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const bool last = before == (uint32_t)u.chunks - 1;
-    if (last) __hip_atomic_store(n, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    *lds = last;
-  }
-  __syncthreads();
-  return *lds != 0;
-}
-__device__ __forceinline__ float4 take_back(const float* p) {
-  return __builtin_bit_cast(float4, __builtin_amdgcn_global_load_b128((u32x4 __attribute__((address_space(1)))*)p, "agent"));
-}
-__device__ __forceinline__ float2 take_back2(const float* p) {
-  return __builtin_bit_cast(float2, __hip_atomic_load((const uint64_t __attribute__((address_space(1)))*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-}
-__device__ __forceinline__ void leave2(float* p, float x, float y) { put((void*)p, make_uint2(__float_as_uint(x), __float_as_uint(y))); }
-
 template <int COLS, int D, bool BF16>
 __device__ __forceinline__ void merge(const AttendArgs& a, int head, const Unit& u, int col0, float* lds, int tid) {
   // lds [chunks][COLS]: M, then what each unit's numbers are multiplied with; behind it [chunks][COLS]: sums
@@ -641,7 +617,7 @@ __device__ __forceinline__ void attend_narrow_body(const AttendArgs& a) {
       if (d == 0) leave2(part + COLS * D + 2 * c, top, sum);
     }
   }
-  if (u.chunks > 1 && arrive(a, head, u, flag, tid)) merge<COLS, D, BF16>(a, head, u, col0, lds, tid);
+  if (u.chunks > 1 && arrive(a.count + (int64_t)head * a.units + u.first, u.chunks, flag, tid)) merge<COLS, D, BF16>(a, head, u, col0, lds, tid);
 }
 
 // A page in LDS as f16, shared by the waves of a workgroup.  Sixteen neighbouring lanes read sixteen keys (channels) at one place, so the
@@ -805,7 +781,7 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
     }
   }
   const int tid = wave * 64 + w.lane;
-  if (u.chunks > 1 && arrive(a, head, u, flag, tid)) merge<COLS, D, BF16>(a, head, u, col0, lds, tid);
+  if (u.chunks > 1 && arrive(a.count + (int64_t)head * a.units + u.first, u.chunks, flag, tid)) merge<COLS, D, BF16>(a, head, u, col0, lds, tid);
 }
 
 }  // namespace daris

@@ -114,14 +114,20 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
   const int split_log = (MT == 1 ? 4 : 3) - a.across;  // tiles side by side: 1 << across; waves on one of them: 1 << split_log
   const int own_tile = wave >> split_log, part = wave & ((1 << split_log) - 1);
-  int m0 = 0, tg = blockIdx.x;
+  int m0 = 0, tg = blockIdx.x, share = 0;  // share: of K, where several workgroups have one
+  if (a.shares > 1) {
+    tg = blockIdx.x / a.shares;
+    share = blockIdx.x - tg * a.shares;
+  }
+  const int unit = tg;
   if (a.rows > ROWS) {
     const int mb = tg / a.wgs;
     m0 = mb * ROWS;
     tg -= mb * a.wgs;
   }
   const int rows = a.rows - m0 < ROWS ? a.rows - m0 : ROWS;
-  const int cs = a.steps, steps = (a.k + 127) >> 7, chunks = a.chunks;
+  const int cs = a.steps, all_steps = (a.k + 127) >> 7, step0 = share * a.share_steps, chunks = a.chunks;
+  const int steps = all_steps - step0 < a.share_steps ? all_steps - step0 : a.share_steps;
   // LDS, in bytes: x [PARTS][step][row][instruction, lane group], the last exchanged by the row's number so that rows lie on different banks, and (of scaled
   // rows) their scales [step][group][ROWS], twice if there is more than one chunk; the weights' scales [tiles * 16][pitch] twice if there is more to
   // come; sums [WAVES][ROWS][16]
@@ -140,8 +146,8 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
     List l;
     l.n = tg < a.groups ? (cs < steps - ch * cs ? cs : steps - ch * cs) - first : 0;
     l.n = l.n < own ? l.n : own;
-    l.to_last = steps - 1 - st;
-    l.w = a.w + (int64_t)(n < a.n ? n : a.n - 1) * a.w_row + st * 64 + g * 16;
+    l.to_last = all_steps - 1 - step0 - st;
+    l.w = a.w + (int64_t)(n < a.n ? n : a.n - 1) * a.w_row + (step0 + st) * 64 + g * 16;
     return l;
   };
   // Channels past K: their x is 0, so any weights will do -- those of lane group 0.
@@ -161,7 +167,7 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
 #pragma unroll
     for (int i = 0; i < kScalePieces; ++i) {
       if ((i * T) >> a.eights >= 16 << a.across) break;
-      const int p = i * T + tid, r = p >> a.eights, from = ch * cs * GS + (p & ((1 << a.eights) - 1)) * 8;
+      const int p = i * T + tid, r = p >> a.eights, from = (step0 + ch * cs) * GS + (p & ((1 << a.eights) - 1)) * 8;
       if (r >= 16 << a.across || from >= groups) continue;
       const int n = (tg << a.across) * 16 + r;
       const uint16_t* s = a.w_scale + (int64_t)(n < a.n ? n : a.n - 1) * groups + from;
@@ -199,7 +205,7 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       if ((i * T) >> row_log >= rows) break;
-      const int p = i * T + tid, m = p >> row_log, q = p & ((1 << row_log) - 1), k = ch * cs * 128 + q * 8;
+      const int p = i * T + tid, m = p >> row_log, q = p & ((1 << row_log) - 1), k = (step0 + ch * cs) * 128 + q * 8;
 #pragma unroll
       for (int e = 0; e < (XT == kRowsF32 ? 2 : 1); ++e) raw[i].v[e] = make_uint4(0u, 0u, 0u, 0u);
       raw[i].scale = 127;
@@ -284,19 +290,29 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
   for (int m = 0; m < MT; ++m) total[m] = f32x4{0.f, 0.f, 0.f, 0.f};
   const Spread<XT> spread;
 
-  // the outputs of a group of tiles from the waves' sums
-  auto write = [&](int tg) {
-    const int wide = a.across + 4;  // log2 of the outputs side by side
-    for (int i = afresh(threadIdx.x); i < rows << wide; i += T) {
-      const int m = i >> wide, o = i & ((1 << wide) - 1);
-      const float __attribute__((address_space(3)))* r = red + (((o >> 4) << split_log) * ROWS + m) * 16 + (o & 15);
-      float s = 0.f;
+  // The outputs of a group of tiles, from the waves' sums or, where K is shared, from what the workgroups left.
+  const int wide = a.across + 4;  // log2 of the outputs side by side
+  auto of_waves = [&](int i) {
+    const int m = i >> wide, o = i & ((1 << wide) - 1);
+    const float __attribute__((address_space(3)))* r = red + (((o >> 4) << split_log) * ROWS + m) * 16 + (o & 15);
+    float s = 0.f;
 #pragma unroll 4
-      for (int p = 0; p < 1 << split_log; ++p) s += r[p * ROWS * 16];
-      int out = (tg << wide) + o;
+    for (int p = 0; p < 1 << split_log; ++p) s += r[p * ROWS * 16];
+    return s;
+  };
+  auto write = [&](int tg, const float* left) {
+    for (int i = afresh(threadIdx.x); i < rows << wide; i += T) {
+      const int m = i >> wide;
+      int out = (tg << wide) + (i & ((1 << wide) - 1));
+      float s = 0.f;
+      if (left) {
+#pragma unroll 8
+        for (int p = 0; p < a.shares; ++p) s += take_back1(left + (int64_t)p * (ROWS << wide) + i);  // (in order, whoever came last)
+      } else {
+        s = of_waves(i);
+      }
       bool on = out < a.n;
-      if (a.gate) {
-        // neighbouring lanes hold a pair: a row of the group is an even number of outputs, so pairs never part
+      if (a.gate) {  // neighbouring lanes hold a pair (a row of the group is an even number of outputs, so pairs never part)
         float other, own;
         lane_pair<1>(s, &own, &other);
         s = s / (1.f + expf(-s)) * other;
@@ -320,7 +336,7 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
   stage_scales(0);
   for (;;) {
     __syncthreads();
-    if (ch == 0 && last >= 0) write(last);
+    if (ch == 0 && last >= 0) write(last, nullptr);
     const bool over = ch + 1 == chunks;
     const int next_ch = over ? 0 : ch + 1, next = over ? tg + a.wgs : tg;
     const bool more = next < a.groups;
@@ -412,7 +428,14 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
     now = after;
   }
   __syncthreads();
-  write(last);
+  const float* left = nullptr;
+  if (a.shares > 1) {
+    float* all = a.part + (int64_t)unit * a.shares * (ROWS << wide);
+    for (int i = threadIdx.x; i < rows << wide; i += T) put(all + share * (ROWS << wide) + i, of_waves(i));
+    if (!arrive(a.count + unit, a.shares, (int*)smem, threadIdx.x)) return;
+    left = all;
+  }
+  write(last, left);
 }
 
 }  // namespace daris

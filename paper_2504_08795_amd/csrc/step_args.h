@@ -92,7 +92,10 @@ struct MatvecArgs {
   int chunks;
   int across;  // log2 of a workgroup's tiles (16 outputs) side by side; its other waves share them
   int groups;  // of so many tiles
-  int wgs;     // workgroups of a block of rows
+  int wgs;     // units of a block of rows: workgroups, or sets of them that share K
+  int shares, share_steps;  // workgroups that share K, where there are few tiles; steps of each
+  float* part;              // what they add to the outputs: [unit][share][rows of a block][outputs of a group]
+  uint32_t* count;          // arrivals of a unit's shares, zero between launches
   int eights;  // log2 of the pieces of scales that a tile's row has in a chunk, rounded up
   int pitch;   // matvec_pitch of a chunk
 };

@@ -2,6 +2,7 @@
 // logic, no GPU needed; in a header because only daris_api.cpp uses it).
 #pragma once
 #include <cstdarg>
+#include <cstddef>
 #include <cstdint>
 #include <cstdio>
 #include <cstring>
@@ -19,6 +20,7 @@ struct StepLaunch {
   uint32_t groups = 0, threads = 0, nbytes = 0;
   // what it needs of the partition's workspace, filled in by place_step: bytes of partial results, counters that are zero
   size_t part_bytes = 0, counters = 0;
+  uint32_t part_at = 0, count_at = 0;  // where its arguments name them
   alignas(8) unsigned char args[336];
 };
 
@@ -231,6 +233,8 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   if (units * o.cache.kv_heads > 0x7fffffll) return kTooMany;
   a.units = (int)units;
   if (wide && a.target == 0 && o.cache.n_seqs == 1) a.snake = (columns + cols - 1) / cols * o.cache.kv_heads <= 2 * (int64_t)n_cu ? 2 : 1;
+  l->part_at = offsetof(AttendArgs, part);
+  l->count_at = offsetof(AttendArgs, count);
   l->counters = a.target ? (size_t)units * o.cache.kv_heads : 0;
   l->part_bytes = a.target ? (size_t)(units * o.cache.kv_heads * unit_floats(cols, o.cache.dim)) * sizeof(float) : 0;
   set_args(l, a);
@@ -250,7 +254,7 @@ inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int 
   const int64_t tiles = ((int64_t)o.n + 15) / 16, room = n_cu / blocks > 1 ? n_cu / blocks : 1;
   // x in LDS, of all of K if it fits (with the weights' scales and the waves' sums), else of the largest chunk that fits twice
   const int per_group = 128 / o.group, step_bytes = 128 * 2 * parts * rows + (type == 1 ? 0 : per_group * block * 4);
-  auto lds = [&](int cs, int across) {
+  auto lds = [&](int cs, int across, int steps) {
     const bool again = cs < steps || (tiles + across - 1) / across > room;
     return (cs < steps ? 2 : 1) * cs * step_bytes + (again ? 2 : 1) * across * 16 * matvec_pitch(cs * per_group) * 2 + waves * block * 16 * 4;
   };
@@ -259,36 +263,53 @@ inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int 
     while ((1 << log) < v) ++log;
     return log;
   };
-  auto fits = [&](int cs, int across) {
-    return ((16ll << log2_up(cs)) * rows <= matvec_pieces(parts) * waves * 64) && (across * 16 << log2_up((cs * per_group + 7) / 8)) <= kScalePieces * waves * 64 && lds(cs, across) <= 160 * 1024;
+  auto fits = [&](int cs, int across, int steps) {
+    return ((16ll << log2_up(cs)) * rows <= matvec_pieces(parts) * waves * 64) && (across * 16 << log2_up((cs * per_group + 7) / 8)) <= kScalePieces * waves * 64 && lds(cs, across, steps) <= 160 * 1024;
   };
-  // Tiles side by side in a workgroup: what makes the shortest sequence of steps for a wave, on the most workgroups.  A wave's share of a chunk
-  // counts in fours (its steps travel four at a time), and a barrier as two steps.
+  // Tiles side by side in a workgroup, and workgroups that share K: what makes the shortest sequence of steps for a wave.  A wave's part of a chunk
+  // counts in fours (its steps travel four at a time), and a barrier as two steps.  K is shared only where that leaves CUs none without a workgroup
+  // more than before and two steps for a wave; to meet takes four steps and the last workgroup two for every eight numbers that a thread fetches.
   int64_t best = -1;
   for (int across = 1; across <= waves; across *= 2) {
-    int cs = steps;
-    if (!fits(cs, across)) {
-      cs = 1 << log2_up(cs);
-      while (cs > 1 && !fits(cs, across)) cs /= 2;
+    const int64_t groups = (tiles + across - 1) / across, rounds = (groups + room - 1) / room;
+    int64_t most = rounds == 1 ? n_cu / (groups * blocks) : 1;
+    most = most < (int64_t)steps * across / (2 * waves) ? most : (int64_t)steps * across / (2 * waves);
+    for (int64_t shares = 1; shares <= (most < 64 ? most : 64) || shares == 1; shares *= 2) {
+      const int each = (int)((steps + shares - 1) / shares);
+      if ((each + 0ll) * (shares - 1) >= steps) continue;  // (the last share would have nothing)
+      int cs = each;
+      if (!fits(cs, across, each)) {
+        cs = 1 << log2_up(cs);
+        while (cs > 1 && !fits(cs, across, each)) cs /= 2;
+      }
+      if (!fits(cs, across, each)) continue;
+      const int64_t chunks = (each + cs - 1) / cs, own = ((int64_t)cs * across + waves - 1) / waves;
+      const int64_t numbers = ((int64_t)rows * across * 16 + waves * 64 - 1) / (waves * 64);
+      const int64_t cost = rounds * chunks * ((own + 3) / 4 * 4 + 2) + (shares > 1 ? 4 + 2 * numbers * ((shares + 7) / 8) : 0);
+      if (best >= 0 && cost >= best) continue;
+      best = cost;
+      a.across = log2_up(across);
+      a.steps = cs;
+      a.chunks = (int)chunks;
+      a.groups = (int)groups;
+      a.wgs = (int)(groups < room ? groups : room);
+      a.shares = (int)shares;
+      a.share_steps = each;
     }
-    if (!fits(cs, across)) continue;
-    const int64_t groups = (tiles + across - 1) / across, rounds = (groups + room - 1) / room, chunks = (steps + cs - 1) / cs;
-    const int64_t own = ((int64_t)cs * across + waves - 1) / waves, cost = rounds * chunks * ((own + 3) / 4 * 4 + 2);
-    if (best >= 0 && cost >= best) continue;
-    best = cost;
-    a.across = log2_up(across);
-    a.steps = cs;
-    a.chunks = (int)chunks;
-    a.groups = (int)groups;
-    a.wgs = (int)(groups < room ? groups : room);
   }
   if (best < 0) return "no chunk of K fits LDS";
   a.chunk = log2_up(a.steps);
   a.eights = log2_up((a.steps * per_group + 7) / 8);
   a.pitch = matvec_pitch(a.steps * per_group);
+  if (a.shares > 1) {
+    l->part_at = offsetof(MatvecArgs, part);
+    l->count_at = offsetof(MatvecArgs, count);
+    l->counters = (size_t)a.wgs * blocks;
+    l->part_bytes = l->counters * a.shares * block * (16 << a.across) * sizeof(float);
+  }
   set_args(l, a);
   const int g = o.group == 32 ? 0 : o.group == 64 ? 1 : 2;
-  return set_grid(l, t.matvec[type][g][many], (int64_t)a.wgs * blocks, waves * 64, lds(a.steps, 1 << a.across)) ? "" : kTooMany;
+  return set_grid(l, t.matvec[type][g][many], (int64_t)a.wgs * blocks * a.shares, waves * 64, lds(a.steps, 1 << a.across, a.share_steps)) ? "" : kTooMany;
 }
 
 // What is wrong with an operator, or "".
@@ -318,11 +339,8 @@ inline std::string encode_step(const StepTable& t, const daris_op& op, int n_cu,
 // The launch's places in the workspace.
 inline void place_step(StepLaunch* l, void* part, uint32_t* counters) {
   if (!l->counters) return;
-  AttendArgs a;
-  std::memcpy(&a, l->args, sizeof a);
-  a.part = static_cast<float*>(part);
-  a.count = counters;
-  std::memcpy(l->args, &a, sizeof a);
+  std::memcpy(l->args + l->part_at, &part, sizeof part);
+  std::memcpy(l->args + l->count_at, &counters, sizeof counters);
 }
 
 }  // namespace daris

@@ -93,7 +93,7 @@ int main() {
     } else if (op.kind == DARIS_STEP_MATVEC) {
       MatvecArgs a;
       std::memcpy(&a, l.args, sizeof a);
-      printf(" %d %d %d %d %d", a.steps, a.chunk, 1 << a.across, a.groups, a.wgs);
+      printf(" %d %d %d %d %d %d %d", a.steps, a.chunk, 1 << a.across, a.groups, a.wgs, a.shares, a.share_steps);
     } else if (op.kind == DARIS_STEP_ATTEND) {
       AttendArgs a;
       std::memcpy(&a, l.args, sizeof a);

@@ -457,6 +457,27 @@ def test_plans_are_kept_freed_and_gone_after_a_shutdown(part):
     assert torch.equal(y, first)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,n,k,group", [(1, 40, 25088, 128), (16, 70, 4224, 64), (33, 34, 3200, 64), (70, 200, 4096, 128), (130, 48, 2112, 32)])
+def test_matvec_of_few_outputs_and_a_long_k(part, dtype, rows, n, k, group):
+    matvec_case(part, rows, n, k, group, dtype)
+    matvec_case(part, rows, n, k, group, dtype, gate=True, skew=1)
+    matvec_case(part, rows, n, k, group, dtype, codes=True)
+    x = rand((rows, k), DT[dtype], 11).cuda()
+    w = torch.randint(0, 256, (n, k // 2), generator=torch.Generator().manual_seed(12), dtype=torch.uint8).cuda()
+    ws = torch.full((n, k // group), 0.25, dtype=torch.bfloat16, device="cuda")
+    y = [torch.empty((rows, n), dtype=DT[dtype], device="cuda") for _ in range(4)]
+    run(part, *[D.make_matvec(x, w, ws, t) for t in y])
+    assert all(torch.equal(t, y[0]) for t in y), "another run, other bits"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,window", [(26, 0), (32, 0), (39, 0), (39, 200)])
+def test_attend_a_chunk_of_one_sequence_on_few_cus(part, dtype, rows, window):
+    # tiles of 128 columns for each of 12 heads on 24 CUs: as many units as go at once, and more
+    attend_case(part + 1, 800 + rows, [150], [rows], 12, 16, 64, dtype, window)
+
+
 def test_operators_without_rows_do_nothing(part):
     e = torch.empty((0, 64), device="cuda")
     w = torch.ones(64, device="cuda")

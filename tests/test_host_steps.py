@@ -39,16 +39,21 @@ def test_matvec_launches_fit_their_kernel(encode):
     for a, p in zip(asked, encode([("matvec",) + x for x in asked])):
         rows, n, k, g, dtype, codes, _, n_cu = a
         assert not isinstance(p, str), (a, p)
-        kernel, groups, threads, lds, _, _, cs, log, across, tgs, wgs = p
+        kernel, groups, threads, lds, part, counters, cs, log, across, tgs, wgs, shares, each = p
         mt, parts = (1 if kernel == 3 else 4), (2 if not codes and dtype == 0 else 1)
         waves, blocks, steps, block_rows = threads // 64, -(-rows // (16 * mt)), -(-k // 128), min(rows, 16 * mt)
         assert (mt == 4) == (rows > 16) and waves == (16 if mt == 1 else 8)
-        assert groups == wgs * blocks and wgs <= max(tgs, 1) and tgs * across * 16 >= n > (tgs - 1) * across * 16, (a, p)
-        assert across in (1, 2, 4, 8, 16) and across <= waves and 1 <= cs <= steps and cs <= 1 << log < 2 * cs, (a, p)
+        assert groups == wgs * blocks * shares and wgs <= max(tgs, 1) and tgs * across * 16 >= n > (tgs - 1) * across * 16, (a, p)
+        assert across in (1, 2, 4, 8, 16) and across <= waves and 1 <= cs <= each and cs <= 1 << log < 2 * cs, (a, p)
+        assert 1 <= shares and (shares - 1) * each < steps <= shares * each, ("shares of K", a, p)
+        if shares > 1:  # one round, no more workgroups than CUs, and a place for each of their numbers
+            assert wgs == tgs and groups <= n_cu and counters == wgs * blocks and part == counters * shares * 16 * mt * 16 * across * 4, (a, p)
+        else:
+            assert part == counters == 0
         assert (16 << log) * block_rows <= (4 if parts == 2 else 8) * threads, ("pieces of x", a, p)
         scales = cs * (128 // g)
         assert -(-scales // 8) * across * 16 <= 2 * threads, ("pieces of scales", a, p)
-        chunks = -(-steps // cs)
+        chunks = -(-each // cs)
         x = parts * cs * 16 * block_rows * 16 + (0 if not codes and dtype == 1 else cs * (128 // g) * 16 * mt * 4)
         need = (2 if chunks > 1 else 1) * x + (2 if chunks > 1 or wgs < tgs else 1) * across * 16 * ((scales + 7) // 8 * 8 + 2) * 2 + waves * 16 * mt * 16 * 4
         assert need <= lds <= 160 * 1024, ("LDS", need, a, p)
