@@ -6,8 +6,11 @@
 //   bf16 x: as it is.  0x4300 | c is the bf16 number 128 + c; a second product with the constant -136 takes the rest away.  Both sums are 17 times
 //     as large as the result, which costs four of fp32's 24 bits.
 //   fp32 x: two f16 parts (22 bits), a group of a row divided by a power of two that makes its largest number 2^14 and more, so that
-//     nothing overflows; 0x6400 | c is the f16 number 1024 + c, one packed addition makes it c - 8.
-//   e4m3 x: f16 holds every one of them.
+//     nothing overflows; 0x3c00 | c << 6 is the f16 number (16 + c) / 16.  The sum begins with -24 / 16 of that of x, which is taken in fp32 when x is
+//     staged; it gets up to four times as large as the result, which costs two of fp32's 24 bits.  (c - 8 took three packed additions more for eight
+//     nibbles, and one row's 4096 products with 25088 channels 26.7 us a call.  Nibbles as subnormal f16 numbers take three instructions less, but
+//     the matrix instructions keep 20 bits of such a sum.)
+//   e4m3 x: f16 holds every one of them, 16 times; the same.
 // The waves of a workgroup share x, and neighbouring ones a tile: each takes neighbouring steps of it, and their sums are added in
 // wave order.  A workgroup goes from group of tiles to group of tiles; x is staged once if all of K fits LDS, else in chunks,
 // the next one while the present one is computed, as are the weights' scales.  Every wave has four steps of weights on their way, across
@@ -22,22 +25,17 @@ enum { kRowsF32 = 0, kRowsBf16 = 1, kRowsF8 = 2 };
 // What spreads nibbles: the constants stay in registers (an instruction that takes both as literals does not exist, and two take twice as long).
 template <int XT>
 struct Spread {
-  uint32_t mask = 0x000f000fu, high = XT == kRowsBf16 ? 0x43004300u : 0x64006400u;
+  uint32_t mask = XT == kRowsBf16 ? 0x000f000fu : 0x03c003c0u, high = XT == kRowsBf16 ? 0x43004300u : 0x3c003c00u;
   u32x4 minus = {0xc308c308u, 0xc308c308u, 0xc308c308u, 0xc308c308u};  // -136 as bf16
   __device__ __forceinline__ Spread() {
     asm volatile("" : "+s"(mask));
     asm volatile("" : "+v"(high));
     if (XT == kRowsBf16) asm volatile("" : "+v"(minus));
   }
-  // Eight nibbles in the order 0 4 1 5 2 6 3 7: plus 128 as bf16, or minus 8 as f16.
+  // Eight nibbles in the order 0 4 1 5 2 6 3 7: 128 + c as bf16, or 1 + c / 16 as f16.
   __device__ __forceinline__ uint4 operator()(uint32_t w) const {
-    uint4 v = make_uint4((w & mask) | high, ((w >> 4) & mask) | high, ((w >> 8) & mask) | high, ((w >> 12) & mask) | high);
-    if (XT != kRowsBf16) {
-      const f16x2 less = {(_Float16)-1032.0f, (_Float16)-1032.0f};
-      v = make_uint4(__builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v.x) + less), __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v.y) + less),
-                     __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v.z) + less), __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, v.w) + less));
-    }
-    return v;
+    if (XT == kRowsBf16) return make_uint4((w & mask) | high, ((w >> 4) & mask) | high, ((w >> 8) & mask) | high, ((w >> 12) & mask) | high);
+    return make_uint4(((w << 6) & mask) | high, ((w << 2) & mask) | high, ((w >> 2) & mask) | high, ((w >> 6) & mask) | high);
   }
 };
 
@@ -129,9 +127,10 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
   const int cs = a.steps, all_steps = (a.k + 127) >> 7, step0 = share * a.share_steps, chunks = a.chunks;
   const int steps = all_steps - step0 < a.share_steps ? all_steps - step0 : a.share_steps;
   // LDS, in bytes: x [PARTS][step][row][instruction, lane group], the last exchanged by the row's number so that rows lie on different banks, and (of scaled
-  // rows) their scales [step][group][ROWS], twice if there is more than one chunk; the weights' scales [tiles * 16][pitch] twice if there is more to
+  // rows) their scales and what their sums begin with [step][four rows][group][2][4], twice if there is more than one chunk; the weights' scales [tiles * 16][pitch] twice if there is more to
   // come; sums [WAVES][ROWS][16]
-  const int part_size = cs * rows * 256, x_size = PARTS * part_size + (XT == kRowsBf16 ? 0 : cs * GS * ROWS * 4), pitch = a.pitch * 2;
+  const int fours = MT == 1 ? (rows + 3) >> 2 : 4 * MT;
+  const int part_size = cs * rows * 256, x_size = PARTS * part_size + (XT == kRowsBf16 ? 0 : cs * fours * GS * 32), pitch = a.pitch * 2;
   const int ws_at = (chunks > 1 ? 2 : 1) * x_size, ws_size = (16 << a.across) * pitch;
   float __attribute__((address_space(3)))* const red = (float __attribute__((address_space(3)))*)(lds + ws_at + (chunks > 1 || a.wgs < a.groups ? 2 : 1) * ws_size);
 
@@ -245,11 +244,14 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
       const int p = i * T + tid, m = p >> row_log, q = p & ((1 << row_log) - 1), in_step = (q & 15) * 8;
       if (XT == kRowsF32) __builtin_amdgcn_sched_barrier(0);  // (piece by piece, or their parts do not fit the registers)
       uint4 high, low = make_uint4(0u, 0u, 0u, 0u);
-      float back = 1.f;
+      float back = 1.f, begin = 0.f;
       if (XT == kRowsBf16) {
         high = in_order(raw[i].v[0]);
       } else if (XT == kRowsF8) {
-        high = in_order(__builtin_bit_cast(uint4, f16_of_codes(raw[i].v[0].x, raw[i].v[0].y)));
+        const f16x8 h = __builtin_bit_cast(f16x8, in_order(__builtin_bit_cast(uint4, f16_of_codes(raw[i].v[0].x, raw[i].v[0].y, 16.f))));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) begin += (float)h[e];
+        high = __builtin_bit_cast(uint4, h);
         back = two_to(raw[i].scale - 127);
       } else {
         float v[8], rest[8];
@@ -258,29 +260,37 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
         for (int e = 0; e < 8; ++e) {
           const uint4& r = raw[i].v[XT == kRowsF32 ? e >> 2 : 0];
           v[e] = __uint_as_float((e & 3) == 0 ? r.x : (e & 3) == 1 ? r.y : (e & 3) == 2 ? r.z : r.w);
-          most = fmaxf(most, size_of(v[e]));
+          most = fmaxf(most, fabsf(v[e]));
         }
         most = wave_max<G / 8>(most);
         // to 2^14 and more, but no further than 2^110 times: what is smaller than 2^-96 loses bits
         int up = 141 - (int)(__float_as_uint(most) >> 23);
         up = up > 110 ? 110 : up;
-        back = two_to(-up);
+        back = two_to(4 - up);  // (for (c - 8) / 16)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = __builtin_amdgcn_ldexpf(v[e], up);
+        for (int e = 0; e < 8; ++e) {
+          v[e] = __builtin_amdgcn_ldexpf(v[e], up);
+          begin += v[e];
+        }
         const f16x8 h = f16_in_order(v);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          rest[e] = is_finite(v[e]) ? v[e] - (float)h[2 * e] : 0.f;
-          rest[e + 4] = is_finite(v[e + 4]) ? v[e + 4] - (float)h[2 * e + 1] : 0.f;
+          rest[e] = v[e] - (float)h[2 * e];
+          rest[e + 4] = v[e + 4] - (float)h[2 * e + 1];
         }
         high = __builtin_bit_cast(uint4, h);
         low = __builtin_bit_cast(uint4, f16_in_order(rest));
       }
+      if (XT != kRowsBf16) begin = wave_sum<G / 8>(begin) * -1.5f;
       if (m < rows && q < in_chunk) {
         const Lds to = frag + (((q >> 4) * rows + m) * 16 + (place<G>(in_step) ^ (m & 15))) * 16;
         *(u32x4 __attribute__((address_space(3)))*)to = __builtin_bit_cast(u32x4, high);
         if (PARTS == 2) *(u32x4 __attribute__((address_space(3)))*)(to + part_size) = __builtin_bit_cast(u32x4, low);
-        if (XT != kRowsBf16 && (in_step & (G - 1)) == 0) ((float __attribute__((address_space(3)))*)(frag + PARTS * part_size))[((q >> 4) * GS + in_step / G) * ROWS + m] = back;
+        if (XT != kRowsBf16 && (in_step & (G - 1)) == 0) {
+          float __attribute__((address_space(3)))* const s = (float __attribute__((address_space(3)))*)(frag + PARTS * part_size) + (((q >> 4) * fours + (m >> 2)) * GS + in_step / G) * 8 + (m & 3);
+          s[0] = back;
+          s[4] = begin;
+        }
       }
     }
   };
@@ -354,10 +364,10 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
       const int xr = m * 16 + c < rows ? m * 16 + c : rows - 1;
       f[m] = x_at + ((first * rows + xr) * 16 + (g ^ (xr & 15))) * 16;
     }
-    Lds xs = lds + x_at + PARTS * part_size + (first * GS * ROWS + g * 4) * 4;
+    Lds xs = lds + x_at + PARTS * part_size + (first * fours + (MT == 1 && g >= fours ? fours - 1 : g)) * GS * 32;  // (rows that are none: any numbers will do)
     Lds ws = lds + ws_at + buf * ws_size + (own_tile * 16 + c) * pitch + first * GS * 2;
 #pragma unroll 1
-    for (int i0 = 0; i0 < turns; i0 += RING, xs += RING * GS * ROWS * 4, ws += RING * GS * 2) {
+    for (int i0 = 0; i0 < turns; i0 += RING, ws += RING * GS * 2) {
       const bool same = i0 + RING < turns;
       const List ahead = same ? now : after;
       const int from = same ? i0 + RING : 0;
@@ -382,7 +392,10 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
           }
 #pragma unroll
           for (int u = 0; u < GS; ++u) {
-            f32x4 sum = {0.f, 0.f, 0.f, 0.f}, less = {0.f, 0.f, 0.f, 0.f};  // two chains: an instruction waits for the one it adds to
+            const Lds of_x = xs + (m * 4 * GS + u) * 32;
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+            if (XT != kRowsBf16) sum = *(const f32x4 __attribute__((address_space(3)))*)(of_x + 16);
+            f32x4 less = {0.f, 0.f, 0.f, 0.f};  // two chains: an instruction waits for the one it adds to
 #pragma unroll
             for (int j = u * (4 / GS); j < (u + 1) * (4 / GS); ++j) {
               if (PARTS == 2) operand(j);
@@ -400,12 +413,13 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
             }
             const float by = bf16_bits_to_f32(*(const uint16_t __attribute__((address_space(3)))*)(ws + (e * GS + u) * 2));
             f32x4 x4 = {1.f, 1.f, 1.f, 1.f};
-            if (XT != kRowsBf16) x4 = *(const f32x4 __attribute__((address_space(3)))*)(xs + ((e * GS + u) * ROWS + m * 16) * 4);
+            if (XT != kRowsBf16) x4 = *(const f32x4 __attribute__((address_space(3)))*)of_x;
 #pragma unroll
             for (int q = 0; q < 4; ++q) total[m][q] = fmaf(sum[q], by * x4[q], total[m][q]);
           }
           f[m] += rows * 256;
         }
+        xs += fours * GS * 32;
       }
     }
     if (over) {

@@ -20,9 +20,9 @@ __device__ __forceinline__ f16x8 halves(f16x2 a, f16x2 b, f16x2 c, f16x2 d) {
 }
 
 // Eight e4m3 codes as f16, which holds every one of them.
-__device__ __forceinline__ f16x8 f16_of_codes(uint32_t lo, uint32_t hi) {
-  return halves(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true),
-                __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
+__device__ __forceinline__ f16x8 f16_of_codes(uint32_t lo, uint32_t hi, float times = 1.0f) {
+  return halves(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, times, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, times, true),
+                __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, times, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, times, true));
 }
 
 __device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u; }

@@ -253,7 +253,7 @@ inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int 
   const int rows = o.rows < block ? o.rows : block, steps = (int)(((int64_t)o.k + 127) / 128), waves = matvec_waves(mt);
   const int64_t tiles = ((int64_t)o.n + 15) / 16, room = n_cu / blocks > 1 ? n_cu / blocks : 1;
   // x in LDS, of all of K if it fits (with the weights' scales and the waves' sums), else of the largest chunk that fits twice
-  const int per_group = 128 / o.group, step_bytes = 128 * 2 * parts * rows + (type == 1 ? 0 : per_group * block * 4);
+  const int per_group = 128 / o.group, step_bytes = 128 * 2 * parts * rows + (type == 1 ? 0 : per_group * (many ? block : (rows + 3) / 4 * 4) * 8);
   auto lds = [&](int cs, int across, int steps) {
     const bool again = cs < steps || (tiles + across - 1) / across > room;
     return (cs < steps ? 2 : 1) * cs * step_bytes + (again ? 2 : 1) * across * 16 * matvec_pitch(cs * per_group) * 2 + waves * block * 16 * 4;

@@ -54,7 +54,7 @@ def test_matvec_launches_fit_their_kernel(encode):
         scales = cs * (128 // g)
         assert -(-scales // 8) * across * 16 <= 2 * threads, ("pieces of scales", a, p)
         chunks = -(-each // cs)
-        x = parts * cs * 16 * block_rows * 16 + (0 if not codes and dtype == 1 else cs * (128 // g) * 16 * mt * 4)
+        x = parts * cs * 16 * block_rows * 16 + (0 if not codes and dtype == 1 else cs * (128 // g) * (64 if mt == 4 else -(-rows // 4) * 4) * 8)
         need = (2 if chunks > 1 else 1) * x + (2 if chunks > 1 or wgs < tgs else 1) * across * 16 * ((scales + 7) // 8 * 8 + 2) * 2 + waves * 16 * mt * 16 * 4
         assert need <= lds <= 160 * 1024, ("LDS", need, a, p)
 
