@@ -406,7 +406,7 @@ struct Columns {
 #pragma unroll 1
     for (int p = lo; p < hi; p += stride) {
       const int t0 = p * kPage, page = uniform(page_of(a.c, u.s, p));
-      if (page < 0 || !is_masked(a, t0, pos_lo, pos_hi)) continue;
+      if (page < 0 || (TILE == 32 && !is_masked(a, t0, pos_lo, pos_hi))) continue;  // (narrow tiles take every page as a masked one)
       const uint8_t* v = a.c.v + ((int64_t)page * a.c.kv_heads + head) * (kPage * D) + c() * kPage;
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) {

@@ -286,6 +286,21 @@ def test_attend_nan_only_where_it_is_seen(part, dtype, rows, window):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("before,rows,group", [([200], [1], 2), ([200, 64, 3000], [1, 1, 1], 4), ([200, 90], [7, 30], 3), ([140], [80], 2)])
+def test_attend_nan_on_pages_that_every_row_sees(part, dtype, dim, before, rows, group):
+    def edit(c):
+        c.v.view(torch.uint8)[int(c.pages[0, 0]), 0, 1, 3] = 0x7F
+        c.v.view(torch.uint8)[int(c.pages[0, 1]), 0, dim - 2, 63] = 0xFF
+        if len(before) > 2:
+            c.k.view(torch.uint8)[int(c.pages[2, 20]), 0, 5, 11] = 0x7F
+    out = attend_case(part, 435, before, rows, 1, group, dim, dtype, edit=edit)
+    gone = torch.isnan(out[: rows[0]])
+    assert bool(gone[..., 1].all() and gone[..., dim - 2].all()) and int(gone.sum()) == 2 * rows[0] * group
+    assert bool(torch.isnan(out[-1]).all()) if len(before) > 2 else True
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_attend_sizes_of_queries_and_scales(part, dtype):
     def wild(c):
         u = c.v_scale.view(torch.uint8)
