@@ -73,6 +73,19 @@ __device__ __forceinline__ bool find_unit(const AttendArgs& a, int unit, Unit* u
   int c = (int)fminf(per, 1.0e9f);
   c = c < 1 ? 1 : c;
   c = (c + 3) / 4 * 4;
+  // Tiles of about as many pages as that become twice as many units, which go in two rounds: a larger unit is taken then, twice as large at most, if
+  // all fit one.  (Of 64 sequences at most, whose lengths the wave still holds.  8 x 24 rows behind 2000 tokens, 384 tiles of 33 pages for 512 places: 52
+  // us before.)
+  if (ns <= 64 && a.target > 0) {
+    const int whole = ((int)fminf(most, 1.0e9f) + 3) / 4 * 4, step = (c + 15) / 16 * 4;
+    for (int i = 0, t = c; i <= 4; ++i, t = i < 4 && t + step < whole ? t + step : whole) {
+      if (t > 2 * c) break;
+      if (wave_sum<64>((float)tiles * (float)(pages <= t ? 1 : (pages + t - 1) / t)) <= (float)a.target) {
+        c = t;
+        break;
+      }
+    }
+  }
   int base = 0;
   for (int s0 = 0; s0 < ns; s0 += 64) {
     if (ns > 64) look(s0 + lane);
@@ -487,6 +500,48 @@ __device__ __forceinline__ float* part_numbers(const AttendArgs& a, int head, in
   return a.part + (int64_t)(head * a.units + unit) * (COLS * (D + 2));
 }
 
+// N places of Q units at once: a fetch takes a microsecond, so as many as registers hold travel together (four at a time, 128 rows of 128 channels
+// in nine units took 50 us to merge).
+template <int COLS, int D, bool BF16, int N, int Q>
+__device__ __forceinline__ void merge_numbers(const AttendArgs& a, int head, const Unit& u, int col0, int cols, const float* part, const float* weights, int tid) {
+  constexpr int STEP = COLS * (D + 2);
+  const int all = cols * (D / 4);
+  for (int i0 = tid; i0 < all; i0 += 256 * N) {
+    float4 s[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) s[n] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = 0; k0 < u.chunks; k0 += Q) {
+      float4 v[N][Q];
+#pragma unroll
+      for (int e = 0; e < Q; ++e) {
+        const float* from = part + (int64_t)(k0 + e < u.chunks ? k0 + e : k0) * STEP;
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n][e] = take_back(from + 4 * (i0 + 256 * n < all ? i0 + 256 * n : i0));
+      }
+#pragma unroll
+      for (int e = 0; e < Q; ++e) {
+        const bool on = k0 + e < u.chunks;  // (no branch: the fetches would be moved behind it, one after the other)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          const int c = (i0 + 256 * n) / (D / 4);
+          const float w = weights[(on ? k0 + e : k0) * COLS + (c < COLS ? c : 0)];
+          s[n].x = fmaf(w, on ? v[n][e].x : 0.f, s[n].x);
+          s[n].y = fmaf(w, on ? v[n][e].y : 0.f, s[n].y);
+          s[n].z = fmaf(w, on ? v[n][e].z : 0.f, s[n].z);
+          s[n].w = fmaf(w, on ? v[n][e].w : 0.f, s[n].w);
+        }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = i0 + 256 * n, c = i / (D / 4), d = (i - c * (D / 4)) * 4;
+      if (i >= all) break;
+      const int col = col0 + c, r = col / a.group;
+      put_out<BF16>(a, (int64_t)(u.row0 + r) * a.out_row + (int64_t)(head * a.group + (col - r * a.group)) * a.out_head + d, s[n]);
+    }
+  }
+}
+
 template <int COLS, int D, bool BF16>
 __device__ __forceinline__ void merge(const AttendArgs& a, int head, const Unit& u, int col0, float* lds, int tid) {
   // lds [chunks][COLS]: M, then what each unit's numbers are multiplied with; behind it [chunks][COLS]: sums
@@ -521,41 +576,10 @@ __device__ __forceinline__ void merge(const AttendArgs& a, int head, const Unit&
       for (int k = j; k < u.chunks; k += EACH) tops[k * COLS] *= back;
   }
   __syncthreads();
-  for (int i = tid; i < cols * (D / 4); i += 256) {
-    const int c = i / (D / 4), d = (i - c * (D / 4)) * 4;
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float* from = part + c * D + d;
-    int k = 0;
-    for (; k + 16 <= u.chunks; k += 16) {
-      float4 v[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = take_back(from + (int64_t)(k + e) * STEP);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float w = lds[(k + e) * COLS + c];
-        s.x = fmaf(w, v[e].x, s.x);
-        s.y = fmaf(w, v[e].y, s.y);
-        s.z = fmaf(w, v[e].z, s.z);
-        s.w = fmaf(w, v[e].w, s.w);
-      }
-    }
-    for (; k < u.chunks; k += 4) {
-      float4 v[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = take_back(from + (int64_t)(k + e < u.chunks ? k + e : k) * STEP);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (k + e >= u.chunks) break;
-        const float w = lds[(k + e) * COLS + c];
-        s.x = fmaf(w, v[e].x, s.x);
-        s.y = fmaf(w, v[e].y, s.y);
-        s.z = fmaf(w, v[e].z, s.z);
-        s.w = fmaf(w, v[e].w, s.w);
-      }
-    }
-    const int col = col0 + c, r = col / a.group;
-    put_out<BF16>(a, (int64_t)(u.row0 + r) * a.out_row + (int64_t)(head * a.group + (col - r * a.group)) * a.out_head + d, s);
-  }
+  if (u.chunks <= 4) merge_numbers<COLS, D, BF16, 4, 4>(a, head, u, col0, cols, part, lds, tid);
+  else if (u.chunks <= 8) merge_numbers<COLS, D, BF16, 2, 8>(a, head, u, col0, cols, part, lds, tid);
+  else if (u.chunks <= 16 || COLS > kNarrowColumns || D == 64) merge_numbers<COLS, D, BF16, 1, 16>(a, head, u, col0, cols, part, lds, tid);
+  else if constexpr (COLS == kNarrowColumns && D > 64) merge_numbers<COLS, D, BF16, 1, 32>(a, head, u, col0, cols, part, lds, tid);  // (heads of 64 would lose half of their waves)
 }
 
 // Four waves on the pages of one 16-column tile, every fourth each.

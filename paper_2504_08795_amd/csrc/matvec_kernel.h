@@ -100,17 +100,16 @@ __device__ __forceinline__ int afresh(int v) {
   return v;
 }
 
-template <int XT, int G, int MT, bool BF16_OUT>
+template <int XT, int G, bool BF16_OUT>
 __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
   // (short: with one row a wave has two or three steps to do, and what it computes around them takes longer than the steps)
-  constexpr int PARTS = XT == kRowsF32 ? 2 : 1, GS = 128 / G, ROWS = 16 * MT, WAVES = matvec_waves(MT), T = WAVES * 64;
+  constexpr int PARTS = XT == kRowsF32 ? 2 : 1, GS = 128 / G, ROWS = kMatvecRows, T = kMatvecWaves * 64;
   constexpr int PIECES = matvec_pieces(PARTS), RING = 4, ES = XT == kRowsF32 ? 4 : XT == kRowsBf16 ? 2 : 1;
-  constexpr bool AHEAD = MT > 1;  // a chunk of x travels while the one before is computed (sixteen waves have no registers for that)
   extern __shared__ uint4 smem[];
   typedef char __attribute__((address_space(3))) * Lds;
   const Lds lds = (Lds)smem;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
-  const int split_log = (MT == 1 ? 4 : 3) - a.across;  // tiles side by side: 1 << across; waves on one of them: 1 << split_log
+  const int split_log = 4 - a.across;  // tiles side by side: 1 << across; waves on one of them: 1 << split_log
   const int own_tile = wave >> split_log, part = wave & ((1 << split_log) - 1);
   int m0 = 0, tg = blockIdx.x, share = 0;  // share: of K, where several workgroups have one
   if (a.shares > 1) {
@@ -128,8 +127,8 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
   const int steps = all_steps - step0 < a.share_steps ? all_steps - step0 : a.share_steps;
   // LDS, in bytes: x [PARTS][step][row][instruction, lane group], the last exchanged by the row's number so that rows lie on different banks, and (of scaled
   // rows) their scales and what their sums begin with [step][four rows][group][2][4], twice if there is more than one chunk; the weights' scales [tiles * 16][pitch] twice if there is more to
-  // come; sums [WAVES][ROWS][16]
-  const int fours = MT == 1 ? (rows + 3) >> 2 : 4 * MT;
+  // come; sums [waves][ROWS][16]
+  const int fours = (rows + 3) >> 2;
   const int part_size = cs * rows * 256, x_size = PARTS * part_size + (XT == kRowsBf16 ? 0 : cs * fours * GS * 32), pitch = a.pitch * 2;
   const int ws_at = (chunks > 1 ? 2 : 1) * x_size, ws_size = (16 << a.across) * pitch;
   float __attribute__((address_space(3)))* const red = (float __attribute__((address_space(3)))*)(lds + ws_at + (chunks > 1 || a.wgs < a.groups ? 2 : 1) * ws_size);
@@ -295,9 +294,7 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
     }
   };
 
-  f32x4 total[MT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) total[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  f32x4 total = {0.f, 0.f, 0.f, 0.f};
   const Spread<XT> spread;
 
   // The outputs of a group of tiles, from the waves' sums or, where K is shared, from what the workgroups left.
@@ -354,17 +351,12 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
     after.n = 0;
     if (more) {
       after = list(next, next_ch);
-      if (AHEAD && chunks > 1) load(next_ch);
       load_scales(next, next_ch);
     }
     const int x_at = chunks > 1 ? buf * x_size : 0;
-    int f[MT];  // where the wave's operands of its first step lie
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const int xr = m * 16 + c < rows ? m * 16 + c : rows - 1;
-      f[m] = x_at + ((first * rows + xr) * 16 + (g ^ (xr & 15))) * 16;
-    }
-    Lds xs = lds + x_at + PARTS * part_size + (first * fours + (MT == 1 && g >= fours ? fours - 1 : g)) * GS * 32;  // (rows that are none: any numbers will do)
+    const int xr = c < rows ? c : rows - 1;
+    int f = x_at + ((first * rows + xr) * 16 + (g ^ xr)) * 16;  // where the wave's operands of its next step lie
+    Lds xs = lds + x_at + PARTS * part_size + (first * fours + (g < fours ? g : fours - 1)) * GS * 32;  // (rows that are none: any numbers will do)
     Lds ws = lds + ws_at + buf * ws_size + (own_tile * 16 + c) * pitch + first * GS * 2;
 #pragma unroll 1
     for (int i0 = 0; i0 < turns; i0 += RING, ws += RING * GS * 2) {
@@ -378,64 +370,60 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
         if (i0 + e >= now.n) continue;
         const uint4 own_w = arranged<G>(__builtin_bit_cast(uint4, mine));
         const uint4 b[4] = {spread(own_w.x), spread(own_w.y), spread(own_w.z), spread(own_w.w)};
+        u32x4 x[PARTS][4];
+        auto operand = [&](int j) {
+          const Lds at = lds + (f ^ (j * 64));
+          x[0][j] = *(const u32x4 __attribute__((address_space(3)))*)at;
+          if (PARTS == 2) x[PARTS - 1][j] = *(const u32x4 __attribute__((address_space(3)))*)(at + part_size);
+        };
+        if (PARTS == 1) {  // (both parts of all four do not fit sixteen waves' registers)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          u32x4 x[PARTS][4];
-          auto operand = [&](int j) {
-            const Lds at = lds + (f[m] ^ (j * 64));
-            x[0][j] = *(const u32x4 __attribute__((address_space(3)))*)at;
-            if (PARTS == 2) x[PARTS - 1][j] = *(const u32x4 __attribute__((address_space(3)))*)(at + part_size);
-          };
-          if (PARTS == 1) {  // (both parts of all four do not fit sixteen waves' registers)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) operand(j);
-          }
-#pragma unroll
-          for (int u = 0; u < GS; ++u) {
-            const Lds of_x = xs + (m * 4 * GS + u) * 32;
-            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-            if (XT != kRowsBf16) sum = *(const f32x4 __attribute__((address_space(3)))*)(of_x + 16);
-            f32x4 less = {0.f, 0.f, 0.f, 0.f};  // two chains: an instruction waits for the one it adds to
-#pragma unroll
-            for (int j = u * (4 / GS); j < (u + 1) * (4 / GS); ++j) {
-              if (PARTS == 2) operand(j);
-              if (XT == kRowsBf16) {
-                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[0][j]), __builtin_bit_cast(bf16x8, b[j]), sum, 0, 0, 0);
-                less = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[0][j]), __builtin_bit_cast(bf16x8, spread.minus), less, 0, 0, 0);
-              } else {
-                sum = mfma16(__builtin_bit_cast(f16x8, x[0][j]), __builtin_bit_cast(f16x8, b[j]), sum);
-                if (PARTS == 2) less = mfma16(__builtin_bit_cast(f16x8, x[PARTS - 1][j]), __builtin_bit_cast(f16x8, b[j]), less);
-              }
-            }
-            if (XT == kRowsBf16 || PARTS == 2) {
-#pragma unroll
-              for (int q = 0; q < 4; ++q) sum[q] += less[q];
-            }
-            const float by = bf16_bits_to_f32(*(const uint16_t __attribute__((address_space(3)))*)(ws + (e * GS + u) * 2));
-            f32x4 x4 = {1.f, 1.f, 1.f, 1.f};
-            if (XT != kRowsBf16) x4 = *(const f32x4 __attribute__((address_space(3)))*)of_x;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) total[m][q] = fmaf(sum[q], by * x4[q], total[m][q]);
-          }
-          f[m] += rows * 256;
+          for (int j = 0; j < 4; ++j) operand(j);
         }
+#pragma unroll
+        for (int u = 0; u < GS; ++u) {
+          const Lds of_x = xs + u * 32;
+          f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+          if (XT != kRowsBf16) sum = *(const f32x4 __attribute__((address_space(3)))*)(of_x + 16);
+          f32x4 less = {0.f, 0.f, 0.f, 0.f};  // two chains: an instruction waits for the one it adds to
+#pragma unroll
+          for (int j = u * (4 / GS); j < (u + 1) * (4 / GS); ++j) {
+            if (PARTS == 2) operand(j);
+            if (XT == kRowsBf16) {
+              sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[0][j]), __builtin_bit_cast(bf16x8, b[j]), sum, 0, 0, 0);
+              less = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x[0][j]), __builtin_bit_cast(bf16x8, spread.minus), less, 0, 0, 0);
+            } else {
+              sum = mfma16(__builtin_bit_cast(f16x8, x[0][j]), __builtin_bit_cast(f16x8, b[j]), sum);
+              if (PARTS == 2) less = mfma16(__builtin_bit_cast(f16x8, x[PARTS - 1][j]), __builtin_bit_cast(f16x8, b[j]), less);
+            }
+          }
+          if (XT == kRowsBf16 || PARTS == 2) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum[q] += less[q];
+          }
+          const float by = bf16_bits_to_f32(*(const uint16_t __attribute__((address_space(3)))*)(ws + (e * GS + u) * 2));
+          f32x4 x4 = {1.f, 1.f, 1.f, 1.f};
+          if (XT != kRowsBf16) x4 = *(const f32x4 __attribute__((address_space(3)))*)of_x;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) total[q] = fmaf(sum[q], by * x4[q], total[q]);
+        }
+        f += rows * 256;
         xs += fours * GS * 32;
       }
     }
     if (over) {
       if (last >= 0 && chunks == 1) __syncthreads();  // (the group before has been written; with chunks a barrier lies between)
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) red[(wave * ROWS + m * 16 + g * 4 + i) * 16 + c] = total[m][i];
-        total[m] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
+      for (int i = 0; i < 4; ++i) red[(wave * ROWS + g * 4 + i) * 16 + c] = total[i];
+      total = f32x4{0.f, 0.f, 0.f, 0.f};
       last = tg;
     }
     if (!more) break;
     buf ^= 1;
-    if (!AHEAD && chunks > 1) load(next_ch);
-    if (chunks > 1) stage(buf);
+    if (chunks > 1) {
+      load(next_ch);
+      stage(buf);
+    }
     stage_scales(buf);
     tg = next;
     ch = next_ch;

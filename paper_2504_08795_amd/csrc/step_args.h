@@ -72,9 +72,9 @@ constexpr int wide_lds(int dim) { return (wide_numbers(dim) + 4) * 4; }
 // numbers of a unit in AttendArgs::part
 constexpr int64_t unit_floats(int columns, int dim) { return (int64_t)columns * (dim + 2); }
 
-// Waves of a workgroup by the blocks of 16 rows; pieces of x (8 channels) and of the weights' scales (8 of them) that a thread stages at
+// Rows of a block, waves of a workgroup; pieces of x (8 channels) and of the weights' scales (8 of them) that a thread stages at
 // a time; the distance of the scales' rows in LDS, an odd number of words.
-constexpr int matvec_waves(int blocks) { return blocks == 1 ? 16 : 8; }
+constexpr int kMatvecRows = 16, kMatvecWaves = 16;
 constexpr int matvec_pieces(int parts) { return parts == 2 ? 4 : 8; }
 constexpr int kScalePieces = 2;
 constexpr int matvec_pitch(int scales) { return (scales + 7) / 8 * 8 + 2; }

@@ -30,7 +30,7 @@ struct StepTable {
   const AqlKernel* append[2][3] = {};      // [bf16][dim 64, 128, 256]
   const AqlKernel* narrow[2][3] = {};
   const AqlKernel* wide[2][3] = {};        // (none of 256)
-  const AqlKernel* matvec[4][3][2] = {};   // [kMatvecTypes][group 32, 64, 128][16 rows, 64]
+  const AqlKernel* matvec[4][3] = {};      // [kMatvecTypes][group 32, 64, 128]
   std::string resolve(const AqlRuntime& rt);
 };
 
@@ -59,8 +59,7 @@ inline std::string StepTable::resolve(const AqlRuntime& rt) {
     }
   }
   for (int t = 0; t < 4; ++t)
-    for (int g = 0; g < 3; ++g)
-      for (int m = 0; m < 2; ++m) matvec[t][g][m] = find("daris::step_matvec<%d, %d, %d, %s>", kMatvecTypes[t].rows, 32 << g, m ? 4 : 1, tf[kMatvecTypes[t].bf16]);
+    for (int g = 0; g < 3; ++g) matvec[t][g] = find("daris::step_matvec<%d, %d, %s>", kMatvecTypes[t].rows, 32 << g, tf[kMatvecTypes[t].bf16]);
   return missing;
 }
 
@@ -223,7 +222,12 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   a.q_vec = aligned_to(o.q, 16) && o.q_row % vec == 0 && o.q_head % vec == 0;
   a.out_vec = aligned_to(o.out, bf16 ? 8 : 16) && o.out_row % 4 == 0 && o.out_head % 4 == 0;
   const int64_t columns = (int64_t)o.n_rows * a.group;
-  const bool wide = columns >= 64 * (int64_t)o.cache.n_seqs && t.wide[bf16][d];
+  // Wide tiles need columns to fill them, and narrow ones are faster while a few a CU hold all columns.  Four heads to a key head, 8 key heads, 256 CUs, us a call
+  // with narrow and with wide tiles; bf16, heads of 128: 64 x 4 rows (512 narrow tiles) 35 and 42, 8 x 32 (512) 38 and 38, 64 x 8 (1024) 48 and 43, 8 x 64
+  // (1024) 68 and 52; heads of 64: 8 x 32 28 and 28, 64 x 8 30 and 33, 8 x 64 41 and 37, 64 x 16 46 and 39.  fp32, whose wide tiles have a CU for
+  // themselves; heads of 64: 8 x 64 (1024) 50 and 51, 8 x 128 (2048) 87 and 70; heads of 128: 8 x 128 (2048) 142 and 143, 8 x 256 (4096) 273 and 205.
+  const int full = bf16 ? 2 : o.cache.dim == 64 ? 4 : 8;
+  const bool wide = columns * o.cache.dim >= 4096 * (int64_t)o.cache.n_seqs && columns * o.cache.kv_heads > (int64_t)full * kNarrowColumns * n_cu && t.wide[bf16][d];
   const int cols = wide ? kWideColumns : kNarrowColumns;
   const int64_t tiles = columns / cols + o.cache.n_seqs;  // at most: each sequence's last one may be part of a tile
   // enough workgroups for the CUs to hold several each; wide tiles that are that many by themselves are not cut
@@ -243,17 +247,20 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
 
 inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int n_cu, StepLaunch* l) {
   const int bf16 = o.dtype == DARIS_BF16, type = o.x_scale ? 2 + bf16 : bf16, parts = type == 0 ? 2 : 1, es = o.x_scale ? 1 : bf16 ? 2 : 4;
-  const int many = o.rows > 16, mt = many ? 4 : 1, block = 16 * mt, blocks = (o.rows + block - 1) / block;
+  // (blocks of 64 rows for more than 16 of them, on eight waves, were slower throughout: 64 rows, 22016 outputs of 4096 channels in bf16 61 us and 44, 17 rows 40
+  // and 28, 2000 rows 1143 and 897)
+  constexpr int block = kMatvecRows, waves = kMatvecWaves;
+  const int blocks = (o.rows + block - 1) / block;
   MatvecArgs a = {};
   a.x = o.x; a.x_scale = o.x_scale; a.w = o.w; a.w_scale = o.w_scale; a.y = o.y;
   a.x_row = o.x_row; a.w_row = o.w_row; a.y_row = o.y_row;
   a.rows = o.rows; a.n = o.n; a.k = o.k; a.gate = o.gate;
   const int x_bytes = es == 1 ? 8 : 16;
   a.x_vec = aligned_to(o.x, x_bytes) && (o.rows == 1 || (o.x_row * es) % x_bytes == 0);
-  const int rows = o.rows < block ? o.rows : block, steps = (int)(((int64_t)o.k + 127) / 128), waves = matvec_waves(mt);
+  const int rows = o.rows < block ? o.rows : block, steps = (int)(((int64_t)o.k + 127) / 128);
   const int64_t tiles = ((int64_t)o.n + 15) / 16, room = n_cu / blocks > 1 ? n_cu / blocks : 1;
   // x in LDS, of all of K if it fits (with the weights' scales and the waves' sums), else of the largest chunk that fits twice
-  const int per_group = 128 / o.group, step_bytes = 128 * 2 * parts * rows + (type == 1 ? 0 : per_group * (many ? block : (rows + 3) / 4 * 4) * 8);
+  const int per_group = 128 / o.group, step_bytes = 128 * 2 * parts * rows + (type == 1 ? 0 : per_group * ((rows + 3) / 4 * 4) * 8);
   auto lds = [&](int cs, int across, int steps) {
     const bool again = cs < steps || (tiles + across - 1) / across > room;
     return (cs < steps ? 2 : 1) * cs * step_bytes + (again ? 2 : 1) * across * 16 * matvec_pitch(cs * per_group) * 2 + waves * block * 16 * 4;
@@ -309,7 +316,7 @@ inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int 
   }
   set_args(l, a);
   const int g = o.group == 32 ? 0 : o.group == 64 ? 1 : 2;
-  return set_grid(l, t.matvec[type][g][many], (int64_t)a.wgs * blocks * a.shares, waves * 64, lds(a.steps, 1 << a.across, a.share_steps)) ? "" : kTooMany;
+  return set_grid(l, t.matvec[type][g], (int64_t)a.wgs * blocks * a.shares, waves * 64, lds(a.steps, 1 << a.across, a.share_steps)) ? "" : kTooMany;
 }
 
 // What is wrong with an operator, or "".

@@ -12,8 +12,8 @@ __global__ __launch_bounds__(T) void step_norm(NormArgs a) { norm_body<BF16, F8,
 template <bool BF16, int D>
 __global__ __launch_bounds__(256) void step_append(AppendArgs a) { append_body<BF16, D>(a); }
 
-template <int XT, int G, int MT, bool BF16_OUT>
-__global__ __launch_bounds__(matvec_waves(MT) * 64) void step_matvec(MatvecArgs a) { matvec_body<XT, G, MT, BF16_OUT>(a); }
+template <int XT, int G, bool BF16_OUT>
+__global__ __launch_bounds__(kMatvecWaves * 64) void step_matvec(MatvecArgs a) { matvec_body<XT, G, BF16_OUT>(a); }
 
 #define NORM(B, F, A)                                      \
   template __global__ void step_norm<B, F, A, 1, 64>(NormArgs);   \
@@ -28,10 +28,7 @@ NORM(true, false, false) NORM(true, false, true) NORM(true, true, false) NORM(tr
 #define APPEND(B) template __global__ void step_append<B, 64>(AppendArgs); template __global__ void step_append<B, 128>(AppendArgs); template __global__ void step_append<B, 256>(AppendArgs);
 APPEND(false) APPEND(true)
 
-#define MATVEC(X, O)                                                                                       \
-  template __global__ void step_matvec<X, 32, 1, O>(MatvecArgs); template __global__ void step_matvec<X, 32, 4, O>(MatvecArgs);   \
-  template __global__ void step_matvec<X, 64, 1, O>(MatvecArgs); template __global__ void step_matvec<X, 64, 4, O>(MatvecArgs);   \
-  template __global__ void step_matvec<X, 128, 1, O>(MatvecArgs); template __global__ void step_matvec<X, 128, 4, O>(MatvecArgs);
+#define MATVEC(X, O) template __global__ void step_matvec<X, 32, O>(MatvecArgs); template __global__ void step_matvec<X, 64, O>(MatvecArgs); template __global__ void step_matvec<X, 128, O>(MatvecArgs);
 MATVEC(kRowsF32, false) MATVEC(kRowsBf16, true) MATVEC(kRowsF8, false) MATVEC(kRowsF8, true)
 
 }  // namespace daris

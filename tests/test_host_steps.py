@@ -40,22 +40,22 @@ def test_matvec_launches_fit_their_kernel(encode):
         rows, n, k, g, dtype, codes, _, n_cu = a
         assert not isinstance(p, str), (a, p)
         kernel, groups, threads, lds, part, counters, cs, log, across, tgs, wgs, shares, each = p
-        mt, parts = (1 if kernel == 3 else 4), (2 if not codes and dtype == 0 else 1)
-        waves, blocks, steps, block_rows = threads // 64, -(-rows // (16 * mt)), -(-k // 128), min(rows, 16 * mt)
-        assert (mt == 4) == (rows > 16) and waves == (16 if mt == 1 else 8)
+        parts = 2 if not codes and dtype == 0 else 1
+        waves, blocks, steps, block_rows = threads // 64, -(-rows // 16), -(-k // 128), min(rows, 16)
+        assert kernel == 3 and waves == 16
         assert groups == wgs * blocks * shares and wgs <= max(tgs, 1) and tgs * across * 16 >= n > (tgs - 1) * across * 16, (a, p)
         assert across in (1, 2, 4, 8, 16) and across <= waves and 1 <= cs <= each and cs <= 1 << log < 2 * cs, (a, p)
         assert 1 <= shares and (shares - 1) * each < steps <= shares * each, ("shares of K", a, p)
         if shares > 1:  # one round, no more workgroups than CUs, and a place for each of their numbers
-            assert wgs == tgs and groups <= n_cu and counters == wgs * blocks and part == counters * shares * 16 * mt * 16 * across * 4, (a, p)
+            assert wgs == tgs and groups <= n_cu and counters == wgs * blocks and part == counters * shares * 16 * 16 * across * 4, (a, p)
         else:
             assert part == counters == 0
         assert (16 << log) * block_rows <= (4 if parts == 2 else 8) * threads, ("pieces of x", a, p)
         scales = cs * (128 // g)
         assert -(-scales // 8) * across * 16 <= 2 * threads, ("pieces of scales", a, p)
         chunks = -(-each // cs)
-        x = parts * cs * 16 * block_rows * 16 + (0 if not codes and dtype == 1 else cs * (128 // g) * (64 if mt == 4 else -(-rows // 4) * 4) * 8)
-        need = (2 if chunks > 1 else 1) * x + (2 if chunks > 1 or wgs < tgs else 1) * across * 16 * ((scales + 7) // 8 * 8 + 2) * 2 + waves * 16 * mt * 16 * 4
+        x = parts * cs * 16 * block_rows * 16 + (0 if not codes and dtype == 1 else cs * (128 // g) * (-(-block_rows // 4) * 4) * 8)
+        need = (2 if chunks > 1 else 1) * x + (2 if chunks > 1 or wgs < tgs else 1) * across * 16 * ((scales + 7) // 8 * 8 + 2) * 2 + waves * 16 * 16 * 4
         assert need <= lds <= 160 * 1024, ("LDS", need, a, p)
 
 
@@ -67,10 +67,11 @@ def test_attend_launches_cover_every_cut(encode):
         kv, seqs = rng.choice([1, 2, 8, 12]), int(2 ** rng.uniform(0, 9))
         asked.append((seqs * rng.choice([1, 1, 3, 40]) + rng.randrange(200), seqs, kv * rng.choice([1, 4, 7, 16]), kv, rng.choice([64, 128, 256]), rng.randrange(2), rng.choice([8, 128, 256])))
     for a, p in zip(asked, encode([("attend",) + x for x in asked])):
-        n_rows, seqs, heads, kv, dim, _, n_cu = a
+        n_rows, seqs, heads, kv, dim, dtype, n_cu = a
         kernel, groups, threads, lds, part, counters, group, target, units = p
         cols, most = (16, 256) if kernel == 1 else (128, 16)
-        assert kernel == (2 if n_rows * group >= 64 * seqs and dim < 256 else 1) and threads == 256 and groups == units * kv and lds <= 160 * 1024, (a, p)
+        full = 2 if dtype == D.BF16 else 4 if dim == 64 else 8
+        assert kernel == (2 if n_rows * group * dim >= 4096 * seqs and n_rows * heads > full * 16 * n_cu and dim < 256 else 1) and threads == 256 and groups == units * kv and lds <= 160 * 1024, (a, p)
         assert counters == (units * kv if target else 0) and part == counters * cols * (dim + 2) * 4, (a, p)
         for _ in range(5):
             cuts = sorted(rng.randrange(n_rows + 1) for _ in range(seqs - 1))
