@@ -73,18 +73,11 @@ __device__ __forceinline__ bool find_unit(const AttendArgs& a, int unit, Unit* u
   int c = (int)fminf(per, 1.0e9f);
   c = c < 1 ? 1 : c;
   c = (c + 3) / 4 * 4;
-  // Tiles of about as many pages as that become twice as many units, which go in two rounds: a larger unit is taken then, twice as large at most, if
-  // all fit one.  (Of 64 sequences at most, whose lengths the wave still holds.  8 x 24 rows behind 2000 tokens, 384 tiles of 33 pages for 512 places: 52
-  // us before.)
-  if (ns <= 64 && a.target > 0) {
-    const int whole = ((int)fminf(most, 1.0e9f) + 3) / 4 * 4, step = (c + 15) / 16 * 4;
-    for (int i = 0, t = c; i <= 4; ++i, t = i < 4 && t + step < whole ? t + step : whole) {
-      if (t > 2 * c) break;
-      if (wave_sum<64>((float)tiles * (float)(pages <= t ? 1 : (pages + t - 1) / t)) <= (float)a.target) {
-        c = t;
-        break;
-      }
-    }
+  // Tiles of little more pages than that would become twice as many units, which go in two rounds: they stay whole if all fit one.  (Of 64 sequences at most,
+  // whose lengths the wave still holds.  8 x 24 rows behind 2000 tokens, 384 tiles of 33 pages for 512 places: 52 us so, 38 in whole.)
+  if (ns <= 64 && a.target > 0 && most > (float)c && most <= 2.f * (float)c) {
+    const float whole = wave_sum<64>((float)tiles), cut = wave_sum<64>((float)tiles * (float)(pages <= c ? 1 : (pages + c - 1) / c));
+    if (cut > (float)a.target && whole <= (float)a.target) c = ((int)most + 3) / 4 * 4;
   }
   int base = 0;
   for (int s0 = 0; s0 < ns; s0 += 64) {
