@@ -10,8 +10,8 @@
  *     of a row (or head) lie side by side; distances between rows and heads ("_row", "_head") count elements, may be anything
  *     that keeps distinct elements of an output apart, and default to nothing: 0 is the distance 0.
  *   - dtype is DARIS_FP32 or DARIS_BF16: the type of activations.  Sums, softmax statistics and norms are fp32; an output is rounded
- *     once.  With DARIS_FP32 matrix products take both operands in two f16 parts (22 bits), with DARIS_BF16 in one, scaled by
- *     powers of two so that none overflows.
+ *     once.  Matrix products take what is fp32 -- queries, weights of the softmax, rows of x -- in two f16 parts (22 bits), divided by
+ *     powers of two so that none overflows; bf16 queries and weights of the softmax in one, bf16 rows of x as they are.  Codes are exact.
  *   - Eight bits are e4m3 numbers (OCP, no infinity, largest 448) and e8m0 scales, one byte each: 2^(byte - 127).  A group's scale is
  *     the smallest power of two, 2^-100 at least, that leaves none of its finite numbers above 448; a number that is not finite
  *     becomes the NaN code and has no part in the scale.
@@ -56,7 +56,7 @@ typedef struct daris_norm {
  * Token t of sequence s is token t mod 64 of page pages[s * pages_row + t / 64].  A page number outside 0 .. n_pages - 1, and
  * a token past the row's pages_row entries, stands for a page that is not there: its tokens are neither written nor attended.
  * before[s]: tokens of sequence s in front of this step's.  No page may belong to two places of the table that one call
- * writes.  dim is 64, 128 or 256.  k and v are aligned to 16 bytes.
+ * writes.  dim is 64, 128 or 256.  k and v are aligned to 16 bytes, the scales, pages and before to 4.
  */
 typedef struct daris_cache {
   uint8_t* k;
@@ -115,6 +115,8 @@ typedef struct daris_attend {
  * w [n][k / 2] bytes, the earlier k in the low half of a byte, rows w_row bytes apart; w and w_row are multiples of 16;
  * w_scale bf16 [n][k / group] dense; group 32, 64 or 128, k a multiple of it.  x is of dtype, or, with x_scale != NULL, e4m3 with
  * scales x_scale[rows][k / group] (dense), as a norm of the same group leaves them.
+ * A row that holds an infinity or a NaN has outputs that are not finite (which of them is left open).  K may be shared between workgroups by the
+ * partition's size, so that the last bits differ from partition to partition, but not from call to call.
  * gate == 0: y[row][i] = r[row][i].  gate != 0: n is even, y[row][i] = silu(r[row][2i]) * r[row][2i + 1], n / 2 columns.
  */
 typedef struct daris_matvec {
@@ -144,12 +146,12 @@ typedef int32_t daris_plan; /* handle of a planned list of operators; <0 is an e
  * wrote.  The caller's streams are synchronised first (as daris_forward does), and the results are visible to every HIP
  * stream and the host on return.  All descriptors are checked before anything is launched: DARIS_EINVAL names the first operator that is
  * wrong, and nothing has run.  Operators without rows do nothing.  Tasks may have active jobs, which go on meanwhile (those
- * that share the queue wait in line).  Attention keeps partial results in a workspace of the partition, which grows when a call
+ * that share the queue wait in line).  Attention and products keep partial results in a workspace of the partition, which grows when a call
  * needs more (DARIS_ENOMEM: nothing has run) and lives until daris_shutdown. */
 daris_status daris_run_ops(const daris_op* ops, int32_t n, daris_part p);
 /* The same in two parts, for a program that runs the same list step after step: daris_plan_ops checks the descriptors and keeps
  * the launches with their arguments in device memory (not the buffers, which it neither reads nor copies); daris_run_plan
- * runs them (a list of one 7.0 us a call in place of 8.8, of eight 19 in place of 23).  daris_free_plan gives a plan up; daris_shutdown gives up all,
+ * runs them (a list of one norm 6.8 us a call in place of 8.8, of eight 18 in place of 23).  daris_free_plan gives a plan up; daris_shutdown gives up all,
  * and handles from before it are DARIS_ERANGE for good.  daris_free_plan alone may be called on another thread. */
 daris_plan daris_plan_ops(const daris_op* ops, int32_t n, daris_part p);
 daris_status daris_run_plan(daris_plan plan);

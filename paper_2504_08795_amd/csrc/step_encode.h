@@ -34,6 +34,9 @@ struct StepTable {
   std::string resolve(const AqlRuntime& rt);
 };
 
+// 16-byte vectors of a row that a thread holds, and threads.  The first that holds the row; bf16, us a call of one row and of 4096, beside the next ones:
+// 512 wide 6.9 / 9.8 (7.1 / 10.3, 7.1 / 10.9, 7.3 / 11.9); 2048 7.2 / 17.9 (7.3 / 18.0, 7.5 / 18.2, 1024 threads 7.4 / 33.6); 8192 8.4 / 59.8 (8.0 / 65.0); read
+// twice, 16384 9.2 / 116.6 and not 8.5 / 106.4.
 constexpr struct { int vectors, threads; } kNormShapes[6] = {{1, 64}, {1, 256}, {2, 256}, {4, 256}, {4, 1024}, {0, 1024}};
 constexpr struct { int rows, bf16; } kMatvecTypes[4] = {{0, 0}, {1, 1}, {2, 0}, {2, 1}};
 
@@ -230,7 +233,8 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   const bool wide = columns * o.cache.dim >= 4096 * (int64_t)o.cache.n_seqs && columns * o.cache.kv_heads > (int64_t)full * kNarrowColumns * n_cu && t.wide[bf16][d];
   const int cols = wide ? kWideColumns : kNarrowColumns;
   const int64_t tiles = columns / cols + o.cache.n_seqs;  // at most: each sequence's last one may be part of a tile
-  // enough workgroups for the CUs to hold several each; wide tiles that are that many by themselves are not cut
+  // Two workgroups for each CU; wide tiles that are that many by themselves are not cut.  With one, two and four a CU, us a call: a token for 8 streams of 2000
+  // (32 heads of 128, 8 key heads) 21.5, 20.2, 20.3; for 64 of 2800 77, 76, 85; for one of 32000 26, 29, 38 (the merge grows with the units).
   const int64_t aim = 2 * (int64_t)n_cu / o.cache.kv_heads;
   a.target = wide && columns / cols >= aim ? 0 : aim < 1 ? 1 : (int)aim;
   const int64_t units = tiles + a.target + 1;
