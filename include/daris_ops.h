@@ -15,6 +15,7 @@
  *   - Eight bits are e4m3 numbers (OCP, no infinity, largest 448) and e8m0 scales, one byte each: 2^(byte - 127).  A group's scale is
  *     the smallest power of two, 2^-100 at least, that leaves none of its finite numbers above 448; a number that is not finite
  *     becomes the NaN code and has no part in the scale.
+ *   - Counts (rows, channels, outputs, sequences) are 2^30 at most; distances are 64 bits wide and may pass 32.
  *   - Lengths and page numbers lie in device memory and change from step to step while the descriptors stay.  The kernels check
  *     them: what they say is outside a buffer is not there.
  */

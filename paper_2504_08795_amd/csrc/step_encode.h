@@ -76,6 +76,7 @@ inline std::string text(const char* fmt, ...) {
   va_end(ap);
   return buf;
 }
+constexpr int kMostRows = 1 << 30;  // of any count that 32-bit sums of the kernels and of this file start from
 inline bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 inline std::string check_dtype(int dtype) { return dtype == DARIS_FP32 || dtype == DARIS_BF16 ? "" : text("dtype %d is neither DARIS_FP32 nor DARIS_BF16", dtype); }
@@ -85,6 +86,7 @@ inline std::string check_norm(const daris_norm& o) {
   if (!e.empty()) return e;
   const size_t es = o.dtype == DARIS_BF16 ? 2 : 4;
   if (o.rows < 0 || o.width < 1) return text("rows %d, width %d", o.rows, o.width);
+  if (o.rows > kMostRows || o.width > kMostRows) return text("more than 2^30 rows or channels (%d, %d)", o.rows, o.width);
   if (!(o.eps >= 0.f)) return "eps is negative or NaN";
   if (o.rows == 0) return "";
   if (!o.x || !o.weight || !o.y) return "NULL buffer";
@@ -101,6 +103,7 @@ inline std::string check_norm(const daris_norm& o) {
 inline std::string check_cache(const daris_cache& c, int n_rows, const int32_t* row_start) {
   if (c.dim != 64 && c.dim != 128 && c.dim != 256) return text("dim %d is not 64, 128 or 256", c.dim);
   if (c.kv_heads < 1 || c.n_seqs < 0 || c.n_pages < 0 || c.pages_row < 0 || n_rows < 0) return "a negative count, or no key head";
+  if (n_rows > kMostRows || c.n_seqs > kMostRows) return text("more than 2^30 rows or sequences (%d, %d)", n_rows, c.n_seqs);
   if (n_rows == 0 || c.n_seqs == 0) return "";
   if (c.pages_row > (1 << 24)) return "more than 2^30 tokens of a sequence";
   if (!c.before || !c.k || !c.v || !c.k_scale || !c.v_scale || !c.pages) return "NULL buffer of the cache";
@@ -144,6 +147,7 @@ inline std::string check_matvec(const daris_matvec& o) {
   if (!e.empty()) return e;
   const size_t es = o.dtype == DARIS_BF16 ? 2 : 4;
   if (o.rows < 0 || o.n < 1 || o.k < 1) return text("rows %d, n %d, k %d", o.rows, o.n, o.k);
+  if (o.rows > kMostRows || o.n > kMostRows || o.k > kMostRows) return text("more than 2^30 rows, outputs or channels (%d, %d, %d)", o.rows, o.n, o.k);
   if (o.group != 32 && o.group != 64 && o.group != 128) return text("group %d is not 32, 64 or 128", o.group);
   if (o.k % o.group) return text("k %d is no multiple of the group %d", o.k, o.group);
   if (o.gate && o.n % 2) return text("a gate of %d outputs, which are no pairs", o.n);

@@ -160,6 +160,8 @@ WRONG = [
     (attend(n_rows=-1), "count"), (attend(cache(before=P + 2)), "4 bytes"),
     (matvec(group=16), "group"), (matvec(k=48), "multiple"), (matvec(n=7, gate=1), "pairs"), (matvec(w=P + 8), "16 bytes"), (matvec(w_row=40), "16 bytes"), (matvec(x=P + 2), "aligned"),
     (matvec(x=None), "NULL"), (matvec(w_scale=P + 1), "aligned"), (matvec(rows=-1), "rows"), (matvec(n=0), "rows"), (matvec(dtype=3), "dtype"), (B.daris_op(7, 0), "no operator"),
+    (norm(width=(1 << 30) + 1), "2^30"), (norm(rows=(1 << 31) - 1), "2^30"), (append(n_rows=(1 << 30) + 1), "2^30"), (attend(n_rows=(1 << 31) - 1), "2^30"), (attend(cache(n_seqs=(1 << 31) - 1)), "2^30"),
+    (matvec(k=(1 << 31) - 128, group=128), "2^30"), (matvec(n=(1 << 31) - 1), "2^30"), (matvec(rows=(1 << 30) + 1), "2^30"),
 ]
 
 
