@@ -48,71 +48,93 @@ __device__ __forceinline__ int seen_pages(const AttendArgs& a, int rows, int bef
   return to < from ? from : to;
 }
 
-// Every wave finds the workgroup's unit by itself, 64 sequences at a time.  False: nothing to do.
-template <int TILE, int MOST>
-__device__ __forceinline__ bool find_unit(const AttendArgs& a, int unit, Unit* u) {
+// Every wave finds the workgroup's unit by itself, 64 * SETS sequences at a time (a token for 200 streams of 500, 8 query and 4 key heads of 128: 36.5 us a call, 44.2 when
+// sets of 64 came one after the other).  False: nothing to do.
+template <int TILE, int MOST, int SETS>
+__device__ __forceinline__ bool find_among(const AttendArgs& a, int unit, Unit* u) {
   const int lane = threadIdx.x & 63, ns = a.c.n_seqs;
-  int row0 = 0, rows = 0, before = 0, tiles = 0, pages = 0;
-  auto look = [&](int s) {
-    row0 = rows = before = tiles = pages = 0;
-    if (s < ns) {
-      row0 = first_row(a.c, s);
-      rows = rows_of(a.c, s);
-      before = tokens_before(a.c, s);
-      tiles = (int)(((int64_t)rows * a.group + TILE - 1) / TILE);
+  int row0[SETS], rows[SETS], before[SETS], tiles[SETS], pages[SETS];
+  auto look = [&](int s0) {  // (no branch around the fetches, so that those of all sets travel together)
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) {
+      const int s = s0 + i * 64 + lane, in = s < ns ? s : ns - 1;
+      row0[i] = first_row(a.c, in);
+      rows[i] = s < ns ? rows_of(a.c, in) : 0;
+      before[i] = tokens_before(a.c, in);
+    }
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) {
+      tiles[i] = (int)(((int64_t)rows[i] * a.group + TILE - 1) / TILE);
       int lo;
-      pages = seen_pages(a, rows, before, &lo);
-      pages -= lo;
+      pages[i] = seen_pages(a, rows[i], before[i], &lo);
+      pages[i] -= lo;
     }
   };
   float work = 0.f, most = 0.f;
-  for (int s0 = 0; s0 < ns; s0 += 64) {
-    look(s0 + lane);
-    work += wave_sum<64>((float)tiles * (float)pages);
-    most = fmaxf(most, wave_max<64>((float)pages));
+  for (int s0 = 0; s0 < ns; s0 += 64 * SETS) {
+    look(s0);
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) {
+      work += (float)tiles[i] * (float)pages[i];
+      most = fmaxf(most, (float)pages[i]);
+    }
   }
+  work = wave_sum<64>(work);
+  most = wave_max<64>(most);
   // pages of a unit: what makes `target` of them, a little more so that rounding never makes too many; the merge holds MOST of a tile
   float per = a.target > 0 ? ceilf(work * 1.0001f / (float)a.target) : most;
   per = fmaxf(per, ceilf(most * (1.f / MOST)));
   int c = (int)fminf(per, 1.0e9f);
   c = c < 1 ? 1 : c;
   c = (c + 3) / 4 * 4;
-  // Tiles of little more pages than that would become twice as many units, which go in two rounds: they stay whole if all fit one.  (Of 64 sequences at most,
-  // whose lengths the wave still holds.  8 x 24 rows behind 2000 tokens, 384 tiles of 33 pages for 512 places: 52 us so, 38 in whole.)
-  if (ns <= 64 && a.target > 0 && most > (float)c && most <= 2.f * (float)c) {
-    const float whole = wave_sum<64>((float)tiles), cut = wave_sum<64>((float)tiles * (float)(pages <= c ? 1 : (pages + c - 1) / c));
-    if (cut > (float)a.target && whole <= (float)a.target) c = ((int)most + 3) / 4 * 4;
+  auto cut = [&](int i) { return tiles[i] == 0 ? 0 : pages[i] <= c ? 1 : (pages[i] + c - 1) / c; };
+  // Tiles of little more pages than that would become twice as many units, which go in two rounds: they stay whole if all fit one.  (While the wave still holds
+  // all lengths.  8 x 24 rows behind 2000 tokens, 384 tiles of 33 pages for 512 places: 52 us so, 38 in whole.)
+  if (ns <= 64 * SETS && a.target > 0 && most > (float)c && most <= 2.f * (float)c) {
+    float whole = 0.f, units = 0.f;
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) {
+      whole += (float)tiles[i];
+      units += (float)tiles[i] * (float)cut(i);
+    }
+    if (wave_sum<64>(units) > (float)a.target && wave_sum<64>(whole) <= (float)a.target) c = ((int)most + 3) / 4 * 4;
   }
   int base = 0;
-  for (int s0 = 0; s0 < ns; s0 += 64) {
-    if (ns > 64) look(s0 + lane);
-    const int chunks = tiles == 0 ? 0 : pages <= c ? 1 : (pages + c - 1) / c;
-    const int mine = tiles * chunks;
-    int upto = mine;
+  for (int s0 = 0; s0 < ns; s0 += 64 * SETS) {
+    if (ns > 64 * SETS) look(s0);
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int o = __builtin_amdgcn_ds_bpermute((lane - d) * 4, upto);
-      if (lane >= d) upto += o;
+    for (int i = 0; i < SETS; ++i) {
+      const int chunks = cut(i), mine = tiles[i] * chunks;
+      int upto = mine;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int o = __builtin_amdgcn_ds_bpermute((lane - d) * 4, upto);
+        if (lane >= d) upto += o;
+      }
+      const int start = base + upto - mine;
+      const uint64_t hit = __ballot(unit >= start && unit < start + mine);
+      if (hit) {
+        const int l = __builtin_ctzll(hit);
+        u->s = s0 + i * 64 + l;
+        u->chunks = __builtin_amdgcn_readlane(chunks, l);
+        const int in = unit - __builtin_amdgcn_readlane(start, l);
+        u->tile = in / u->chunks;
+        u->chunk = in - u->tile * u->chunks;
+        u->first = unit - u->chunk;
+        u->per = c;
+        u->row0 = __builtin_amdgcn_readlane(row0[i], l);
+        u->rows = __builtin_amdgcn_readlane(rows[i], l);
+        u->before = __builtin_amdgcn_readlane(before[i], l);
+        return true;
+      }
+      base += __builtin_amdgcn_readlane(upto, 63);
     }
-    const int start = base + upto - mine;
-    const uint64_t hit = __ballot(unit >= start && unit < start + mine);
-    if (hit) {
-      const int l = __builtin_ctzll(hit);
-      u->s = s0 + l;
-      u->chunks = __builtin_amdgcn_readlane(chunks, l);
-      const int in = unit - __builtin_amdgcn_readlane(start, l);
-      u->tile = in / u->chunks;
-      u->chunk = in - u->tile * u->chunks;
-      u->first = unit - u->chunk;
-      u->per = c;
-      u->row0 = __builtin_amdgcn_readlane(row0, l);
-      u->rows = __builtin_amdgcn_readlane(rows, l);
-      u->before = __builtin_amdgcn_readlane(before, l);
-      return true;
-    }
-    base += __builtin_amdgcn_readlane(upto, 63);
   }
   return false;
+}
+template <int TILE, int MOST>
+__device__ __forceinline__ bool find_unit(const AttendArgs& a, int unit, Unit* u) {
+  return a.c.n_seqs <= 64 ? find_among<TILE, MOST, 1>(a, unit, u) : find_among<TILE, MOST, 4>(a, unit, u);
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -139,6 +161,12 @@ __device__ __forceinline__ uint4 seen(uint4 x, int t1, int lo, int hi) {
 template <bool BF16, int D, int TILE>
 struct Columns {
   static constexpr int PARTS = BF16 ? 1 : 2;
+  // Pages that all columns see have a form of their own where its registers leave two waves on a SIMD (64 streams, bf16, heads of 128: 83.4 us a call, 85.6
+  // with the masked form for all; fp32 of 128 would have one wave, and 256 would spill).
+  static constexpr bool kBoth = TILE == 32 || (BF16 && D < 256);
+  // A page's keys are fetched while the values of the one before are used (8 x 32 rows behind 2000 tokens, bf16, heads of 64: 22 us a call in place of 28; fp32
+  // heads of 128 and heads of 256, whose registers leave little room, were 3 % slower with it).
+  static constexpr bool kKeysAhead = kBoth || D == 64;
   static constexpr int G = 64 / TILE;            // lanes of a column
   static constexpr int DEPTH = TILE == 16 ? 32 : 16;  // channels (tokens) of a matrix instruction
   static constexpr int KT = kPage / TILE;        // score tiles of a page
@@ -267,15 +295,18 @@ struct Columns {
       x[1] = f16_of_codes(w.z, w.w);
     }
   };
-  __device__ __forceinline__ void fetch(const AttendArgs& a, int head, int page, Page* p) const {
+  __device__ __forceinline__ void fetch_keys(const AttendArgs& a, int head, int page, Page* p) const {
     const int64_t ph = (int64_t)page * a.c.kv_heads + head;
     p->ks = *(const uint32_t*)(a.c.k_scale + ph * 4);
-    p->vs = *(const uint32_t*)(a.c.v_scale + ph * 4);
     const uint8_t* k = a.c.k + ph * (kPage * D) + g() * (D / G);
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
       for (int i = 0; i < KV; ++i) p->kr[t][i] = *(const uint4*)(k + token_of(t, c()) * D + i * 16);
+  }
+  __device__ __forceinline__ void fetch_values(const AttendArgs& a, int head, int page, Page* p) const {
+    const int64_t ph = (int64_t)page * a.c.kv_heads + head;
+    p->vs = *(const uint32_t*)(a.c.v_scale + ph * 4);
     const uint8_t* v = a.c.v + ph * (kPage * D) + c() * kPage;
 #pragma unroll
     for (int t = 0; t < VT; ++t)
@@ -283,9 +314,11 @@ struct Columns {
       for (int h = 0; h < HALVES; ++h) p->vr[t][h] = *(const uint4*)(v + t * TILE * kPage + sixteenth(h) * 16);
   }
 
-  // The page that starts at token t0.  MASKED: some column does not see all of it; [see_lo, see_hi]: tokens that any column sees.
-  template <bool MASKED, typename P>
-  __device__ __forceinline__ void take_page(const AttendArgs& a, const P& p, int t0, int see_lo, int see_hi) {
+  // The page that starts at token t0.  MASKED: some column does not see all of it; [see_lo, see_hi]: tokens that any column sees; over: what is done
+  // once its keys are no longer needed.
+  template <bool MASKED, typename P, typename F>
+  __device__ __forceinline__ void take_page(const AttendArgs& a, const P& p, int t0, int see_lo, int see_hi, const F& over) {
+    const uint32_t ks = p.ks, vs = p.vs;
     // tokens of its sixteenths that the column sees
     struct {
       int from[HALVES], to[HALVES];
@@ -334,6 +367,7 @@ struct Columns {
           s[t] = mma(k, q[0][j], s[t]);
         }
     }
+    over();
     // A score is s * f + v in powers of two, v the values' scale; f > 0 and v are a sixteenth's, so its largest score is that of its largest s.
     constexpr int PER = 16 / R;  // score tiles of a sixteenth (16-column tiles: four; 32: one)
     float f[HALVES], v[HALVES];
@@ -341,8 +375,8 @@ struct Columns {
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) {
       const int part = sixteenth(h);
-      f[h] = fmaxf(factor * two_to((int)((p.ks >> (8 * part)) & 0xff) - 127), 1.0e-37f);  // (0 would make -inf a NaN)
-      v[h] = (float)((int)((p.vs >> (8 * part)) & 0xff) - 127);
+      f[h] = fmaxf(factor * two_to((int)((ks >> (8 * part)) & 0xff) - 127), 1.0e-37f);  // (0 would make -inf a NaN)
+      v[h] = (float)((int)((vs >> (8 * part)) & 0xff) - 127);
       float m = -INFINITY;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -381,7 +415,7 @@ struct Columns {
         w[0][h * 2 + (e >> 3)][e & 7] = hi;
         if (PARTS == 2) w[PARTS - 1][h * 2 + (e >> 3)][e & 7] = (_Float16)(x - (float)hi);
       }
-      sum = fmaf(add, two_to(127 - (int)((p.vs >> (8 * sixteenth(h))) & 0xff)), sum);
+      sum = fmaf(add, two_to(127 - (int)((vs >> (8 * sixteenth(h))) & 0xff)), sum);
     }
     f16x8 x[2], next[2];  // (as above, sixteen values ahead)
     auto values = [&](int n, f16x8 (&to)[2]) { p.template values<MASKED>(n / HALVES, n % HALVES, t0 + sixteenth(n % HALVES) * 16, see_lo, see_hi, &found, to); };
@@ -416,7 +450,7 @@ struct Columns {
 #pragma unroll 1
     for (int p = lo; p < hi; p += stride) {
       const int t0 = p * kPage, page = uniform(page_of(a.c, u.s, p));
-      if (page < 0 || (TILE == 32 && !is_masked(a, t0, pos_lo, pos_hi))) continue;  // (narrow tiles take every page as a masked one)
+      if (page < 0 || (kBoth && !is_masked(a, t0, pos_lo, pos_hi))) continue;
       const uint8_t* v = a.c.v + ((int64_t)page * a.c.kv_heads + head) * (kPage * D) + c() * kPage;
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) {
@@ -440,13 +474,6 @@ struct Columns {
     }
   }
 
-  template <typename P>
-  __device__ __forceinline__ void take(const AttendArgs& a, const P& p, int t0, bool masked, int see_lo, int see_hi) {
-    // (a page in registers has one form: two would hold twice the addresses, and memory has to be waited for anyway)
-    if (!P::kShared || masked) take_page<true>(a, p, t0, see_lo, see_hi);
-    else take_page<false>(a, p, t0, see_lo, see_hi);
-  }
-
   // Whether some column does not see all of the page that starts at token t0.
   static __device__ __forceinline__ bool is_masked(const AttendArgs& a, int t0, int pos_lo, int pos_hi) { return t0 + kPage - 1 > pos_lo || (a.window > 0 && t0 <= pos_hi - a.window); }
 
@@ -459,14 +486,26 @@ struct Columns {
     for (int base = lo; base < hi; base += 64 * stride) {
       const int at = base + lane * stride;
       const int mine = at < hi ? page_of(a.c, u.s, at) : -1;
-      const int n = (hi - base + stride - 1) / stride < 64 ? (hi - base + stride - 1) / stride : 64;
-      for (int i = 0; i < n; ++i) {
-        const int page = __builtin_amdgcn_readlane(mine, i);
-        if (page < 0) continue;
+      uint64_t left = __ballot(mine >= 0);
+      if (left == 0) continue;
+      int i = __builtin_ctzll(left);
+      Page p;
+      fetch_keys(a, head, __builtin_amdgcn_readlane(mine, i), &p);
+      fetch_values(a, head, __builtin_amdgcn_readlane(mine, i), &p);
+      for (;;) {
+        // the next page's keys travel while this one's values are used, and its values while its keys are
+        left &= left - 1;
+        const int next = left ? __builtin_ctzll(left) : i, page = __builtin_amdgcn_readlane(mine, next);
         const int t0 = (base + i * stride) * kPage;
-        Page p;
-        fetch(a, head, page, &p);
-        take(a, p, t0, is_masked(a, t0, pos_lo, pos_hi), see_lo, see_hi);
+        auto over = [&] {
+          if (kKeysAhead && left) fetch_keys(a, head, page, &p);
+        };
+        if (!kBoth || is_masked(a, t0, pos_lo, pos_hi)) take_page<true>(a, p, t0, see_lo, see_hi, over);
+        else take_page<false>(a, p, t0, see_lo, see_hi, over);
+        if (!left) break;
+        if (!kKeysAhead) fetch_keys(a, head, page, &p);
+        fetch_values(a, head, page, &p);
+        i = next;
       }
     }
     mark_nans(a, u, head, lo, hi, stride, pos_lo, pos_hi);
@@ -776,7 +815,10 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
     now.lane = w.lane;
     const int after = advance(p + 1), t0 = p * kPage;
     if (after < hi) fetch(page);
-    if (t0 <= pos_hi && (a.window == 0 || t0 + kPage > see_lo)) w.take(a, now, t0, w.is_masked(a, t0, pos_lo, pos_hi), see_lo, pos_hi);
+    if (t0 <= pos_hi && (a.window == 0 || t0 + kPage > see_lo)) {
+      if (w.is_masked(a, t0, pos_lo, pos_hi)) w.template take_page<true>(a, now, t0, see_lo, pos_hi, [] {});
+      else w.template take_page<false>(a, now, t0, see_lo, pos_hi, [] {});
+    }
     buf ^= 1;
     if (after < hi) store(buf);
     p = after;

@@ -59,3 +59,11 @@ def test_cuts_of_tiles_alike(parts, dtype, seqs):
     # narrow tiles, fewer than the partition's places, as many and more
     attend_case(parts[0], 930, [300] * seqs, [2] * seqs, 1, 8, 64, dtype)
     attend_case(parts[0], 931, [300 + 61 * i for i in range(seqs)], [1] * seqs, 1, 4, 64, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("seqs", [64, 65, 256, 257, 530])
+def test_more_sequences_than_a_wave_holds(parts, dtype, seqs):
+    before = [(37 * i) % 130 for i in range(seqs)]
+    attend_case(parts[1], 940 + seqs, before, [1] * seqs, 1, 2, 64, dtype, gpu_start=False)
+    attend_case(parts[1], 941 + seqs, before[:-1] + [700], [(5 * i) % 3 for i in range(seqs - 1)] + [2], 1, 1, 64, dtype)
