@@ -230,10 +230,10 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   a.out_vec = aligned_to(o.out, bf16 ? 8 : 16) && o.out_row % 4 == 0 && o.out_head % 4 == 0;
   const int64_t columns = (int64_t)o.n_rows * a.group;
   // Wide tiles need columns to fill them, and narrow ones are faster while a few a CU hold all columns.  Four heads to a key head, 8 key heads, 256 CUs, us a call
-  // with narrow and with wide tiles; bf16, heads of 128: 64 x 4 rows (512 narrow tiles) 35 and 42, 8 x 32 (512) 38 and 38, 64 x 8 (1024) 48 and 43, 8 x 64
-  // (1024) 68 and 52; heads of 64: 8 x 32 28 and 28, 64 x 8 30 and 33, 8 x 64 41 and 37, 64 x 16 46 and 39.  fp32, whose wide tiles have a CU for
-  // themselves; heads of 64: 8 x 64 (1024) 50 and 51, 8 x 128 (2048) 87 and 70; heads of 128: 8 x 128 (2048) 142 and 143, 8 x 256 (4096) 273 and 205.
-  const int full = bf16 ? 2 : o.cache.dim == 64 ? 4 : 8;
+  // with narrow and with wide tiles, bf16 and fp32.  Heads of 64: 16 x 48 rows (1536 narrow tiles) 37 and 43, 52 and 59; 8 x 128 (2048) 53 and 49, 81 and 70.  Heads of
+  // 128: 16 x 24 (768) 40 and 42, 46 and 73; 8 x 64 (1024) 60 and 52, 70 and 98; 1 x 1024 (2048) 207 and 116, 237 and 236; fp32's wide tiles have a CU for
+  // themselves.  64 x 4 rows, which fill an eighth of wide tiles: 33 and 42.
+  const int full = o.cache.dim == 64 ? 6 : bf16 ? 3 : 8;
   const bool wide = columns * o.cache.dim >= 4096 * (int64_t)o.cache.n_seqs && columns * o.cache.kv_heads > (int64_t)full * kNarrowColumns * n_cu && t.wide[bf16][d];
   const int cols = wide ? kWideColumns : kNarrowColumns;
   const int64_t tiles = columns / cols + o.cache.n_seqs;  // at most: each sequence's last one may be part of a tile

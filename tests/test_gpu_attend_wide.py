@@ -30,25 +30,25 @@ def test_chunks_of_a_prompt(parts, dtype, dim, window):
 @pytest.mark.parametrize("window", [0, 900])
 def test_units_of_a_tile(parts, dtype, window):
     p = parts[0]
-    attend_case(p, 900, [4000], [65], 1, 10, 64, dtype, window)                       # 6 tiles in 16 units
+    attend_case(p, 900, [4000], [65], 1, 12, 64, dtype, window)                       # 7 tiles in 16 units
     attend_case(p, 901, [1500], [80], 1, 14, 128, dtype, window)
     attend_case(p, 902, [20, 2600, 0, 70], [33, 34, 40, 70], 1, 6, 64, dtype, window)  # one sequence of four is long
     attend_case(p, 903, [2600, 0, 1], [40, 33, 40], 2, 5, 128, dtype, window)
 
 
 def test_a_long_sequence_among_short_ones_in_many_units(parts):
-    attend_case(parts[0], 910, [9000] + [0] * 3, [32] * 4, 1, 5, 64, "bf16")
+    attend_case(parts[0], 910, [9000] + [0] * 3, [32] * 4, 1, 7, 64, "bf16")
     attend_case(parts[0], 911, [0, 9000], [230, 32], 1, 4, 128, "fp32")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_masks_nans_and_sizes(parts, dtype):
     for p in parts:
-        steps.test_attend_nothing_and_pages_that_are_not_there(p, dtype, [40, 3, 30, 90])
-        for rows, window in (([80], 0), ([80], 20), ([300], 0), ([300], 200)):
+        steps.test_attend_nothing_and_pages_that_are_not_there(p, dtype, [200, 3, 60, 190])
+        for rows, window in (([80], 0), ([80], 20), ([400], 0), ([400], 200)):
             steps.test_attend_nan_only_where_it_is_seen(p, dtype, rows, window)
         steps.test_attend_sizes_of_queries_and_scales(p, dtype)
-        attend_case(p, 920, [100], [300], 1, 2, 64, dtype, strided=True)
+        attend_case(p, 920, [100], [300], 1, 3, 64, dtype, strided=True)
         attend_case(p, 921, [200], [90], 1, 12, 128, dtype, scale=-0.05)
         steps.test_attend_nan_on_pages_that_every_row_sees(p, dtype, 128, [140], [260], 4)
 

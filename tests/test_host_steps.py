@@ -70,7 +70,7 @@ def test_attend_launches_cover_every_cut(encode):
         n_rows, seqs, heads, kv, dim, dtype, n_cu = a
         kernel, groups, threads, lds, part, counters, group, target, units = p
         cols, most = (16, 256) if kernel == 1 else (128, 16)
-        full = 2 if dtype == D.BF16 else 4 if dim == 64 else 8
+        full = 6 if dim == 64 else 3 if dtype == D.BF16 else 8
         assert kernel == (2 if n_rows * group * dim >= 4096 * seqs and n_rows * heads > full * 16 * n_cu and dim < 256 else 1) and threads == 256 and groups == units * kv and lds <= 160 * 1024, (a, p)
         assert counters == (units * kv if target else 0) and part == counters * cols * (dim + 2) * 4, (a, p)
         for _ in range(5):
