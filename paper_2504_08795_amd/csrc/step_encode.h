@@ -282,7 +282,7 @@ inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int 
     return ((16ll << log2_up(cs)) * rows <= matvec_pieces(parts) * waves * 64) && (across * 16 << log2_up((cs * per_group + 7) / 8)) <= kScalePieces * waves * 64 && lds(cs, across, steps) <= 160 * 1024;
   };
   // Tiles side by side in a workgroup, and workgroups that share K: what makes the shortest sequence of steps for a wave.  A wave's part of a chunk
-  // counts in fours (its steps travel four at a time), and a barrier as two steps.  K is shared only where that leaves CUs none without a workgroup
+  // counts in fours (its steps travel four at a time), a barrier as two steps and a thread's piece of x as half a step.  K is shared only where that leaves CUs none without a workgroup
   // more than before and two steps for a wave; to meet takes four steps and the last workgroup two for every eight numbers that a thread fetches.
   int64_t best = -1;
   for (int across = 1; across <= waves; across *= 2) {
@@ -300,7 +300,8 @@ inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int 
       if (!fits(cs, across, each)) continue;
       const int64_t chunks = (each + cs - 1) / cs, own = ((int64_t)cs * across + waves - 1) / waves;
       const int64_t numbers = ((int64_t)rows * across * 16 + waves * 64 - 1) / (waves * 64);
-      const int64_t cost = rounds * chunks * ((own + 3) / 4 * 4 + 2) + (shares > 1 ? 4 + 2 * numbers * ((shares + 7) / 8) : 0);
+      const int64_t pieces = ((int64_t)rows * cs * 16 + waves * 64 - 1) / (waves * 64) * parts * (chunks > 1 ? rounds * chunks : 1);
+      const int64_t cost = 2 * rounds * chunks * ((own + 3) / 4 * 4 + 2) + pieces + (shares > 1 ? 8 + 4 * numbers * ((shares + 7) / 8) : 0);
       if (best >= 0 && cost >= best) continue;
       best = cost;
       a.across = log2_up(across);
