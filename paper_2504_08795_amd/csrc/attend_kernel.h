@@ -14,11 +14,11 @@
 // (bf16) or two (fp32).  The scale of V joins the exponent: w = 2^(s + log2(scale_v) - M + 10), M a running maximum
 // of s + log2(scale_v) (at most 5 behind): w fits f16 whatever the scales are, and the sum of weights takes 1 / scale_v back out.
 //
-// Masks cost nothing on pages that all columns see.  On the others scores are selected away, and values that no column sees, as well as
+// Masks cost nothing on pages that all columns see, where these have a form of their own (kBoth).  On the others scores are selected away, and values that no column sees, as well as
 // NaN codes, whose product with a zero weight would spoil other columns, are cleared; mark_nans finds the columns that see them.
 //
-// Narrow tiles are bound by the bytes of the cache: 64 streams, 8 key heads of 128, 368 MB in 84 us, 4.4 TB/s (a pure read reaches 6.2, a copy 5.1); one
-// stream of 8001 tokens, 16 MB, takes 11.3 us, which is the chain lengths -> pages -> keys -> values -> the units' numbers -> the merge.
+// Narrow tiles are bound by the bytes of the cache: 64 streams, 8 key heads of 128, 368 MB in 78 to 81 us, 4.6 TB/s (a pure read reaches 6.2, a copy 5.1); one
+// stream of 8001 tokens, 16 MB, takes 10.9 us, which is the chain lengths -> pages -> keys -> values -> the units' numbers -> the merge.
 // Wide ones are bound by instruction issue: 2048 rows behind 4100 tokens (32 heads of 128), 172 GFLOP in 203 us, 850 TFLOP/s (a large matrix product:
 // 1190).  The matrix instructions take 40 % of a SIMD's cycles and the vector ones (a wave's page: 32 exponentials at a quarter of the rate and some 250
 // others) the rest; what one wave computes does not hide behind another's matrix instructions.

@@ -238,7 +238,7 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   const int cols = wide ? kWideColumns : kNarrowColumns;
   const int64_t tiles = columns / cols + o.cache.n_seqs;  // at most: each sequence's last one may be part of a tile
   // Two workgroups for each CU; wide tiles that are that many by themselves are not cut.  With one, two and four a CU, us a call: a token for 8 streams of 2000
-  // (32 heads of 128, 8 key heads) 21.5, 20.2, 20.3; for 64 of 2800 77, 76, 85; for one of 32000 26, 29, 38 (the merge grows with the units).
+  // (32 heads of 128, 8 key heads) 19.0, 18.8, 19.3; for 64 of 2800 73, 73, 82; for one of 32000 24, 27, 36 (the merge grows with the units).
   const int64_t aim = 2 * (int64_t)n_cu / o.cache.kv_heads;
   a.target = wide && columns / cols >= aim ? 0 : aim < 1 ? 1 : (int)aim;
   const int64_t units = tiles + a.target + 1;
