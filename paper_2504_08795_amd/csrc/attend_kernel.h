@@ -12,7 +12,8 @@
 // Keys [token][channel] and values [channel][token] are loaded in the operands' own order, 16 bytes a lane, and spread from
 // e4m3 to f16 two at a time (exact).  Queries are divided by a power of two that brings their largest number to 2^14, in one f16 part
 // (bf16) or two (fp32).  The scale of V joins the exponent: w = 2^(s + log2(scale_v) - M + 10), M a running maximum
-// of s + log2(scale_v) (at most 5 behind): w fits f16 whatever the scales are, and the sum of weights takes 1 / scale_v back out.
+// of s + log2(scale_v) (at most 5 behind): w fits f16 whatever the scales are, and the sum of weights takes 1 / scale_v back out.  What is nothing beside the
+// largest s + log2(scale_v) may have the largest s (zeros beside large values), so the sum is scaled in steps that leave fp32's range no more than it does itself.
 //
 // Masks cost nothing on pages that all columns see, where these have a form of their own (kBoth).  On the others scores are selected away, and values that no column sees, as well as
 // NaN codes, whose product with a zero weight would spoil other columns, are cleared; mark_nans finds the columns that see them.
@@ -28,6 +29,7 @@
 namespace daris {
 
 constexpr float kWeightBits = 10.f, kMaxLag = 5.f;  // a weight is at most 2^15
+constexpr float kLeastWeight = 100.f;               // 2^-100: 26 bits above the smallest number, far below f16's
 
 // What a workgroup has to do.
 struct Unit {
@@ -370,7 +372,7 @@ struct Columns {
     over();
     // A score is s * f + v in powers of two, v the values' scale; f > 0 and v are a sixteenth's, so its largest score is that of its largest s.
     constexpr int PER = 16 / R;  // score tiles of a sixteenth (16-column tiles: four; 32: one)
-    float f[HALVES], v[HALVES];
+    float f[HALVES], v[HALVES], biggest[HALVES];
     float big = -INFINITY;
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) {
@@ -387,35 +389,55 @@ struct Columns {
         }
         m = fmaxf(m, x);
       }
-      big = fmaxf(big, fmaf(m, f[h], v[h]));
+      biggest[h] = fmaf(m, f[h], v[h]);
+      big = fmaxf(big, biggest[h]);
     }
     big = lanes_max<TILE, 64>(big);
     // M follows only when it has been passed by kMaxLag: up to there the weights have room, and most pages then leave the outputs alone
     const float now = big > top + kMaxLag ? big : top;
     if (__any(now != top)) {
       asm volatile("");  // (a branch: left to itself the compiler multiplies always)
-      const float shrink = now == top ? 1.f : exp2_fast(top - now);
+      const float half = now == top ? 1.f : exp2_fast(0.5f * (top - now)), shrink = half * half;
 #pragma unroll
       for (int t = 0; t < VT; ++t)
 #pragma unroll
         for (int i = 0; i < R; ++i) o[t][i] *= shrink;
-      sum *= shrink;
+      sum = sum * half * half;
       top = now;
     }
     const float base = (top == -INFINITY ? 0.f : top) - kWeightBits;
+    // Weights below 2^-kLeastWeight are nothing among the outputs, but may be all of the sum, if their values are far smaller than others: they are
+    // then taken times a power of two, which the sum takes out again with their scale.
+    float least = INFINITY, from[HALVES];
+    int back[HALVES];
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+      least = fminf(least, biggest[h]);
+      from[h] = v[h] - base;
+      back[h] = 127 - (int)((vs >> (8 * sixteenth(h))) & 0xff);
+    }
+    if (__any(least < base - kLeastWeight)) {
+      asm volatile("");  // (a branch, as above)
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) {
+        const int up = (int)fminf(fmaxf(base - kLeastWeight - biggest[h], 0.f), 300.f);
+        from[h] += (float)up;
+        back[h] -= up;
+      }
+    }
     f16x8 w[PARTS][2 * HALVES];
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) {
       float add = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const float x = exp2_fast(fmaf(s[h * PER + e / R][e % R], f[h], v[h] - base));
+        const float x = exp2_fast(fmaf(s[h * PER + e / R][e % R], f[h], from[h]));
         add += x;
         const _Float16 hi = (_Float16)x;
         w[0][h * 2 + (e >> 3)][e & 7] = hi;
         if (PARTS == 2) w[PARTS - 1][h * 2 + (e >> 3)][e & 7] = (_Float16)(x - (float)hi);
       }
-      sum = fmaf(add, two_to(127 - (int)((vs >> (8 * sixteenth(h))) & 0xff)), sum);
+      sum += __builtin_amdgcn_ldexpf(add, back[h]);
     }
     f16x8 x[2], next[2];  // (as above, sixteen values ahead)
     auto values = [&](int n, f16x8 (&to)[2]) { p.template values<MASKED>(n / HALVES, n % HALVES, t0 + sixteenth(n % HALVES) * 16, see_lo, see_hi, &found, to); };
@@ -602,9 +624,9 @@ __device__ __forceinline__ void merge(const AttendArgs& a, int head, const Unit&
     const float base = top == -INFINITY ? 0.f : top;
     if (c < cols)
       for (int k = j; k < u.chunks; k += EACH) {
-        const float w = exp2_fast(tops[k * COLS] - base);
-        tops[k * COLS] = w;
-        sum = fmaf(w, sums[k * COLS], sum);
+        const float half = exp2_fast(0.5f * (tops[k * COLS] - base));  // (of the weight, which may be 0 where its part of the sum is not)
+        tops[k * COLS] = half * half;
+        sum = fmaf(half * sums[k * COLS], half, sum);
       }
     sum = wave_sum<EACH>(sum);
     const float back = sum == 0.f ? 0.f : 1.f / sum;
@@ -656,9 +678,9 @@ __device__ __forceinline__ void attend_narrow_body(const AttendArgs& a) {
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const float f = exp2_fast(tops[k * COLS + c] - base);
+      const float half = exp2_fast(0.5f * (tops[k * COLS + c] - base)), f = half * half;  // (as in merge)
       const float4 v = *(const float4*)(lds + (k * COLS + c) * PITCH + d);
-      sum = fmaf(f, sums[k * COLS + c], sum);
+      sum = fmaf(half * sums[k * COLS + c], half, sum);
       s.x = fmaf(f, v.x, s.x);
       s.y = fmaf(f, v.y, s.y);
       s.z = fmaf(f, v.z, s.z);
