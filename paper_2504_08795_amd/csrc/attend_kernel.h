@@ -127,7 +127,9 @@ __device__ __forceinline__ bool find_among(const AttendArgs& a, int unit, Unit* 
         u->row0 = __builtin_amdgcn_readlane(row0[i], l);
         u->rows = __builtin_amdgcn_readlane(rows[i], l);
         u->before = __builtin_amdgcn_readlane(before[i], l);
-        return true;
+        // A row_start that decreases counts rows twice, and the last units are none that was launched: a tile that has such units is left out as a whole, lest
+        // those that were launched wait at its counter for good.
+        return u->chunks == 1 || u->first + u->chunks <= a.units;
       }
       base += __builtin_amdgcn_readlane(upto, 63);
     }

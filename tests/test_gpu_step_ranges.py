@@ -3,8 +3,8 @@ import pytest
 import torch
 
 import paper_2504_08795_amd as D
-from step_helpers import PAGE
-from test_gpu_steps import attend_case
+from step_helpers import PAGE, Cache
+from test_gpu_steps import attend_case, rand, run
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,21 @@ def test_zeros_beside_large_values_keep_their_weights(parts, dtype, where, byte)
 def test_units_of_zeros_keep_their_weights(parts, dtype, zero):
     attend_case(parts[0], 20, [6000], [1], 1, 2, 64, dtype, edit=zeros_beside(220, zero))
     attend_case(parts[1], 21, [4000], [65], 1, 12, 64, dtype, edit=zeros_beside(220, zero))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_table_of_rows_that_decreases_spoils_no_later_call(parts, dtype):
+    # 160 rows three times (the last time 40 of them, behind 6360 tokens): 20 tiles of one unit and 3 of 5, of which 32 units are launched -- two of the last tile
+    starts, before, units = [0, 160, 0, 160, 0, 40], [0, 0, 0, 0, 6360], 160 // 16 + 5 + 16 + 1
+    pages = [-(-(b + max(0, y - x)) // PAGE) for b, x, y in zip(before, starts, starts[1:])]
+    tiles = [-(-max(0, y - x) // 16) for x, y in zip(starts, starts[1:])]
+    per = (-(-int(sum(t * q for t, q in zip(tiles, pages)) * 1.0001 + 1) // 16) + 3) // 4 * 4
+    firsts = [20 + i * -(-pages[4] // per) for i in range(tiles[4])]
+    assert tiles == [10, 0, 10, 0, 3] and -(-pages[4] // per) == 5 and firsts[2] < units < firsts[2] + 5
+    c = Cache(30, before, [160, 0, 0, 0, 40], 1, 64).filled(31)
+    q = rand((160, 1, 64), dtype, 32).cuda()
+    out = torch.zeros_like(q)
+    run(parts[1], D.make_attend(c.gpu(D), q, out, row_start=torch.tensor(starts, dtype=torch.int32).cuda(), scale=0.1))
+    # a tile whose units meet at the counter of that last one
+    name = "bf16" if dtype == torch.bfloat16 else "fp32"
+    attend_case(parts[1], 33, [10] * firsts[2] + [9000], [1] * (firsts[2] + 1), 1, 2, 64, name)
