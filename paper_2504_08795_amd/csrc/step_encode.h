@@ -224,7 +224,7 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   a.q = o.q; a.out = o.out;
   a.q_row = o.q_row; a.q_head = o.q_head; a.out_row = o.out_row; a.out_head = o.out_head;
   a.group = o.q_heads / o.cache.kv_heads;
-  a.window = o.window;
+  a.window = o.window > (1 << 30) ? 0 : o.window;  // (no token lies further back; its distance to a position in front of the first would pass 32 bits)
   a.scale = o.scale * 1.44269504088896341f;
   a.q_vec = aligned_to(o.q, 16) && o.q_row % vec == 0 && o.q_head % vec == 0;
   a.out_vec = aligned_to(o.out, bf16 ? 8 : 16) && o.out_row % 4 == 0 && o.out_head % 4 == 0;

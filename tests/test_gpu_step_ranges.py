@@ -73,3 +73,12 @@ def test_a_table_of_rows_that_decreases_spoils_no_later_call(parts, dtype):
     # a tile whose units meet at the counter of that last one
     name = "bf16" if dtype == torch.bfloat16 else "fp32"
     attend_case(parts[1], 33, [10] * firsts[2] + [9000], [1] * (firsts[2] + 1), 1, 2, 64, name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 30 + 1, 2 ** 30])
+def test_windows_that_reach_everything(parts, dtype, window):
+    attend_case(parts[0], 40, [-5], [8], 1, 1, 64, dtype, window)
+    attend_case(parts[0], 41, [0, 100], [40, 3], 1, 2, 64, dtype, window)
+    attend_case(parts[1], 42, [0, -5], [90, 80], 2, 4, 64, dtype, window)
+    attend_case(parts[1], 43, [300], [130], 2, 5, 128, dtype, window)
