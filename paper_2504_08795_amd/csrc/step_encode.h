@@ -240,7 +240,11 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   // Two workgroups for each CU; wide tiles that are that many by themselves are not cut.  With one, two and four a CU, us a call: a token for 8 streams of 2000
   // (32 heads of 128, 8 key heads) 19.0, 18.8, 19.3; for 64 of 2800 73, 73, 82; for one of 32000 24, 27, 36 (the merge grows with the units).
   const int64_t aim = 2 * (int64_t)n_cu / o.cache.kv_heads;
-  a.target = wide && columns / cols >= aim ? 0 : aim < 1 ? 1 : (int)aim;
+  // Nor are those of one sequence that are as many, whose pages are alike, and narrow ones that are 64 for each place: a workspace for every tile would grow with a
+  // prompt's rows.  (us a call whole and cut, 8 query and 8 key heads of 256: 32 x 256 rows behind 0 to 3100 tokens, 64 a place, 3524 and 3519; 32 x 256 rows and a row
+  // behind 32000, 1834 and 1621; 8 x 256 and such a row, 16 a place, 902 and 415.)
+  const bool whole = columns / cols >= (wide || o.cache.n_seqs == 1 ? 1 : 64) * aim;
+  a.target = whole ? 0 : aim < 1 ? 1 : (int)aim;
   const int64_t units = tiles + a.target + 1;
   if (units * o.cache.kv_heads > 0x7fffffll) return kTooMany;
   a.units = (int)units;

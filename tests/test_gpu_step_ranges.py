@@ -82,3 +82,9 @@ def test_windows_that_reach_everything(parts, dtype, window):
     attend_case(parts[0], 41, [0, 100], [40, 3], 1, 2, 64, dtype, window)
     attend_case(parts[1], 42, [0, -5], [90, 80], 2, 4, 64, dtype, window)
     attend_case(parts[1], 43, [300], [130], 2, 5, 128, dtype, window)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_narrow_tiles_of_prompts_stay_whole(parts, dtype):
+    attend_case(parts[1], 50, [70], [40], 1, 16, 256, dtype)                                    # one sequence, more tiles than places
+    attend_case(parts[1], 51, [70, 0, 200], [300, 1, 41], 8, 6, 256, dtype, window=50)          # 128 a key head, 64 for each of its two places
