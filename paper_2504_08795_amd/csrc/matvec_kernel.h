@@ -3,8 +3,8 @@
 // y^T is computed in tiles of 16 outputs: a wave reads 16 rows of weights, 128 channels (a step) at a time, 16 bytes a lane straight
 // into registers, spreads the nibbles and multiplies them with the rows of x on the matrix instructions.  A group's sum is
 // taken by them alone and multiplied by the weights' scale once, in fp32.  x lies in LDS in the order of the nibbles.
-//   bf16 x: as it is.  0x4300 | c is the bf16 number 128 + c; a second product with the constant -136 takes the rest away.  Both sums are 17 times
-//     as large as the result, which costs four of fp32's 24 bits.
+//   bf16 x: as it is.  0x3b80 | c is the bf16 number 2^-15 (128 + c); a second product with the constant -136 * 2^-15 takes the rest away.  Both sums are 17 times
+//     as large as the result, which costs four of fp32's 24 bits; the power of two, which the end takes out again, keeps those of 128 of the largest numbers finite.
 //   fp32 x: two f16 parts (22 bits), a group of a row divided by a power of two that makes its largest number 2^14 and more, so that
 //     nothing overflows; 0x3c00 | c << 6 is the f16 number (16 + c) / 16.  The sum begins with -24 / 16 of that of x, which is taken in fp32 when x is
 //     staged; it gets up to four times as large as the result, which costs two of fp32's 24 bits.  (c - 8 took three packed additions more for eight
@@ -28,14 +28,14 @@ enum { kRowsF32 = 0, kRowsBf16 = 1, kRowsF8 = 2 };
 // What spreads nibbles: the constants stay in registers (an instruction that takes both as literals does not exist, and two take twice as long).
 template <int XT>
 struct Spread {
-  uint32_t mask = XT == kRowsBf16 ? 0x000f000fu : 0x03c003c0u, high = XT == kRowsBf16 ? 0x43004300u : 0x3c003c00u;
-  u32x4 minus = {0xc308c308u, 0xc308c308u, 0xc308c308u, 0xc308c308u};  // -136 as bf16
+  uint32_t mask = XT == kRowsBf16 ? 0x000f000fu : 0x03c003c0u, high = XT == kRowsBf16 ? 0x3b803b80u : 0x3c003c00u;
+  u32x4 minus = {0xbb88bb88u, 0xbb88bb88u, 0xbb88bb88u, 0xbb88bb88u};  // -136 * 2^-15 as bf16
   __device__ __forceinline__ Spread() {
     asm volatile("" : "+s"(mask));
     asm volatile("" : "+v"(high));
     if (XT == kRowsBf16) asm volatile("" : "+v"(minus));
   }
-  // Eight nibbles in the order 0 4 1 5 2 6 3 7: 128 + c as bf16, or 1 + c / 16 as f16.
+  // Eight nibbles in the order 0 4 1 5 2 6 3 7: 2^-15 (128 + c) as bf16, or 1 + c / 16 as f16.
   __device__ __forceinline__ uint4 operator()(uint32_t w) const {
     if (XT == kRowsBf16) return make_uint4((w & mask) | high, ((w >> 4) & mask) | high, ((w >> 8) & mask) | high, ((w >> 12) & mask) | high);
     return make_uint4(((w << 6) & mask) | high, ((w << 2) & mask) | high, ((w >> 2) & mask) | high, ((w >> 6) & mask) | high);
@@ -417,7 +417,7 @@ __device__ __forceinline__ void matvec_body(const MatvecArgs& a) {
     if (over) {
       if (last >= 0 && chunks == 1) __syncthreads();  // (the group before has been written; with chunks a barrier lies between)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) red[(wave * ROWS + g * 4 + i) * 16 + c] = total[i];
+      for (int i = 0; i < 4; ++i) red[(wave * ROWS + g * 4 + i) * 16 + c] = XT == kRowsBf16 ? total[i] * 32768.f : total[i];
       total = f32x4{0.f, 0.f, 0.f, 0.f};
       last = tg;
     }

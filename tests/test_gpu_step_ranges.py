@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2504_08795_amd as D
-from step_helpers import PAGE, Cache
+from step_helpers import PAGE, Cache, close, matvec
 from test_gpu_steps import attend_case, rand, run
 
 pytestmark = pytest.mark.gpu
@@ -88,3 +88,23 @@ def test_windows_that_reach_everything(parts, dtype, window):
 def test_narrow_tiles_of_prompts_stay_whole(parts, dtype):
     attend_case(parts[1], 50, [70], [40], 1, 16, 256, dtype)                                    # one sequence, more tiles than places
     attend_case(parts[1], 51, [70, 0, 200], [300, 1, 41], 8, 6, 256, dtype, window=50)          # 128 a key head, 64 for each of its two places
+
+
+# ---- 4-bit products -----------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("rows,n,k,group", [(3, 40, 512, 128), (16, 17, 4096, 64), (1, 4096, 256, 32), (1, 40, 25088, 128)])
+@pytest.mark.parametrize("one_sign", [False, True])
+def test_rows_of_the_largest_numbers(parts, rows, n, k, group, one_sign):
+    g = torch.Generator().manual_seed(60 + rows)
+    w = torch.randint(0, 256, (n, k // 2), generator=g, dtype=torch.uint8)
+    ws = (torch.rand((n, k // group), generator=g) * (0.1 / k)).bfloat16()                # the sizes of all terms together stay below 0.8 of the largest number
+    x = (torch.rand((rows, k), generator=g) * 0.1 + 0.9) * 3.38e38
+    if not one_sign:
+        x *= torch.randint(0, 2, (rows, k), generator=g) * 2 - 1
+    x = x.bfloat16()
+    assert bool(torch.isfinite(x).all())
+    y = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda")
+    run(parts[0], D.make_matvec(x.cuda(), w.cuda(), ws.cuda(), y))
+    want, slack = matvec(x.double(), w, ws, False, "bf16")
+    close(y, want, slack, "y")
