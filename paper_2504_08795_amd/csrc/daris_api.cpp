@@ -211,7 +211,7 @@ struct Global {
   int64_t closed_total_left = -1;  // closed-loop runs: releases left over all tasks, -1 = no common budget
   bool prof = false;                // driver profile: where a stage's wall time goes (host clock and GPU markers)
   int64_t prof_acc[8] = {0};
-  std::mutex plans_mu;              // the two below: a plan may be freed on another thread
+  // under g_plans_mu, since a plan may be freed on another thread
   std::unordered_map<int32_t, std::shared_ptr<StepPlan>> plans;
   StepSlots slots;
 };
@@ -219,6 +219,14 @@ struct Global {
 int32_t g_next_plan = 0;  // never the same twice, so that a handle from before a shutdown is none
 
 Global* G = nullptr;
+std::mutex g_plans_mu;  // outlives G: daris_free_plan may come while another thread shuts the library down
+
+// G and its `inited` change under the mutex that daris_free_plan looks at them with; the other calls are the API thread's.
+void replace_global(Global* to) {
+  std::lock_guard<std::mutex> lk(g_plans_mu);
+  delete G;
+  G = to;
+}
 
 int64_t now_ns() {
   return std::chrono::duration_cast<std::chrono::nanoseconds>(std::chrono::steady_clock::now() - G->epoch).count();
@@ -743,8 +751,7 @@ int32_t daris_cu_per_partition(int32_t os_num, int32_t os_den, int32_t n_cu_max,
 daris_status daris_init(int device, uint64_t seed, int flags) {
   if (G && G->inited) return fail(DARIS_ESTATE, "already initialised");
   if ((flags & DARIS_NO_DEVICE) && !(flags & DARIS_VIRTUAL_TIME)) return fail(DARIS_EINVAL, "DARIS_NO_DEVICE needs DARIS_VIRTUAL_TIME");
-  delete G;
-  G = new Global();
+  replace_global(new Global());
   G->device = device;
   G->seed = seed;
   G->flags = flags;
@@ -760,15 +767,13 @@ daris_status daris_init(int device, uint64_t seed, int flags) {
     int n = 0;
     hipError_t e = hipGetDeviceCount(&n);
     if (e != hipSuccess || device < 0 || device >= n) {
-      delete G;
-      G = nullptr;
+      replace_global(nullptr);
       return fail(DARIS_EHIP, "no usable HIP device %d (%s)", device, e == hipSuccess ? "index out of range" : hipGetErrorString(e));
     }
     e = hipSetDevice(device);
     if (e == hipSuccess) e = hipFree(nullptr);  // HIP's context (and with it the HSA runtime) exists from here on
     if (e != hipSuccess) {
-      delete G;
-      G = nullptr;
+      replace_global(nullptr);
       return fail(DARIS_EHIP, "hipSetDevice failed: %s", hipGetErrorString(e));
     }
     std::string err;
@@ -799,11 +804,11 @@ daris_status daris_init(int device, uint64_t seed, int flags) {
       if (!G->util_sig.handle) err = "signal creation failed";
     }
     if (!err.empty()) {
-      delete G;
-      G = nullptr;
+      replace_global(nullptr);
       return fail(DARIS_EHIP, "%s", err.c_str());
     }
   }
+  std::lock_guard<std::mutex> lk(g_plans_mu);
   G->inited = true;
   return DARIS_OK;
 }
@@ -848,7 +853,7 @@ daris_status daris_shutdown(void) {
       if (P.step_count) (void)hipFree(P.step_count);
     }
     {
-      std::lock_guard<std::mutex> lk(G->plans_mu);
+      std::lock_guard<std::mutex> lk(g_plans_mu);
       G->plans.clear();
       for (void* m : G->slots.slabs) g_rt.free_mem(m);
     }
@@ -861,8 +866,7 @@ daris_status daris_shutdown(void) {
       }
     g_rt.free_signal(G->util_sig);
   }
-  delete G;
-  G = nullptr;
+  replace_global(nullptr);
   return DARIS_OK;
 }
 
@@ -1486,7 +1490,7 @@ daris_plan daris_plan_ops(const daris_op* ops, int32_t n, daris_part p) try {
   const daris_status st = encode_steps(ops, n, p, plan.get());
   if (st != DARIS_OK) return st;
   const size_t count = plan->launches.size();
-  std::lock_guard<std::mutex> lk(G->plans_mu);
+  std::lock_guard<std::mutex> lk(g_plans_mu);
   StepSlots& s = G->slots;
   while (s.free.size() < count) {
     char* slab = (char*)g_rt.alloc_device_for_host(StepSlots::kSlab);
@@ -1515,7 +1519,7 @@ daris_status daris_run_plan(daris_plan handle) try {
   if (check_failed() != DARIS_OK) return DARIS_EHIP;
   std::shared_ptr<StepPlan> plan;
   {
-    std::lock_guard<std::mutex> lk(G->plans_mu);
+    std::lock_guard<std::mutex> lk(g_plans_mu);
     auto it = G->plans.find(handle);
     if (it == G->plans.end()) return fail(DARIS_ERANGE, "plan handle %d out of range", handle);
     plan = it->second;
@@ -1526,8 +1530,8 @@ daris_status daris_run_plan(daris_plan handle) try {
 }
 
 daris_status daris_free_plan(daris_plan handle) {
+  std::lock_guard<std::mutex> lk(g_plans_mu);
   if (!G || !G->inited) return fail(DARIS_ESTATE, "library not initialised");
-  std::lock_guard<std::mutex> lk(G->plans_mu);
   auto it = G->plans.find(handle);
   if (it == G->plans.end()) return fail(DARIS_ERANGE, "plan handle %d out of range", handle);
   // (after a wait that failed its launches may still run: the slots stay as they are until daris_shutdown)
