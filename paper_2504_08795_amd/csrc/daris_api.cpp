@@ -1493,6 +1493,8 @@ daris_plan daris_plan_ops(const daris_op* ops, int32_t n, daris_part p) try {
   std::lock_guard<std::mutex> lk(g_plans_mu);
   StepSlots& s = G->slots;
   while (s.free.size() < count) {
+    s.slabs.reserve(s.slabs.size() + 1);
+    s.free.reserve((s.slabs.size() + 1) * (StepSlots::kSlab / StepSlots::kSlot));  // all slots that there are: daris_free_plan gives them back without allocating
     char* slab = (char*)g_rt.alloc_device_for_host(StepSlots::kSlab);
     if (!slab) {
       // (a machine whose host cannot write device memory: all slabs are the host's then, and the kernels read them over the bus)
@@ -1505,11 +1507,10 @@ daris_plan daris_plan_ops(const daris_op* ops, int32_t n, daris_part p) try {
     for (size_t at = 0; at < StepSlots::kSlab; at += StepSlots::kSlot) s.free.push_back(slab + at);
   }
   plan->args.assign(s.free.end() - count, s.free.end());
-  s.free.resize(s.free.size() - count);
   plan->moved = ~0ull;  // its arguments are written by the first run
-  const int32_t handle = g_next_plan++;
-  G->plans[handle] = std::move(plan);
-  return handle;
+  G->plans.emplace(g_next_plan, std::move(plan));
+  s.free.resize(s.free.size() - count);
+  return g_next_plan++;
 } catch (const std::bad_alloc&) {
   return fail(DARIS_ENOMEM, "host memory");
 }
