@@ -123,6 +123,13 @@ __device__ __forceinline__ bool find_among(const AttendArgs& a, int unit, Unit* 
         u->tile = in / u->chunks;
         u->chunk = in - u->tile * u->chunks;
         u->first = unit - u->chunk;
+        if (TILE == kWideColumns && u->chunks == 1) {
+          // Later tiles see more pages, and the longest come first.  Of one sequence whose tiles go in two rounds of workgroups the second comes the other way round, so
+          // that a CU gets a long and a short one.  (4 query heads to each of 8 key heads of 128, bf16, us a call in this order and in that of the rows: 1500 rows
+          // behind 4100 tokens 175 and 193, 1900 199 and 217, 2047 208 and 226, 2 x 2048 rows 108 and 138, 1000 to 4000 rows 319 and 352.)
+          const int all = __builtin_amdgcn_readlane(tiles[i], l);
+          u->tile = ns > 1 || u->tile < a.round || all > 2 * a.round ? all - 1 - u->tile : u->tile - a.round;
+        }
         u->per = c;
         u->row0 = __builtin_amdgcn_readlane(row0[i], l);
         u->rows = __builtin_amdgcn_readlane(rows[i], l);
@@ -754,15 +761,7 @@ __device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
   int* flag = (int*)(lds + wide_numbers(D));
   const int head = blockIdx.x % a.c.kv_heads, wave = uniform(threadIdx.x >> 6);
   Unit u;
-  int unit = blockIdx.x / a.c.kv_heads;
-  if (a.snake) {
-    // One sequence, a unit a tile: later tiles see more pages.  The longest come first; where two rounds of workgroups are all there are, the second comes
-    // the other way round, so that a CU gets a long one and a short one.
-    const int tiles = (int)(((int64_t)rows_of(a.c, 0) * a.group + COLS - 1) / COLS), half = (tiles + 1) / 2;
-    if (unit < tiles && (a.snake == 1 || unit < half)) unit = tiles - 1 - unit;
-    else if (unit < tiles) unit = unit - half;
-  }
-  if (!find_unit<COLS, MOST>(a, unit, &u)) return;
+  if (!find_unit<COLS, MOST>(a, blockIdx.x / a.c.kv_heads, &u)) return;
   const int all = u.rows * a.group, col0 = u.tile * COLS, mine0 = col0 + wave * 32;
   const int tile_cols = all - col0 < COLS ? all - col0 : COLS, cols = all - mine0 < 32 ? all - mine0 : 32;  // (cols may be none)
   // pages of the workgroup, and of the wave

@@ -55,7 +55,7 @@ struct AttendArgs {
   int window;
   int target;       // units to aim at for each key head, 0 = one a tile
   int units;        // launched units for each key head, at most
-  int snake;        // wide, one sequence, target 0: 1 = the last tiles first, 2 = the last half backwards, then the first half
+  int round;        // workgroups of a key head that have a CU each
   float scale;      // times log2(e)
   int q_vec, out_vec;  // rows of q are 16-byte vectors; four channels of out are one vector
 };

@@ -243,12 +243,13 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   // Nor are those of one sequence that are as many, whose pages are alike, and narrow ones that are 64 for each place: a workspace for every tile would grow with a
   // prompt's rows.  (us a call whole and cut, 8 query and 8 key heads of 256: 32 x 256 rows behind 0 to 3100 tokens, 64 a place, 3524 and 3519; 32 x 256 rows and a row
   // behind 32000, 1834 and 1621; 8 x 256 and such a row, 16 a place, 902 and 415.)
-  const bool whole = columns / cols >= (wide || o.cache.n_seqs == 1 ? 1 : 64) * aim;
+  const int64_t least = o.cache.n_seqs == 1 ? (columns + cols - 1) / cols : columns / cols;  // tiles that there are at least
+  const bool whole = least >= (wide || o.cache.n_seqs == 1 ? 1 : 64) * aim;
   a.target = whole ? 0 : aim < 1 ? 1 : (int)aim;
   const int64_t units = tiles + a.target + 1;
   if (units * o.cache.kv_heads > 0x7fffffll) return kTooMany;
   a.units = (int)units;
-  if (wide && a.target == 0 && o.cache.n_seqs == 1) a.snake = (columns + cols - 1) / cols * o.cache.kv_heads <= 2 * (int64_t)n_cu ? 2 : 1;
+  a.round = n_cu / o.cache.kv_heads;
   l->part_at = offsetof(AttendArgs, part);
   l->count_at = offsetof(AttendArgs, count);
   l->counters = a.target ? (size_t)units * o.cache.kv_heads : 0;

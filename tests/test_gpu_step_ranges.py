@@ -90,6 +90,13 @@ def test_narrow_tiles_of_prompts_stay_whole(parts, dtype):
     attend_case(parts[1], 51, [70, 0, 200], [300, 1, 41], 8, 6, 256, dtype, window=50)          # 128 a key head, 64 for each of its two places
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [40, 63, 64, 65, 100, 127, 128, 129, 200])
+def test_wide_tiles_in_less_and_more_than_two_rounds(parts, dtype, rows):
+    attend_case(parts[1], 55, [70], [rows], 1, 16, 64, dtype)               # 8 tiles of 128 columns have a CU each
+    attend_case(parts[1], 56, [300, 10], [rows, 50], 1, 16, 64, dtype, window=90)
+
+
 # ---- 4-bit products -----------------------------------------------------------------------------------------------------------
 
 

@@ -11,3 +11,14 @@ def test_the_workspace_of_attention_does_not_grow_with_the_rows_of_prompts(encod
         assert p[4] <= 600 << 20, (a, p[4] >> 20)
         if a[1] == 1:  # one sequence: units of no more tiles than go at once
             assert p[4] <= 80 << 20, (a, p[4] >> 20)
+
+
+def test_launches_of_attention_change_with_the_tiles_not_with_a_row(encode):  # noqa: F811
+    for heads, kv, dim in ((32, 8, 128), (64, 8, 128), (32, 4, 64), (16, 16, 128)):
+        per = 128 * kv // heads     # rows of a wide tile
+        rows = [r for tiles in (40, 64, 65, 128, 130) for r in (tiles * per - per + 1, tiles * per - 1, tiles * per)]
+        got = encode([("attend", r, 1, heads, kv, dim, 1, 256) for r in rows])
+        for i in range(0, len(rows), 3):
+            wide = [p for p in got[i:i + 3] if p[0] == 2]     # (40 tiles of 4 key heads of 64 are narrow ones)
+            assert len({p[7] for p in wide}) <= 1, ("units aimed at", rows[i:i + 3], got[i:i + 3])
+        assert sum(p[0] == 2 for p in got) >= 12
