@@ -123,8 +123,14 @@ def _ptr(x):
     return C.c_void_p(int(x))
 
 
+_device = None     # of the last daris_init
+
+
 def daris_init(device=0, seed=0, flags=0):
-    return _chk(lib().daris_init(device, seed, flags))
+    global _device
+    code = _chk(lib().daris_init(device, seed, flags))
+    _device = device
+    return code
 
 
 def daris_shutdown():
@@ -547,7 +553,18 @@ def make_ops(ops):
     return Ops(ops)
 
 
+def _kept(things):
+    for t in things:
+        if hasattr(t, "device"):
+            yield t
+        elif hasattr(t, "keep"):
+            yield from _kept(t.keep)
+
+
 def daris_plan_ops(ops, p=0):
+    for i, things in enumerate(ops.keep):
+        for t in _kept(things):
+            _need(_device is None or t.device.index == _device, f"operator {i}: a tensor is on {t.device}, the library on device {_device}")
     return _chk(lib().daris_plan_ops(ops.array, len(ops), p))
 
 

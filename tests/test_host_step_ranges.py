@@ -1,5 +1,11 @@
 """Launches and refusals of the operators of a generation step at the ends of their ranges, on the host.  No GPU."""
-from test_host_steps import encode  # noqa: F401 (a fixture)
+import pytest
+import torch
+
+import paper_2504_08795_amd as D
+from lib_helpers import Session
+from paper_2504_08795_amd import binding as B
+from test_host_steps import HOST, attend, cache, encode, norm  # noqa: F401 (encode: a fixture)
 
 
 def test_the_workspace_of_attention_does_not_grow_with_the_rows_of_prompts(encode):  # noqa: F811
@@ -22,3 +28,32 @@ def test_launches_of_attention_change_with_the_tiles_not_with_a_row(encode):  # 
             wide = [p for p in got[i:i + 3] if p[0] == 2]     # (40 tiles of 4 key heads of 64 are narrow ones)
             assert len({p[7] for p in wide}) <= 1, ("units aimed at", rows[i:i + 3], got[i:i + 3])
         assert sum(p[0] == 2 for p in got) >= 12
+
+
+class On:
+    """What a planned list looks at of a tensor."""
+
+    def __init__(self, index):
+        self.device = torch.device("cuda", index)
+
+
+@pytest.mark.parametrize("nested", [False, True])
+def test_tensors_of_another_gpu_are_refused(nested):
+    def ops(index):
+        first, op = norm(), attend() if nested else norm()
+        first.keep = ()
+        if nested:
+            op.keep = (cache(), On(0))
+            op.keep[0].keep = (On(0), On(index))
+        else:
+            op.keep = (On(0), None, On(index))
+        return D.make_ops([first, op])
+    with Session(HOST):
+        D.daris_create_partition(8)
+        for call in (D.daris_plan_ops, D.daris_run_ops):
+            with pytest.raises(D.DarisError) as e:
+                call(ops(1), 0)
+            assert e.value.code == D.EINVAL and "operator 1" in str(e.value) and "cuda:1" in str(e.value)
+            with pytest.raises(D.DarisError) as e:      # tensors of the library's GPU: there is none here
+                call(ops(0), 0)
+            assert e.value.code == D.ESTATE
