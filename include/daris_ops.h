@@ -97,7 +97,7 @@ typedef struct daris_append {
 
 /*
  * Attention of q [n_rows][q_heads][dim] over the cache, which holds the step's own tokens already: the row of position p
- * attends tokens p - window + 1 .. p of its sequence (window == 0: 0 .. p) with weights softmax(scale * q.k); query head
+ * attends tokens p - window + 1 .. p of its sequence (window == 0: 0 .. p) with weights softmax(scale * q.k), |scale| <= 1e38; query head
  * h reads key head h / (q_heads / kv_heads).  out [n_rows][q_heads][dim] of dtype; a row that attends nothing gets zeros.  Tokens
  * that a row does not attend have no influence on it, NaN included.
  */

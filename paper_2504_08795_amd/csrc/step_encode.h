@@ -136,6 +136,7 @@ inline std::string check_attend(const daris_attend& o) {
   const size_t es = o.dtype == DARIS_BF16 ? 2 : 4;
   if (o.q_heads < 1 || o.q_heads % o.cache.kv_heads) return text("%d query heads on %d key heads", o.q_heads, o.cache.kv_heads);
   if (o.window < 0) return "window is negative";
+  if (!(o.scale >= -1e38f && o.scale <= 1e38f)) return "scale is not finite, or above 1e38";
   if (o.n_rows == 0 || o.cache.n_seqs == 0) return "";
   if (!o.q || !o.out) return "NULL buffer";
   if (!aligned_to(o.q, es) || !aligned_to(o.out, es)) return "a buffer is not aligned to its elements";

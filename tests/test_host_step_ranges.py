@@ -57,3 +57,14 @@ def test_tensors_of_another_gpu_are_refused(nested):
             with pytest.raises(D.DarisError) as e:      # tensors of the library's GPU: there is none here
                 call(ops(0), 0)
             assert e.value.code == D.ESTATE
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -float("inf"), 3e38])
+def test_a_scale_of_scores_that_is_no_number_is_refused(scale):
+    with Session(HOST):
+        D.daris_create_partition(8)
+        op = attend(scale=scale)
+        op.keep = ()
+        with pytest.raises(D.DarisError) as e:
+            D.daris_plan_ops(D.make_ops([op]), 0)
+        assert e.value.code == D.EINVAL and "operator 0" in str(e.value) and "scale" in str(e.value)
