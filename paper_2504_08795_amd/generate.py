@@ -117,6 +117,8 @@ class Decoder:
         counts = [len(t) for t in texts]
         if len(texts) != self.streams or min(counts) < 1:
             raise ValueError("a text for every stream")
+        if min(map(min, texts)) < 0 or max(map(max, texts)) >= len(self.words):
+            raise ValueError(f"a word outside 0 .. {len(self.words) - 1}")
         self._grow(counts)
         ends = np.cumsum([0] + counts)
         rows = Rows(self, int(ends[-1]), torch.tensor(ends, dtype=torch.int32, device="cuda"))
@@ -130,7 +132,9 @@ class Decoder:
         return self.logits.argmax(1), rows
 
     def step(self, words):
-        """Appends a word to every stream; the words that follow."""
+        """Appends a word to every stream (a tensor, as prompt and step return them); the words that follow."""
+        if words.shape != (self.streams,):
+            raise ValueError(f"{tuple(words.shape)} words for {self.streams} streams")
         self._grow([1] * self.streams)
         torch.index_select(self.words, 0, words, out=self.rows.x)
         D.daris_run_ops(self.step_ops, self.part)
