@@ -163,7 +163,7 @@ def main(argv=None):
     texts = [[(7 * s + 13 * t) % 8192 for t in range(max(1, a.prompt - s))] for s in range(a.streams)]
     runs = []
     for again in range(2 if a.check else 1):
-        m = Decoder(a.streams, a.prompt + a.tokens, a.blocks, a.width, a.q_heads, a.kv_heads, a.dim, a.hidden, window=a.window,
+        m = Decoder(a.streams, a.prompt + a.tokens + 1, a.blocks, a.width, a.q_heads, a.kv_heads, a.dim, a.hidden, window=a.window,
                     dtype=torch.bfloat16 if a.dtype == "bf16" else torch.float32, part=part)
         torch.cuda.synchronize()
         t0 = time.perf_counter()
@@ -174,7 +174,7 @@ def main(argv=None):
             words = m.step(words)
             out.append(words.tolist())
         t2 = time.perf_counter()
-        for _ in range(20):                                             # the last step's list by itself, with the lengths that it had
+        for _ in range(20):                                             # the next step's list by itself, at one position
             t = time.perf_counter()
             D.daris_run_ops(m.step_ops, part)
             list_us.append((time.perf_counter() - t) * 1e6)
