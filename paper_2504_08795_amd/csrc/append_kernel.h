@@ -4,7 +4,7 @@
 // sixteenth's codes and scale, whatever part of it the step fills, so nothing is atomic.  Keys lie with a token's channels
 // side by side, lane l holds channels l * D / 64 and on; values lie with a channel's tokens side by side, lane l holds channels
 // l, l + 64, ... and writes their sixteen bytes at once.  Single tokens are bound by the latency of length -> page -> codes, prompts by
-// the bytes of k and v.  A token for each of 32 streams (32 + 8 heads of 128): 6.9 us, of which three dependent fetches are 3; nine prompts of
+// the bytes of k and v.  A token for each of 32 streams (32 + 8 heads of 128): 7.0 us, of which three dependent fetches are 3; nine prompts of
 // 4800 tokens in all (16 + 4 heads of 64, fp32), 52 MB: 14.9 us, 3.5 TB/s.
 #pragma once
 #include "step_common.h"

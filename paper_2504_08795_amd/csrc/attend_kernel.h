@@ -18,11 +18,11 @@
 // Masks cost nothing on pages that all columns see, where these have a form of their own (kBoth).  On the others scores are selected away, and values that no column sees, as well as
 // NaN codes, whose product with a zero weight would spoil other columns, are cleared; mark_nans finds the columns that see them.
 //
-// Narrow tiles are bound by the bytes of the cache: 64 streams, 8 key heads of 128, 368 MB in 78 to 81 us, 4.6 TB/s (a pure read reaches 6.2, a copy 5.1); one
-// stream of 8001 tokens, 16 MB, takes 10.9 us, which is the chain lengths -> pages -> keys -> values -> the units' numbers -> the merge.
-// Wide ones are bound by instruction issue: 2048 rows behind 4100 tokens (32 heads of 128), 172 GFLOP in 203 us, 850 TFLOP/s (a large matrix product:
-// 1190).  The matrix instructions take 40 % of a SIMD's cycles and the vector ones (a wave's page: 32 exponentials at a quarter of the rate and some 250
-// others) the rest; what one wave computes does not hide behind another's matrix instructions.
+// Narrow tiles are bound by the bytes of the cache: 64 streams, 8 key heads of 128, 368 MB in 81 to 83 us, 4.5 TB/s (a pure read reaches 6.2, a copy 5.1); one
+// stream of 8001 tokens, 16 MB, takes 11.0 us, which is the chain lengths -> pages -> keys -> values -> the units' numbers -> the merge.
+// Wide ones are bound by instruction issue: 2048 rows behind 4100 tokens (32 heads of 128), 172 GFLOP in 206 to 214 us a call, 800 to 835 TFLOP/s (a large
+// matrix product: 1190); 1900 rows 199 us, 2049 279.  The matrix instructions take 41 % of a SIMD's cycles and the vector ones (a wave's page: 32 exponentials at a
+// quarter of the rate and some 260 others) the rest; what one wave computes does not hide behind another's matrix instructions.
 #pragma once
 #include "step_common.h"
 
@@ -50,7 +50,7 @@ __device__ __forceinline__ int seen_pages(const AttendArgs& a, int rows, int bef
   return to < from ? from : to;
 }
 
-// Every wave finds the workgroup's unit by itself, 64 * SETS sequences at a time (a token for 200 streams of 500, 8 query and 4 key heads of 128: 36.5 us a call, 44.2 when
+// Every wave finds the workgroup's unit by itself, 64 * SETS sequences at a time (a token for 200 streams of 500, 8 query and 4 key heads of 128: 37 us a call, 44 when
 // sets of 64 came one after the other).  False: nothing to do.
 template <int TILE, int MOST, int SETS>
 __device__ __forceinline__ bool find_among(const AttendArgs& a, int unit, Unit* u) {
@@ -91,7 +91,7 @@ __device__ __forceinline__ bool find_among(const AttendArgs& a, int unit, Unit* 
   c = (c + 3) / 4 * 4;
   auto cut = [&](int i) { return tiles[i] == 0 ? 0 : pages[i] <= c ? 1 : (pages[i] + c - 1) / c; };
   // Tiles of little more pages than that would become twice as many units, which go in two rounds: they stay whole if all fit one.  (While the wave still holds
-  // all lengths.  8 x 24 rows behind 2000 tokens, 384 tiles of 33 pages for 512 places: 52 us so, 38 in whole.)
+  // all lengths.  8 x 24 rows behind 2000 tokens, 384 tiles of 33 pages for 512 places: 49 us so, 37 in whole.)
   if (ns <= 64 * SETS && a.target > 0 && most > (float)c && most <= 2.f * (float)c) {
     float whole = 0.f, units = 0.f;
 #pragma unroll
@@ -172,11 +172,11 @@ __device__ __forceinline__ uint4 seen(uint4 x, int t1, int lo, int hi) {
 template <bool BF16, int D, int TILE>
 struct Columns {
   static constexpr int PARTS = BF16 ? 1 : 2;
-  // Pages that all columns see have a form of their own where its registers leave two waves on a SIMD (64 streams, bf16, heads of 128: 83.4 us a call, 85.6
-  // with the masked form for all; fp32 of 128 would have one wave, and 256 would spill).
+  // Pages that all columns see have a form of their own where its registers leave two waves on a SIMD (64 streams, bf16, heads of 128: 83.0 us a call, 85.7
+  // with the masked form for all; 8 x 32 rows behind 2000 tokens, heads of 64, 22.7 and 26.8; fp32 of 128 would have one wave, and 256 would spill).
   static constexpr bool kBoth = TILE == 32 || (BF16 && D < 256);
-  // A page's keys are fetched while the values of the one before are used (8 x 32 rows behind 2000 tokens, bf16, heads of 64: 22 us a call in place of 28; fp32
-  // heads of 128 and heads of 256, whose registers leave little room, were 3 % slower with it).
+  // A page's keys are fetched while the values of the one before are used (200 streams of 500, bf16, heads of 128: 37.1 us a call in place of 38.2, 8 x 24
+  // rows behind 2000 36.8 and 37.5, though 64 streams of 8192 83.0 and 82.3; fp32 heads of 128 and heads of 256, whose registers leave little room, were 3 % slower with it).
   static constexpr bool kKeysAhead = kBoth || D == 64;
   static constexpr int G = 64 / TILE;            // lanes of a column
   static constexpr int DEPTH = TILE == 16 ? 32 : 16;  // channels (tokens) of a matrix instruction

@@ -12,12 +12,13 @@
 //     the matrix instructions keep 20 bits of such a sum.)
 //   e4m3 x: f16 holds every one of them, 16 times; the same.
 // The waves of a workgroup share x, and neighbouring ones a tile: each takes neighbouring steps of it, and their sums are added in
-// wave order.  A workgroup goes from group of tiles to group of tiles; x is staged once if all of K fits LDS, else in chunks,
-// the next one while the present one is computed, as are the weights' scales.  Every wave has four steps of weights on their way, across
-// chunks and tiles.  Where tiles are few, several workgroups share K.  The floor of few rows is the weights' bytes; what they take is the issue of instructions: some
-// 50 a step of 1 KB, staging x, the first fetches and the last sums.  One row, 4096 outputs of 4096 channels (e4m3): 6.5 us (9 MB, 1.7 us at a copy's
-// rate); 16 rows, 22016 of 4096, gated (bf16): 18 us (47 MB, 9.2); one row, 4096 of 25088 (fp32): 20.3 us (55 MB, 10.7); 2000 rows, 22016 of 4096
-// (bf16): 890 us, 405 TFLOP/s.
+// wave order.  A workgroup goes from group of tiles to group of tiles; x is staged once if all of K fits LDS, else in chunks: a wave fetches its part of the
+// next one when it is done with the present one, and waits for it; only the weights' scales are fetched a chunk ahead.  Every wave has four steps of weights on
+// their way, across chunks and tiles.  Where tiles are few, several workgroups share K.  The floor of few rows is the weights' bytes.  What they take is for two thirds the issue
+// of vector instructions (16 rows in bf16 118 for each step of 1 KB in all, one row in fp32 141; the matrix instructions hold a SIMD for a sixth of its
+// cycles), else what goes one after the other: x into LDS, a barrier, the first fetches, the last sums.  One row, 4096 outputs of 4096 channels (e4m3): 6.5 us (9 MB,
+// 1.7 us at a copy's rate); 16 rows, 22016 of 4096, gated (bf16): 18.1 us (47 MB, 9.2); one row, 4096 of 25088 (fp32): 20.1 us (55 MB, 10.7); 2000 rows,
+// 22016 of 4096 (bf16): 900 us a call, 400 TFLOP/s.
 #pragma once
 #include "step_common.h"
 

@@ -3,7 +3,8 @@
 // One workgroup a row, one pass over memory: the row stays in registers (NV 16-byte vectors a thread) between the sum of its
 // squares and its outputs, and the weights arrive while the sum is taken.  Rows beyond that are read twice (NV = 0).  Nothing is
 // computed that memory would wait for: bound by bandwidth for many rows and by latency for one.  8192 rows of 4096 (bf16, residual, codes):
-// 235 MB in 38 us with what the last-level cache holds of them, 47 us without (5.0 TB/s; a large copy reaches 5.1); one row 3.3 us.
+// 235 MB in 38 us with what the last-level cache holds of them, 47 us without (5.0 TB/s; a large copy reaches 5.1); one row 3.3 us.  Rows that are not aligned to 16
+// bytes travel element by element and take two to three times as long (8192 rows, fp32, us a call: 4096 wide 56, 4095 wide 114; bf16 with residual, 4095 wide, 184).
 #pragma once
 #include "step_common.h"
 

@@ -231,15 +231,15 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   a.out_vec = aligned_to(o.out, bf16 ? 8 : 16) && o.out_row % 4 == 0 && o.out_head % 4 == 0;
   const int64_t columns = (int64_t)o.n_rows * a.group;
   // Wide tiles need columns to fill them, and narrow ones are faster while a few a CU hold all columns.  Four heads to a key head, 8 key heads, 256 CUs, us a call
-  // with narrow and with wide tiles, bf16 and fp32.  Heads of 64: 16 x 48 rows (1536 narrow tiles) 37 and 43, 52 and 59; 8 x 128 (2048) 53 and 49, 81 and 70.  Heads of
-  // 128: 16 x 24 (768) 40 and 42, 46 and 73; 8 x 64 (1024) 60 and 52, 70 and 98; 1 x 1024 (2048) 207 and 116, 237 and 236; fp32's wide tiles have a CU for
+  // with narrow and with wide tiles, bf16 and fp32.  Heads of 64: 16 x 48 rows (1536 narrow tiles) 38 and 43, 53 and 59; 8 x 128 (2048) 53 and 49, 81 and 70.  Heads of
+  // 128: 16 x 24 (768) 41 and 43, 47 and 75; 8 x 64 (1024) 61 and 53, 71 and 100; 1 x 1024 (2048) 208 and 117, 240 and 243; 1 x 2048 444 and 203, 510 and 457; fp32's wide tiles have a CU for
   // themselves.  64 x 4 rows, which fill an eighth of wide tiles: 33 and 42.
   const int full = o.cache.dim == 64 ? 6 : bf16 ? 3 : 8;
   const bool wide = columns * o.cache.dim >= 4096 * (int64_t)o.cache.n_seqs && columns * o.cache.kv_heads > (int64_t)full * kNarrowColumns * n_cu && t.wide[bf16][d];
   const int cols = wide ? kWideColumns : kNarrowColumns;
   const int64_t tiles = columns / cols + o.cache.n_seqs;  // at most: each sequence's last one may be part of a tile
   // Two workgroups for each CU; wide tiles that are that many by themselves are not cut.  With one, two and four a CU, us a call: a token for 8 streams of 2000
-  // (32 heads of 128, 8 key heads) 19.0, 18.8, 19.3; for 64 of 2800 73, 73, 82; for one of 32000 24, 27, 36 (the merge grows with the units).
+  // (32 heads of 128, 8 key heads) 19.1, 19.0, 19.3; for 64 of 2800 74, 74, 83; for one of 32000 24, 27, 36 (the merge grows with the units).
   const int64_t aim = 2 * (int64_t)n_cu / o.cache.kv_heads;
   // Nor are those of one sequence that are as many, whose pages are alike, and narrow ones that are 64 for each place: a workspace for every tile would grow with a
   // prompt's rows.  (us a call whole and cut, 8 query and 8 key heads of 256: 32 x 256 rows behind 0 to 3100 tokens, 64 a place, 3524 and 3519; 32 x 256 rows and a row
@@ -261,8 +261,8 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
 
 inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int n_cu, StepLaunch* l) {
   const int bf16 = o.dtype == DARIS_BF16, type = o.x_scale ? 2 + bf16 : bf16, parts = type == 0 ? 2 : 1, es = o.x_scale ? 1 : bf16 ? 2 : 4;
-  // (blocks of 64 rows for more than 16 of them, on eight waves, were slower throughout: 64 rows, 22016 outputs of 4096 channels in bf16 61 us and 44, 17 rows 40
-  // and 28, 2000 rows 1143 and 897)
+  // (blocks of 64 rows for more than 16 of them, on eight waves, were slower throughout: 64 rows, 22016 outputs of 4096 channels in bf16 61 us and 43, 17 rows 40
+  // and 27, 2000 rows 1143 and 900)
   constexpr int block = kMatvecRows, waves = kMatvecWaves;
   const int blocks = (o.rows + block - 1) / block;
   MatvecArgs a = {};
