@@ -12,7 +12,8 @@
  *   - dtype is DARIS_FP32 or DARIS_BF16: the type of activations.  Sums, softmax statistics and norms are fp32; an output is rounded
  *     once.  Matrix products take what is fp32 -- queries, weights of the softmax, rows of x -- in two f16 parts (22 bits), divided by
  *     powers of two so that none overflows; bf16 queries and weights of the softmax in one, bf16 rows of x as they are.  Codes are exact.
- *     So a row of a norm with numbers above 1e19, whose squares pass fp32, gives zeros, and scores (scale * q.k) above 1e7, which fp32 holds
+ *     What a weight of the softmax has below 2^-35 of its row's largest (times their values' scales) is lost, in an output whose larger terms are zero, too.
+ *     A row of a norm with numbers above 1e19, whose squares pass fp32, gives zeros, and scores (scale * q.k) above 1e7, which fp32 holds
  *     to the next whole number only, leave their row of attention open.
  *   - Eight bits are e4m3 numbers (OCP, no infinity, largest 448) and e8m0 scales, one byte each: 2^(byte - 127).  A group's scale is
  *     the smallest power of two, 2^-100 at least, that leaves none of its finite numbers above 448; a number that is not finite

@@ -12,8 +12,9 @@
 // Keys [token][channel] and values [channel][token] are loaded in the operands' own order, 16 bytes a lane, and spread from
 // e4m3 to f16 two at a time (exact).  Queries are divided by a power of two that brings their largest number to 2^14, in one f16 part
 // (bf16) or two (fp32).  The scale of V joins the exponent: w = 2^(s + log2(scale_v) - M + 10), M a running maximum
-// of s + log2(scale_v) (at most 5 behind): w fits f16 whatever the scales are, and the sum of weights takes 1 / scale_v back out.  What is nothing beside the
-// largest s + log2(scale_v) may have the largest s (zeros beside large values), so the sum is scaled in steps that leave fp32's range no more than it does itself.
+// of s + log2(scale_v) (at most 5 behind): w fits f16 whatever the scales are (its smallest step is 2^-34 of the largest w, what is less is lost), and
+// the sum of weights takes 1 / scale_v back out.  What is nothing beside the largest s + log2(scale_v) may have the largest s (zeros beside large values), so
+// the sum is scaled in steps that leave fp32's range no more than it does itself.
 //
 // Masks cost nothing on pages that all columns see, where these have a form of their own (kBoth).  On the others scores are selected away, and values that no column sees, as well as
 // NaN codes, whose product with a zero weight would spoil other columns, are cleared; mark_nans finds the columns that see them.
