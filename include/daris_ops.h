@@ -32,7 +32,9 @@ extern "C" {
 #endif
 
 enum { DARIS_STEP_NORM = 0, DARIS_STEP_APPEND = 1, DARIS_STEP_ATTEND = 2, DARIS_STEP_MATVEC = 3 };
-enum { DARIS_PAGE_TOKENS = 64, DARIS_SCALE_TOKENS = 16 };
+/* ... of a step whose words are drafted (see daris_tree_append and on) */
+enum { DARIS_STEP_TREE_APPEND = 4, DARIS_STEP_TREE_ATTEND = 5, DARIS_STEP_SAMPLE = 6, DARIS_STEP_ACCEPT = 8, DARIS_STEP_KEEP = 9, DARIS_STEP_COPY = 10 };
+enum { DARIS_PAGE_TOKENS = 64, DARIS_SCALE_TOKENS = 16, DARIS_TREE_WORDS = 16, DARIS_SAMPLE_WORDS = 1 << 20 };
 
 /*
  * Root-mean-square norm of rows, after the addition of a residual.
@@ -133,6 +135,107 @@ typedef struct daris_matvec {
   int32_t rows, n, k, group, dtype, gate;
 } daris_matvec;
 
+/*
+ * A drafted step: the new rows of a sequence are the nodes of a tree of words that hang on its cached tokens, and all go through the model at once.
+ *
+ *     append (tree) -> attend (tree) -> ... -> sample -> accept -> keep
+ *
+ * tree [n_rows][tree_words] (dense, aligned to 8 bytes, 1 to DARIS_TREE_WORDS words a row): bit j mod 64 of word j / 64 of a row's mask is set if the row sees
+ * node j of its sequence, which is the sequence's row j.  A node's own bit and those of the nodes above it make a tree, whose nodes are numbered from
+ * the root on (a node behind the one that it hangs on); any other masks over the step's rows may stand there too.  Bits of rows that the sequence does not have are ignored.
+ *
+ * Append and attend as above with these differences.  Node j lies in the cache as token before + j, but its position -- for the turning of keys and
+ * queries -- is before + (the number of bits in its mask) - 1.  A row attends the cached tokens 0 .. before - 1 and the nodes of its mask, in this
+ * order; window != 0: the last `window` of them.  k and v of an append have the same distances.
+ */
+typedef struct daris_tree_append {
+  daris_cache cache;
+  const void* k;
+  const void* v;
+  const void* q;
+  void* q_out;
+  const float* turn;
+  const int32_t* row_start;
+  const uint64_t* tree;
+  int64_t kv_row, kv_head, q_row, q_head, qo_row, qo_head;
+  int32_t n_rows, q_heads, dtype, turn_rows, rot_dim, pairs, tree_words;
+} daris_tree_append;
+
+typedef struct daris_tree_attend {
+  daris_attend attend;
+  const uint64_t* tree;
+  int32_t tree_words;
+} daris_tree_attend;
+
+/*
+ * A word for each row of logits [rows][n] (n at most DARIS_SAMPLE_WORDS), drawn by the caller's random numbers.  With M a row's largest logit and T =
+ * temperature[row], word i weighs exp((x_i - M) / T); what weighs less than 2^-64, and NaN and -infinity, is nothing.  In this order,
+ *   top_k[row] > 0   leaves the top_k largest;
+ *   top_p[row] < 1   leaves the shortest front of these, the largest first, whose weights come to top_p of the sum of them all (one word at least);
+ *   min_p[row] > 0   leaves those of them that weigh min_p or more (and the largest).
+ * Of equal logits the word of the lower number is the larger.  word[row] is the first word that is left, by number, at which the sum of the weights that
+ * are left is more than random[row] times all of it (random in [0, 1); NaN and what is below 0 count as 0; from 1 on it is the last word).  Weights and sums have 64 bits.
+ * chance[row], if not NULL, is its weight divided by that sum.  T <= 0 or NaN, and random == NULL, give the largest (and 1); a row with nothing but NaN and
+ * -infinity gives -1 (and 0).  A row with +infinity is drawn among those words.  temperature == NULL is 1, the others' NULL leaves everything.  All per row: float, top_k int32.
+ */
+typedef struct daris_sample {
+  const void* logits;
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* random;
+  int32_t* word;
+  float* chance;
+  int64_t logits_row;
+  int32_t rows, n, dtype;
+} daris_sample;
+
+/*
+ * Which nodes of a tree stand: answers[row] is the word that the model gave behind the row's node, words[row] the node's own.  The walk starts at a
+ * sequence's node 0 (its last word, of which the cache holds no token yet) and goes from a node to the first node below it (the one of the lowest number whose mask's highest bit
+ * in front of its own is that node) whose word is the node's answer and not negative, until there is none.  path[row_start[s] + j] is the j-th node of the walk, and -1 behind the last;
+ * count[s] how many there are, word[s] the last one's answer: the sequence's new last word.  after[s] = before[s] + count[s] (after may be NULL, or before itself if
+ * no operator that follows in the list needs the old one).  A sequence without rows has count 0 and word -1.  Rows from 64 * tree_words on are no nodes.
+ */
+typedef struct daris_accept {
+  const uint64_t* tree;
+  const int32_t* words;
+  const int32_t* answers;
+  const int32_t* row_start;
+  const int32_t* before;
+  int32_t* path;
+  int32_t* count;
+  int32_t* word;
+  int32_t* after;
+  int32_t n_rows, n_seqs, tree_words;
+} daris_accept;
+
+/*
+ * Keeps the tokens of some of the step's rows: token before[s] + path[row_start[s] + j] of the cache becomes token before[s] + j, for j < count[s] (at most the
+ * sequence's rows; path as daris_accept leaves it).  Entries increase and name rows of the sequence; the first that does not ends the list.  before is what it was for the
+ * step's append.  A sixteenth that gets tokens has the largest scale of the tokens that it then holds, and its codes are rounded again where theirs was smaller; one that gets
+ * none, and what lies behind the last kept token, stays as it is.  A token whose old or new page is not there is not moved.
+ */
+typedef struct daris_keep {
+  daris_cache cache;
+  const int32_t* path;
+  const int32_t* count;
+  const int32_t* row_start;
+  int32_t n_rows;
+} daris_keep;
+
+/*
+ * Copies pages of a cache, all heads' keys, values and scales: page pairs[i][0] over page pairs[i][1] (device int32[n][2]), for sequences that are continued twice and for pages
+ * that gather elsewhere.  A pair with a page outside 0 .. n_pages - 1 is left out.  No page may be written twice, or read by one pair and written by another.
+ * Only k, v, the scales, n_pages, kv_heads and dim of the cache count.
+ */
+typedef struct daris_copy {
+  daris_cache cache;
+  const int32_t* pairs;
+  int32_t n;
+} daris_copy;
+
 typedef struct daris_op {
   int32_t kind; /* DARIS_STEP_... : which member counts */
   int32_t reserved; /* 0 */
@@ -141,6 +244,12 @@ typedef struct daris_op {
     daris_append append;
     daris_attend attend;
     daris_matvec matvec;
+    daris_tree_append tree_append;
+    daris_tree_attend tree_attend;
+    daris_sample sample;
+    daris_accept accept;
+    daris_keep keep;
+    daris_copy copy;
   } u;
 } daris_op;
 

@@ -355,8 +355,9 @@ def daris_probe_cus(p, n_groups=2048, spin=2000):
 
 # ---- operators of a generation step (include/daris_ops.h) ------------------------------------------------------------------
 
-STEP_NORM, STEP_APPEND, STEP_ATTEND, STEP_MATVEC = range(4)
-PAGE_TOKENS, SCALE_TOKENS = 64, 16
+STEP_NORM, STEP_APPEND, STEP_ATTEND, STEP_MATVEC, STEP_TREE_APPEND, STEP_TREE_ATTEND, STEP_SAMPLE = range(7)
+STEP_ACCEPT, STEP_KEEP, STEP_COPY = range(8, 11)
+PAGE_TOKENS, SCALE_TOKENS, TREE_WORDS, SAMPLE_WORDS = 64, 16, 16, 1 << 20
 
 
 def _struct(name, *fields):
@@ -372,9 +373,19 @@ daris_attend = _struct("daris_attend", (daris_cache, "cache"), (_P, "q out row_s
                        (_I, "n_rows q_heads dtype window"), (_F, "scale"))
 daris_matvec = _struct("daris_matvec", (_P, "x x_scale w w_scale y"), (_L, "x_row w_row y_row"), (_I, "rows n k group dtype gate"))
 
+daris_tree_append = _struct("daris_tree_append", (daris_cache, "cache"), (_P, "k v q q_out turn row_start tree"), (_L, "kv_row kv_head q_row q_head qo_row qo_head"),
+                            (_I, "n_rows q_heads dtype turn_rows rot_dim pairs tree_words"))
+daris_tree_attend = _struct("daris_tree_attend", (daris_attend, "attend"), (_P, "tree"), (_I, "tree_words"))
+daris_sample = _struct("daris_sample", (_P, "logits temperature top_k top_p min_p random word chance"), (_L, "logits_row"), (_I, "rows n dtype"))
+daris_accept = _struct("daris_accept", (_P, "tree words answers row_start before path count word after"), (_I, "n_rows n_seqs tree_words"))
+daris_keep = _struct("daris_keep", (daris_cache, "cache"), (_P, "path count row_start"), (_I, "n_rows"))
+daris_copy = _struct("daris_copy", (daris_cache, "cache"), (_P, "pairs"), (_I, "n"))
+_KINDS = {STEP_NORM: "norm", STEP_APPEND: "append", STEP_ATTEND: "attend", STEP_MATVEC: "matvec", STEP_TREE_APPEND: "tree_append", STEP_TREE_ATTEND: "tree_attend",
+          STEP_SAMPLE: "sample", STEP_ACCEPT: "accept", STEP_KEEP: "keep", STEP_COPY: "copy"}
+
 
 class _step(C.Union):
-    _fields_ = [("norm", daris_norm), ("append", daris_append), ("attend", daris_attend), ("matvec", daris_matvec)]
+    _fields_ = [(name, globals()["daris_" + name]) for name in _KINDS.values()]
 
 
 class daris_op(C.Structure):
@@ -431,7 +442,7 @@ def _at(t):
 
 def _made(kind, value, *keep):
     op = daris_op(kind, 0)
-    setattr(op.u, ("norm", "append", "attend", "matvec")[kind], value)
+    setattr(op.u, _KINDS[kind], value)
     op.keep = keep      # the buffers live as long as their descriptor
     return op
 
@@ -484,8 +495,34 @@ def _rows(cache, name, t, row_start, heads=None):
     return t
 
 
-def make_append(cache, k, v, row_start=None, q=None, q_out=None, turn=None, rot_dim=0, pairs=False):
-    """Appends rows k, v [rows][heads][dim] to the cache, keys and q -> q_out turned by turn [positions][rot_dim] (see daris_append)."""
+def _tree(t, rows):
+    _tensor("tree", t, 2, ("int64", "uint64"))
+    _need(1 <= t.shape[1] <= TREE_WORDS, f"masks of {t.shape[1]} words, not 1 to {TREE_WORDS}")
+    return _dense("tree", t, (rows, t.shape[1]), ("int64", "uint64"))
+
+
+def tree_masks(parents, words=None):
+    """Masks [rows][words] (an int64 tensor of the CPU) of trees: parents[s][i] is the node of sequence s above node i, which lies in front of it, or -1 for
+    one that hangs on the cached tokens.  A node's mask has the bits of itself and of all nodes above it."""
+    import torch
+    most = max([len(p) for p in parents] + [1])
+    words = -(-most // 64) if words is None else words
+    _need(most <= 64 * words and 1 <= words <= TREE_WORDS, f"trees of up to {most} nodes in {words} words of 64, {TREE_WORDS} words at most")
+    out = np.zeros((sum(len(p) for p in parents), words), np.uint64)
+    at = 0
+    for s, p in enumerate(parents):
+        for i, above in enumerate(p):
+            _need(-1 <= above < i, f"node {i} of sequence {s} is below node {above}")
+            if above >= 0:
+                out[at + i] = out[at + above]
+            out[at + i, i // 64] |= np.uint64(1 << (i % 64))
+        at += len(p)
+    return torch.from_numpy(out.view(np.int64))
+
+
+def make_append(cache, k, v, row_start=None, q=None, q_out=None, turn=None, rot_dim=0, pairs=False, tree=None):
+    """Appends rows k, v [rows][heads][dim] to the cache, keys and q -> q_out turned by turn [positions][rot_dim] (see daris_append); tree: masks
+    [rows][words] of rows that are nodes of trees (see daris_tree_append)."""
     _rows(cache, "k", k, row_start, cache.kv_heads)
     _like("v", _rows(cache, "v", v, row_start, cache.kv_heads), k)
     _need(v.shape[0] == k.shape[0], f"{v.shape[0]} rows of v, {k.shape[0]} of k")
@@ -499,15 +536,72 @@ def make_append(cache, k, v, row_start=None, q=None, q_out=None, turn=None, rot_
     z = (0, 0, 0)
     a = daris_append(cache, _at(k), _at(v), _at(q), _at(q_out), _at(turn), _at(row_start), *k.stride()[:2], *v.stride()[:2], *(q.stride() if q is not None else z)[:2],
                      *(q_out.stride() if q is not None else z)[:2], k.shape[0], q.shape[1] if q is not None else 0, _dtype(k), turn.shape[0] if turn is not None else 0, rot_dim, int(pairs))
-    return _made(STEP_APPEND, a, cache, k, v, q, q_out, turn, row_start)
+    if tree is None:
+        return _made(STEP_APPEND, a, cache, k, v, q, q_out, turn, row_start)
+    _tree(tree, k.shape[0])
+    _need(k.stride()[:2] == v.stride()[:2], f"with a tree, k and v lie alike: their distances are {k.stride()[:2]} and {v.stride()[:2]}")
+    t = daris_tree_append(cache, a.k, a.v, a.q, a.q_out, a.turn, a.row_start, _at(tree), a.k_row, a.k_head, a.q_row, a.q_head, a.qo_row, a.qo_head,
+                          a.n_rows, a.q_heads, a.dtype, a.turn_rows, a.rot_dim, a.pairs, tree.shape[1])
+    return _made(STEP_TREE_APPEND, t, cache, k, v, q, q_out, turn, row_start, tree)
 
 
-def make_attend(cache, q, out, row_start=None, scale=1.0, window=0):
-    """out = attention of q [rows][heads][dim] over the cache (see daris_attend)."""
+def make_attend(cache, q, out, row_start=None, scale=1.0, window=0, tree=None):
+    """out = attention of q [rows][heads][dim] over the cache (see daris_attend); tree: masks [rows][words] of rows that are nodes of trees (see daris_tree_attend)."""
     _rows(cache, "q", q, row_start)
     _need(_like("out", _rows(cache, "out", out, row_start, q.shape[1]), q).shape[0] == q.shape[0], f"{out.shape[0]} rows of out, {q.shape[0]} of q")
     a = daris_attend(cache, _at(q), _at(out), _at(row_start), *q.stride()[:2], *out.stride()[:2], q.shape[0], q.shape[1], _dtype(q), window, scale)
-    return _made(STEP_ATTEND, a, cache, q, out, row_start)
+    if tree is None:
+        return _made(STEP_ATTEND, a, cache, q, out, row_start)
+    _tree(tree, q.shape[0])
+    return _made(STEP_TREE_ATTEND, daris_tree_attend(a, _at(tree), tree.shape[1]), cache, q, out, row_start, tree)
+
+
+def make_sample(logits, word, random=None, temperature=None, top_k=None, top_p=None, min_p=None, chance=None):
+    """word [rows] (int32) drawn from logits [rows][n] by random [rows] (see daris_sample); temperature, top_p, min_p, chance [rows] of float32, top_k of int32."""
+    _tensor("logits", logits, 2, _ACT)
+    rows, n = logits.shape
+    _dense("word", word, (rows,), ("int32",))
+    for name, t in (("random", random), ("temperature", temperature), ("top_p", top_p), ("min_p", min_p), ("chance", chance)):
+        if t is not None:
+            _dense(name, t, (rows,), ("float32",))
+    if top_k is not None:
+        _dense("top_k", top_k, (rows,), ("int32",))
+    a = daris_sample(_at(logits), _at(temperature), _at(top_k), _at(top_p), _at(min_p), _at(random), _at(word), _at(chance), logits.stride(0), rows, n, _dtype(logits))
+    return _made(STEP_SAMPLE, a, logits, word, random, temperature, top_k, top_p, min_p, chance)
+
+
+def make_accept(tree, words, answers, path, count, word, row_start=None, before=None, after=None):
+    """Walks down the trees of masks tree [rows][words]: path [rows], count and word [sequences] from words and answers [rows], all int32 (see daris_accept);
+    after = before + count [sequences]."""
+    rows = _tensor("words", words, 1, ("int32",)).shape[0]
+    _dense("words", words, (rows,), ("int32",))
+    _tree(tree, rows)
+    _dense("answers", answers, (rows,), ("int32",))
+    _dense("path", path, (rows,), ("int32",))
+    seqs = _tensor("count", count, 1, ("int32",)).shape[0]
+    _dense("count", count, (seqs,), ("int32",))
+    for name, t in (("word", word), ("before", before), ("after", after)):
+        if t is not None or name == "word":
+            _dense(name, t, (seqs,), ("int32",))
+    if row_start is not None:
+        _dense("row_start", row_start, (seqs + 1,), ("int32",))
+    a = daris_accept(_at(tree), _at(words), _at(answers), _at(row_start), _at(before), _at(path), _at(count), _at(word), _at(after), rows, seqs, tree.shape[1])
+    return _made(STEP_ACCEPT, a, tree, words, answers, path, count, word, row_start, before, after)
+
+
+def make_keep(cache, path, count, row_start=None):
+    """Keeps the tokens of the nodes path [rows] (count [sequences] of each sequence), int32, one behind the other in the cache (see daris_keep)."""
+    _dense("path", path, (_tensor("path", path, 1, ("int32",)).shape[0],), ("int32",))
+    _dense("count", count, (cache.n_seqs,), ("int32",))
+    if row_start is not None:
+        _dense("row_start", row_start, (cache.n_seqs + 1,), ("int32",))
+    return _made(STEP_KEEP, daris_keep(cache, _at(path), _at(count), _at(row_start), path.shape[0]), cache, path, count, row_start)
+
+
+def make_copy(cache, pairs):
+    """Copies pages pairs[i][0] of the cache over pages pairs[i][1], pairs [n][2] of int32 (see daris_copy)."""
+    _dense("pairs", pairs, (_tensor("pairs", pairs, 2, ("int32",)).shape[0], 2), ("int32",))
+    return _made(STEP_COPY, daris_copy(cache, _at(pairs), pairs.shape[0]), cache, pairs)
 
 
 def make_matvec(x, w, w_scale, y, x_scale=None, gate=False):

@@ -13,7 +13,7 @@ DEVICE_SOURCES = {"kernels.hip": "daris_kernels", "taps_kernels.hip": "daris_tap
 # ... of the kernels that compute several layers in a row
 JOINED_SOURCES = {"joined_kernels.hip": "daris_joined_kernels", "tall_kernels.hip": "daris_tall_kernels", "pointwise_kernels.hip": "daris_pointwise_kernels"}
 # ... of the operators of a generation step
-STEP_SOURCES = {"step_kernels.hip": "daris_step_kernels", "attend_kernels.hip": "daris_attend_kernels"}
+STEP_SOURCES = {"step_kernels.hip": "daris_step_kernels", "attend_kernels.hip": "daris_attend_kernels", "draft_kernels.hip": "daris_draft_kernels"}
 HOST_SOURCES = ["aql.cpp", "launch.cpp", "sched_core.cpp", "net_plan.cpp", "net_encode.cpp", "daris_api.cpp"]
 COMMON = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-Wall", "-Wno-unused-function"]
 # no packed fp32 arithmetic in device code (some forms have given wrong results on this hardware)

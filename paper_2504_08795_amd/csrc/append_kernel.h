@@ -58,14 +58,26 @@ __device__ __forceinline__ uint32_t shrunk(uint32_t codes, float shrink) {
   return codes4(lo.x * shrink, lo.y * shrink, hi.x * shrink, hi.y * shrink);
 }
 
-template <bool BF16, int D>
-__device__ __forceinline__ void append_sixteenth(const AppendArgs& a, int head, int row0, int page, int part, int lo, int hi, int pos0) {
-  // tokens lo .. hi - 1 of the sixteenth are rows row0 ... at positions pos0 ... of the step
+// Position of a row in its sequence: `at` where rows follow each other; of a node that of the first new token and the nodes above it.
+template <bool TREE>
+__device__ __forceinline__ int position_of(const TreeMasks& tree, int row, int before, int at) {
+  if (!TREE) return at;
+  const uint64_t* mask = tree.mask + (int64_t)row * tree.words;
+  int n = -1;
+  for (int w = 0; w < tree.words; ++w) n += __popcll(mask[w]);
+  return before + n;
+}
+
+template <bool BF16, int D, bool TREE>
+__device__ __forceinline__ void append_sixteenth(const AppendArgs& a, const TreeMasks& tree, int head, int row0, int page, int part, int lo, int hi, int pos0, int before) {
+  // tokens lo .. hi - 1 of the sixteenth are rows row0 ... of the step, their places pos0 ... of the sequence
   constexpr int E = D / 64, Q = 4;  // channels of a lane; tokens that are read together
   const int lane = threadIdx.x & 63;
   const int64_t ph = (int64_t)page * a.c.kv_heads + head;
   const int had_k = lo > 0 ? a.c.k_scale[ph * 4 + part] : kLeastScale, had_v = lo > 0 ? a.c.v_scale[ph * 4 + part] : kLeastScale;
 
+  const int mine = lane < lo ? lo : lane < hi ? lane : hi - 1;  // (TREE: lane i has the position of token i)
+  const int position = position_of<TREE>(tree, row0 + mine - lo, before, 0);
   float xv[kScaleTokens][E];
   {  // ---- keys
     Turn t[E];
@@ -92,7 +104,7 @@ __device__ __forceinline__ void append_sixteenth(const AppendArgs& a, int head, 
           xv[tok][e] = load_elem<BF16>(a.v, vr + lane + 64 * e);
           c[i][e] = 1.f;
           s[i][e] = 0.f;
-          if (a.rot_dim) table_entry(a, t[e], pos0 + in - lo, &c[i][e], &s[i][e]);
+          if (a.rot_dim) table_entry(a, t[e], TREE ? __builtin_amdgcn_readlane(position, in) : pos0 + in - lo, &c[i][e], &s[i][e]);
         }
       }
 #pragma unroll
@@ -205,9 +217,9 @@ __device__ __forceinline__ int sequence_at(const CacheArgs& c, int at) {
   return found > 0 ? found - 1 : 0;
 }
 
-// Waves: first a.items sixteenths x key heads, then a.q_items groups of query heads.
-template <bool BF16, int D>
-__device__ __forceinline__ void append_body(const AppendArgs& a) {
+// Waves: first a.items sixteenths x key heads, then a.q_items groups of query heads.  TREE: rows are nodes of trees.
+template <bool BF16, int D, bool TREE = false>
+__device__ __forceinline__ void append_body(const AppendArgs& a, const TreeMasks& tree = {}) {
   const int wave = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (wave < a.items) {
     const int item = wave / a.c.kv_heads, head = wave - item * a.c.kv_heads;
@@ -228,7 +240,7 @@ __device__ __forceinline__ void append_body(const AppendArgs& a) {
     const int page = page_of(a.c, s, (int)(t0 / kPage));
     if (page < 0) return;
     const int tok = (int)t0 + lo;
-    append_sixteenth<BF16, D>(a, head, row0 + (tok - before), page, (int)(sixteenth % (kPage / kScaleTokens)), lo, hi, tok);
+    append_sixteenth<BF16, D, TREE>(a, tree, head, row0 + (tok - before), page, (int)(sixteenth % (kPage / kScaleTokens)), lo, hi, tok, before);
   } else if (wave < a.items + a.q_items) {
     const int per_row = (a.q_heads + kTurnHeads - 1) / kTurnHeads;
     const int i = wave - a.items, row = i / per_row, head = (i - row * per_row) * kTurnHeads;
@@ -237,7 +249,8 @@ __device__ __forceinline__ void append_body(const AppendArgs& a) {
       s = sequence_at<1, 0>(a.c, row);
       if (row < first_row(a.c, s) || row >= first_row(a.c, s + 1)) return;
     }
-    turn_queries<BF16, D>(a, row, head, tokens_before(a.c, s) + (row - first_row(a.c, s)));
+    const int before = tokens_before(a.c, s);
+    turn_queries<BF16, D>(a, row, head, position_of<TREE>(tree, row, before, before + (row - first_row(a.c, s))));
   }
 }
 

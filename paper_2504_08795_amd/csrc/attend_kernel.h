@@ -39,10 +39,11 @@ struct Unit {
   int row0 = 0, rows = 0, before = 0;
 };
 
-// Pages that any row of sequence s sees: [*lo, return value).
+// Pages that any row of sequence s sees: [*lo, return value).  (A row of a tree may see one cached token more than its window: none of its nodes.)
+template <bool TREE>
 __device__ __forceinline__ int seen_pages(const AttendArgs& a, int rows, int before, int* lo) {
   const int end = before + rows;
-  int from = a.window > 0 && before >= a.window ? before - a.window + 1 : 0;
+  int from = a.window > 0 && before >= a.window ? before - a.window + (TREE ? 0 : 1) : 0;
   from /= kPage;
   *lo = from;
   if (end <= 0 || rows == 0) return from;
@@ -53,7 +54,7 @@ __device__ __forceinline__ int seen_pages(const AttendArgs& a, int rows, int bef
 
 // Every wave finds the workgroup's unit by itself, 64 * SETS sequences at a time (a token for 200 streams of 500, 8 query and 4 key heads of 128: 37 us a call, 44 when
 // sets of 64 came one after the other).  False: nothing to do.
-template <int TILE, int MOST, int SETS>
+template <int TILE, int MOST, int SETS, bool TREE>
 __device__ __forceinline__ bool find_among(const AttendArgs& a, int unit, Unit* u) {
   const int lane = threadIdx.x & 63, ns = a.c.n_seqs;
   int row0[SETS], rows[SETS], before[SETS], tiles[SETS], pages[SETS];
@@ -69,7 +70,7 @@ __device__ __forceinline__ bool find_among(const AttendArgs& a, int unit, Unit* 
     for (int i = 0; i < SETS; ++i) {
       tiles[i] = (int)(((int64_t)rows[i] * a.group + TILE - 1) / TILE);
       int lo;
-      pages[i] = seen_pages(a, rows[i], before[i], &lo);
+      pages[i] = seen_pages<TREE>(a, rows[i], before[i], &lo);
       pages[i] -= lo;
     }
   };
@@ -144,9 +145,9 @@ __device__ __forceinline__ bool find_among(const AttendArgs& a, int unit, Unit* 
   }
   return false;
 }
-template <int TILE, int MOST>
+template <int TILE, int MOST, bool TREE>
 __device__ __forceinline__ bool find_unit(const AttendArgs& a, int unit, Unit* u) {
-  return a.c.n_seqs <= 64 ? find_among<TILE, MOST, 1>(a, unit, u) : find_among<TILE, MOST, 4>(a, unit, u);
+  return a.c.n_seqs <= 64 ? find_among<TILE, MOST, 1, TREE>(a, unit, u) : find_among<TILE, MOST, 4, TREE>(a, unit, u);
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -169,8 +170,60 @@ __device__ __forceinline__ uint4 seen(uint4 x, int t1, int lo, int hi) {
                     x.w & bytes_below(b - 12) & ~bytes_below(a - 12));
 }
 
-// One wave's columns, TILE = 16 or 32 of them, and its running sums.
-template <bool BF16, int D, int TILE>
+// The lowest n of sixteen bits.
+__device__ __forceinline__ uint32_t bits_below(int n) { return n >= 16 ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+
+// What the row of a column sees where the step's rows are nodes of a tree: cached tokens from `from` on, and the nodes of its mask from `least` on.
+struct Sight {
+  const uint64_t* mask;
+  int before, nodes, words, from, least;
+  // row: its number among all rows.  A window leaves the last tokens of those that it sees.
+  __device__ __forceinline__ void start(const AttendArgs& a, const TreeMasks& tree, const Unit& u, int row) {
+    mask = tree.mask + (int64_t)row * tree.words;
+    before = u.before;
+    words = tree.words;
+    nodes = u.rows < 64 * words ? u.rows : 64 * words;
+    from = least = 0;
+    if (a.window <= 0) return;
+    auto word = [&](int w) {
+      const int left = nodes - 64 * w;
+      return mask[w] & (left >= 64 ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1);
+    };
+    int over = -a.window;
+    for (int w = 0; w < words; ++w) over += __popcll(word(w));
+    from = before + over;
+    for (int w = 0; w < words && over > 0; ++w) {
+      uint64_t m = word(w);
+      if (const int n = __popcll(m); over >= n) {
+        over -= n;
+        least = 64 * w + 64;
+      } else {
+        for (; over > 0; --over) m &= m - 1;
+        least = 64 * w + __builtin_ctzll(m);
+      }
+    }
+  }
+  // ... of tokens t1 .. t1 + 15, a bit each
+  __device__ __forceinline__ uint32_t bits(int t1) const {
+    uint32_t seen = bits_below(before - t1) & ~bits_below(from - t1);
+    const int node = t1 - before;  // the token t1 is this node
+    if (node > -16 && node < nodes) {
+      const int w = node < 0 ? 0 : node >> 6, shift = node & 63;
+      uint64_t m = mask[w];
+      if (node < 0) {
+        m <<= -node;
+      } else {
+        m >>= shift;
+        if (shift > 48 && w + 1 < words) m |= mask[w + 1] << (64 - shift);
+      }
+      seen |= (uint32_t)m & bits_below(nodes - node) & ~bits_below(least - node);
+    }
+    return seen;
+  }
+};
+
+// One wave's columns, TILE = 16 or 32 of them, and its running sums.  TREE: the step's rows are nodes of trees.
+template <bool BF16, int D, int TILE, bool TREE = false>
 struct Columns {
   static constexpr int PARTS = BF16 ? 1 : 2;
   // Pages that all columns see have a form of their own where its registers leave two waves on a SIMD (64 streams, bf16, heads of 128: 83.0 us a call, 85.7
@@ -198,19 +251,21 @@ struct Columns {
   float top, sum;   // M; the lane's share of the sum of weights
   float factor;     // of a score: scale * log2(e) / the queries' power of two
   int pos;          // position of the column's row
+  Sight sight;      // (TREE: in its place)
   bool nans;        // there were NaN codes among the values of a masked page
   int lane;
   __device__ __forceinline__ int c() const { return lane & (TILE - 1); }  // column of the lane, and which of the column's lanes it is
   __device__ __forceinline__ int g() const { return lane / TILE; }
 
   // columns col0 .. of `rows` rows; those behind the last repeat it and are not stored
-  __device__ __forceinline__ void start(const AttendArgs& a, const Unit& u, int head, int col0) {
+  __device__ __forceinline__ void start(const AttendArgs& a, const TreeMasks& tree, const Unit& u, int head, int col0) {
     lane = threadIdx.x & 63;
     const int c = this->c(), g = this->g();
     const int cols = u.rows * a.group;
     const int col = col0 + c < cols ? col0 + c : cols - 1;
     const int r = col / a.group;
-    pos = u.before + r;
+    if constexpr (TREE) sight.start(a, tree, u, u.row0 + r);
+    else pos = u.before + r;
     const int64_t at = (int64_t)(u.row0 + r) * a.q_row + (int64_t)(head * a.group + (col - r * a.group)) * a.q_head + g * (D / G);
     constexpr int W = BF16 ? 1 : 2;  // 16-byte vectors of eight channels
     uint4 raw[KS][W];
@@ -334,12 +389,17 @@ struct Columns {
     // tokens of its sixteenths that the column sees
     struct {
       int from[HALVES], to[HALVES];
+      uint32_t bits[HALVES];
     } sees;
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) {
       const int t1 = t0 + sixteenth(h) * 16;
-      sees.to[h] = pos + 1 - t1;
-      sees.from[h] = a.window > 0 ? sees.to[h] - a.window : -(1 << 30);
+      if constexpr (TREE) {
+        sees.bits[h] = MASKED ? sight.bits(t1) : 0u;
+      } else {
+        sees.to[h] = pos + 1 - t1;
+        sees.from[h] = a.window > 0 ? sees.to[h] - a.window : -(1 << 30);
+      }
     }
     uint32_t found = 0;
     Acc s[KT];
@@ -394,7 +454,7 @@ struct Columns {
       for (int e = 0; e < 16; ++e) {
         float x = s[h * PER + e / R][e % R];
         if (MASKED) {
-          x = e >= sees.from[h] && e < sees.to[h] ? x : -INFINITY;
+          x = (TREE ? (sees.bits[h] >> e & 1) != 0 : e >= sees.from[h] && e < sees.to[h]) ? x : -INFINITY;
           s[h * PER + e / R][e % R] = x;
         }
         m = fmaxf(m, x);
@@ -486,10 +546,17 @@ struct Columns {
       const uint8_t* v = a.c.v + ((int64_t)page * a.c.kv_heads + head) * (kPage * D) + c() * kPage;
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) {
-        const int t1 = t0 + sixteenth(h) * 16, to = pos + 1 - t1, from = a.window > 0 ? to - a.window : -(1 << 30);
+        const int t1 = t0 + sixteenth(h) * 16;
         f16x8 see[2];
+        if constexpr (TREE) {
+          const uint32_t bits = sight.bits(t1);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) see[e >> 3][e & 7] = e >= from && e < to ? (_Float16)1.f : (_Float16)0.f;
+          for (int e = 0; e < 16; ++e) see[e >> 3][e & 7] = bits >> e & 1 ? (_Float16)1.f : (_Float16)0.f;
+        } else {
+          const int to = pos + 1 - t1, from = a.window > 0 ? to - a.window : -(1 << 30);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) see[e >> 3][e & 7] = e >= from && e < to ? (_Float16)1.f : (_Float16)0.f;
+        }
 #pragma unroll
         for (int t = 0; t < VT; ++t) {
           __builtin_amdgcn_sched_barrier(0);
@@ -651,8 +718,8 @@ __device__ __forceinline__ void merge(const AttendArgs& a, int head, const Unit&
 }
 
 // Four waves on the pages of one 16-column tile, every fourth each.
-template <bool BF16, int D>
-__device__ __forceinline__ void attend_narrow_body(const AttendArgs& a) {
+template <bool BF16, int D, bool TREE = false>
+__device__ __forceinline__ void attend_narrow_body(const AttendArgs& a, const TreeMasks& tree = {}) {
   constexpr int COLS = 16, MOST = kNarrowUnits, PITCH = D + 4;
   extern __shared__ float4 smem4[];
   float* lds = (float*)smem4;  // [4][16][PITCH] numbers, [4][16] M, [4][16] sums of weights, a flag; the merge takes the numbers' place
@@ -661,12 +728,13 @@ __device__ __forceinline__ void attend_narrow_body(const AttendArgs& a) {
   int* flag = (int*)(sums + 4 * COLS);
   const int head = blockIdx.x % a.c.kv_heads, tid = threadIdx.x, wave = uniform(tid >> 6);
   Unit u;
-  if (!find_unit<COLS, MOST>(a, blockIdx.x / a.c.kv_heads, &u)) return;
+  if (!find_unit<COLS, MOST, TREE>(a, blockIdx.x / a.c.kv_heads, &u)) return;
   const int col0 = u.tile * COLS, cols = u.rows * a.group - col0 < COLS ? u.rows * a.group - col0 : COLS;
-  const int pos_lo = u.before + col0 / a.group, pos_hi = u.before + (col0 + cols - 1) / a.group;
-  Columns<BF16, D, COLS> w;
-  w.start(a, u, head, col0);
-  int lo, hi = seen_pages(a, u.rows, u.before, &lo);
+  // (of a tree: all columns see the cached tokens, and each may see any of the nodes)
+  const int pos_lo = TREE ? u.before - 1 : u.before + col0 / a.group, pos_hi = TREE ? u.before + u.rows - 1 : u.before + (col0 + cols - 1) / a.group;
+  Columns<BF16, D, COLS, TREE> w;
+  w.start(a, tree, u, head, col0);
+  int lo, hi = seen_pages<TREE>(a, u.rows, u.before, &lo);
   lo += u.chunk * u.per;
   hi = hi < lo + u.per ? hi : lo + u.per;
   const int end = pos_hi < 0 ? 0 : pos_hi / kPage + 1;
@@ -754,30 +822,30 @@ struct SharedPage {
 // Four waves side by side on 32 columns each.  They share the pages: each fetches a quarter of the next one in whole cache lines while
 // the present one is used from LDS, and spreads it to f16 once for all (a wave's operands straight from memory are 32 rows a load, 64 cycles of the CU's address
 // unit: 4096 a page for the four, of 1024 for the matrix instructions).
-template <bool BF16, int D>
-__device__ __forceinline__ void attend_wide_body(const AttendArgs& a) {
+template <bool BF16, int D, bool TREE = false>
+__device__ __forceinline__ void attend_wide_body(const AttendArgs& a, const TreeMasks& tree = {}) {
   constexpr int COLS = 128, MOST = kWideUnits, PIECES = SharedPage<D>::PIECES, EACH = kPage * D / 16 / 256 * 2;  // 16-byte pieces of a page that a thread fetches
   extern __shared__ uint4 smem_pages[];
   float* lds = (float*)smem_pages;  // two pages; later for the merge [2][MOST][128]; a flag
   int* flag = (int*)(lds + wide_numbers(D));
   const int head = blockIdx.x % a.c.kv_heads, wave = uniform(threadIdx.x >> 6);
   Unit u;
-  if (!find_unit<COLS, MOST>(a, blockIdx.x / a.c.kv_heads, &u)) return;
+  if (!find_unit<COLS, MOST, TREE>(a, blockIdx.x / a.c.kv_heads, &u)) return;
   const int all = u.rows * a.group, col0 = u.tile * COLS, mine0 = col0 + wave * 32;
   const int tile_cols = all - col0 < COLS ? all - col0 : COLS, cols = all - mine0 < 32 ? all - mine0 : 32;  // (cols may be none)
   // pages of the workgroup, and of the wave
-  int lo, hi = seen_pages(a, u.rows, u.before, &lo);
+  int lo, hi = seen_pages<TREE>(a, u.rows, u.before, &lo);
   lo += u.chunk * u.per;
   hi = hi < lo + u.per ? hi : lo + u.per;
-  const int tile_lo = u.before + col0 / a.group, tile_hi = u.before + (col0 + tile_cols - 1) / a.group;
+  const int tile_lo = TREE ? u.before - 1 : u.before + col0 / a.group, tile_hi = TREE ? u.before + u.rows - 1 : u.before + (col0 + tile_cols - 1) / a.group;
   const int end = tile_hi < 0 ? 0 : tile_hi / kPage + 1, from = a.window > 0 && tile_lo >= a.window ? (tile_lo - a.window + 1) / kPage : 0;
   hi = hi < end ? hi : end;
   lo = lo > from ? lo : from;
-  const int pos_lo = u.before + mine0 / a.group, pos_hi = cols > 0 ? u.before + (mine0 + cols - 1) / a.group : -1;
+  const int pos_lo = TREE ? tile_lo : u.before + mine0 / a.group, pos_hi = cols > 0 ? (TREE ? tile_hi : u.before + (mine0 + cols - 1) / a.group) : -1;
   const int see_lo = a.window > 0 ? pos_lo - a.window + 1 : 0;
 
-  Columns<BF16, D, 32> w;
-  w.start(a, u, head, cols > 0 ? mine0 : col0);
+  Columns<BF16, D, 32, TREE> w;
+  w.start(a, tree, u, head, cols > 0 ? mine0 : col0);
 
   u32x4 next[EACH];
   uint32_t next_ks = 0, next_vs = 0;

@@ -53,11 +53,13 @@ extern "C" const char daris_tall_kernels_co[];
 extern "C" const char daris_tall_kernels_co_end[];
 extern "C" const char daris_point_kernels_co[];
 extern "C" const char daris_point_kernels_co_end[];
-// ... and those of the operators of a generation step (step_kernels.hip, attend_kernels.hip)
+// ... and those of the operators of a generation step (step_kernels.hip, attend_kernels.hip, draft_kernels.hip)
 extern "C" const char daris_step_kernels_co[];
 extern "C" const char daris_step_kernels_co_end[];
 extern "C" const char daris_attend_kernels_co[];
 extern "C" const char daris_attend_kernels_co_end[];
+extern "C" const char daris_draft_kernels_co[];
+extern "C" const char daris_draft_kernels_co_end[];
 
 namespace {
 
@@ -787,7 +789,8 @@ daris_status daris_init(int device, uint64_t seed, int flags) {
                                {daris_tall_kernels_co, (size_t)(daris_tall_kernels_co_end - daris_tall_kernels_co)},
                                {daris_point_kernels_co, (size_t)(daris_point_kernels_co_end - daris_point_kernels_co)},
                                {daris_step_kernels_co, (size_t)(daris_step_kernels_co_end - daris_step_kernels_co)},
-                               {daris_attend_kernels_co, (size_t)(daris_attend_kernels_co_end - daris_attend_kernels_co)}});
+                               {daris_attend_kernels_co, (size_t)(daris_attend_kernels_co_end - daris_attend_kernels_co)},
+                               {daris_draft_kernels_co, (size_t)(daris_draft_kernels_co_end - daris_draft_kernels_co)}});
       if (err.empty()) {
         err = g_kt.resolve(g_rt);
         if (err.empty()) err = g_joined.resolve(g_rt);

@@ -31,6 +31,12 @@ struct CacheArgs {
   int n_pages, n_seqs, kv_heads, n_rows;
 };
 
+// Masks of the step's rows, where these are nodes of trees: [n_rows][words].
+struct TreeMasks {
+  const uint64_t* mask;
+  int words;
+};
+
 struct AppendArgs {
   CacheArgs c;
   const void* k;
@@ -43,6 +49,10 @@ struct AppendArgs {
   int items, q_items;  // sixteenths x key heads at most; (row, kTurnHeads query heads)
 };
 constexpr int kTurnHeads = 4;
+struct TreeAppendArgs {
+  AppendArgs append;
+  TreeMasks tree;
+};
 
 struct AttendArgs {
   CacheArgs c;
@@ -58,6 +68,10 @@ struct AttendArgs {
   int round;        // workgroups of a key head that have a CU each
   float scale;      // times log2(e)
   int q_vec, out_vec;  // rows of q are 16-byte vectors; four channels of out are one vector
+};
+struct TreeAttendArgs {
+  AttendArgs attend;
+  TreeMasks tree;
 };
 
 constexpr int kNarrowColumns = 16, kWideColumns = 128;  // columns (query heads of a row) of a unit
@@ -99,5 +113,51 @@ struct MatvecArgs {
   int eights;  // log2 of the pieces of scales that a tile's row has in a chunk, rounded up
   int pitch;   // matvec_pitch of a chunk
 };
+
+struct SampleArgs {
+  const void* logits;
+  const float* temperature;  // null: 1
+  const float* top_p;        // null: all, as the next two
+  const float* min_p;
+  const int32_t* top_k;
+  const float* random;       // null: the largest
+  int32_t* word;
+  float* chance;             // may be null
+  int64_t row;
+  int rows, n;
+  int vec;     // rows are 16-byte vectors
+  int chunks;  // of kSampleChunk numbers
+};
+constexpr int kSampleChunk = 512, kSampleMost = 1 << 20;  // numbers that a wave reads at once; of a row, at most
+constexpr int kSampleWaves = 16, kSampleSteps = 4096, kSampleFew = 1024;
+constexpr int kSampleLds = kSampleMost / kSampleChunk * 12 + kSampleSteps * 12 + kSampleFew * 8 + kSampleWaves * 20 + 24;
+
+struct AcceptArgs {
+  const uint64_t* tree;
+  const int32_t* words;
+  const int32_t* answers;
+  const int32_t* row_start;
+  const int32_t* before;
+  int32_t* path;
+  int32_t* count;
+  int32_t* word;
+  int32_t* after;  // may be null
+  int n_rows, n_seqs, tree_words;
+};
+constexpr int kTreeWords = 16, kTreeNodes = 64 * kTreeWords;  // of a row's mask, at most
+
+struct KeepArgs {
+  CacheArgs c;
+  const int32_t* path;
+  const int32_t* count;
+};
+
+struct CopyArgs {
+  CacheArgs c;
+  const int32_t* pairs;
+  int n;
+  int pieces;  // of kCopyPiece bytes in a page's keys; as many in its values
+};
+constexpr int kCopyPiece = 16384;
 
 }  // namespace daris

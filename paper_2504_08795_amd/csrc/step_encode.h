@@ -31,6 +31,14 @@ struct StepTable {
   const AqlKernel* narrow[2][3] = {};
   const AqlKernel* wide[2][3] = {};        // (none of 256)
   const AqlKernel* matvec[4][3] = {};      // [kMatvecTypes][group 32, 64, 128]
+  // ... where the step's rows are nodes of trees
+  const AqlKernel* tree_append[2][3] = {};
+  const AqlKernel* tree_narrow[2][3] = {};
+  const AqlKernel* tree_wide[2][3] = {};
+  const AqlKernel* sample[2] = {};  // [bf16]
+  const AqlKernel* accept = nullptr;
+  const AqlKernel* keep[3] = {};    // [dim 64, 128, 256]
+  const AqlKernel* copy[3] = {};
   std::string resolve(const AqlRuntime& rt);
 };
 
@@ -59,7 +67,16 @@ inline std::string StepTable::resolve(const AqlRuntime& rt) {
       append[b][d] = find("daris::step_append<%s, %d>", tf[b], 64 << d);
       narrow[b][d] = find("daris::step_attend_narrow<%s, %d>", tf[b], 64 << d);
       if (d < 2) wide[b][d] = find("daris::step_attend_wide<%s, %d>", tf[b], 64 << d);
+      tree_append[b][d] = find("daris::step_append_tree<%s, %d>", tf[b], 64 << d);
+      tree_narrow[b][d] = find("daris::step_attend_tree_narrow<%s, %d>", tf[b], 64 << d);
+      if (d < 2) tree_wide[b][d] = find("daris::step_attend_tree_wide<%s, %d>", tf[b], 64 << d);
     }
+    sample[b] = find("daris::step_sample<%s>", tf[b]);
+  }
+  accept = find("%s", "daris::step_accept");
+  for (int d = 0; d < 3; ++d) {
+    keep[d] = find("daris::step_keep<%d>", 64 << d);
+    copy[d] = find("daris::step_copy<%d>", 64 << d);
   }
   for (int t = 0; t < 4; ++t)
     for (int g = 0; g < 3; ++g) matvec[t][g] = find("daris::step_matvec<%d, %d, %s>", kMatvecTypes[t].rows, 32 << g, tf[kMatvecTypes[t].bf16]);
@@ -159,6 +176,81 @@ inline std::string check_matvec(const daris_matvec& o) {
   return "";
 }
 
+// Masks of n_rows rows.
+inline std::string check_tree(const uint64_t* tree, int words, int n_rows, int n_seqs) {
+  if (words < 1 || words > kTreeWords) return text("masks of %d words, not 1 to %d", words, kTreeWords);
+  if (n_rows == 0 || n_seqs == 0) return "";
+  if (!tree) return "no masks";
+  if (!aligned_to(tree, 8)) return "masks are not aligned to 8 bytes";
+  return "";
+}
+
+// The same operator without a tree.
+inline daris_append plain_append(const daris_tree_append& o) {
+  daris_append p = {};
+  p.cache = o.cache;
+  p.k = o.k; p.v = o.v; p.q = o.q; p.q_out = o.q_out; p.turn = o.turn; p.row_start = o.row_start;
+  p.k_row = p.v_row = o.kv_row; p.k_head = p.v_head = o.kv_head;
+  p.q_row = o.q_row; p.q_head = o.q_head; p.qo_row = o.qo_row; p.qo_head = o.qo_head;
+  p.n_rows = o.n_rows; p.q_heads = o.q_heads; p.dtype = o.dtype; p.turn_rows = o.turn_rows; p.rot_dim = o.rot_dim; p.pairs = o.pairs;
+  return p;
+}
+inline std::string check_tree_append(const daris_tree_append& o) {
+  const std::string e = check_append(plain_append(o));
+  return e.empty() ? check_tree(o.tree, o.tree_words, o.n_rows, o.cache.n_seqs) : e;
+}
+inline std::string check_tree_attend(const daris_tree_attend& o) {
+  const std::string e = check_attend(o.attend);
+  return e.empty() ? check_tree(o.tree, o.tree_words, o.attend.n_rows, o.attend.cache.n_seqs) : e;
+}
+
+inline std::string check_sample(const daris_sample& o) {
+  std::string e = check_dtype(o.dtype);
+  if (!e.empty()) return e;
+  if (o.rows < 0 || o.n < 1) return text("rows %d, n %d", o.rows, o.n);
+  if (o.rows > kMostRows || o.n > kSampleMost) return text("more than 2^30 rows or 2^20 words (%d, %d)", o.rows, o.n);
+  if (o.rows == 0) return "";
+  if (!o.logits || !o.word) return "NULL buffer";
+  if (!aligned_to(o.logits, o.dtype == DARIS_BF16 ? 2 : 4) || !aligned_to(o.temperature, 4) || !aligned_to(o.top_k, 4) || !aligned_to(o.top_p, 4) || !aligned_to(o.min_p, 4) ||
+      !aligned_to(o.random, 4) || !aligned_to(o.word, 4) || !aligned_to(o.chance, 4))
+    return "a buffer is not aligned to its elements";
+  return "";
+}
+
+inline std::string check_accept(const daris_accept& o) {
+  if (o.n_rows < 0 || o.n_seqs < 0) return "a negative count";
+  if (o.n_rows > kMostRows || o.n_seqs > kMostRows) return text("more than 2^30 rows or sequences (%d, %d)", o.n_rows, o.n_seqs);
+  const std::string e = check_tree(o.tree, o.tree_words, o.n_rows, o.n_seqs);
+  if (!e.empty() || o.n_seqs == 0) return e;
+  if (!o.row_start && o.n_rows != o.n_seqs) return text("%d rows for %d sequences without row_start", o.n_rows, o.n_seqs);
+  if ((o.n_rows && (!o.words || !o.answers || !o.path)) || !o.count || !o.word) return "NULL buffer";
+  if (o.after && !o.before) return "after without before";
+  if (!aligned_to(o.words, 4) || !aligned_to(o.answers, 4) || !aligned_to(o.row_start, 4) || !aligned_to(o.before, 4) || !aligned_to(o.path, 4) || !aligned_to(o.count, 4) || !aligned_to(o.word, 4) ||
+      !aligned_to(o.after, 4))
+    return "a buffer is not aligned to 4 bytes";
+  return "";
+}
+
+inline std::string check_keep(const daris_keep& o) {
+  const std::string e = check_cache(o.cache, o.n_rows, o.row_start);
+  if (!e.empty() || o.n_rows == 0 || o.cache.n_seqs == 0) return e;
+  if (!o.path || !o.count) return "NULL buffer";
+  if (!aligned_to(o.path, 4) || !aligned_to(o.count, 4)) return "a buffer is not aligned to 4 bytes";
+  return "";
+}
+
+inline std::string check_copy(const daris_copy& o) {
+  const daris_cache& c = o.cache;  // (of which only the pages count)
+  if (c.dim != 64 && c.dim != 128 && c.dim != 256) return text("dim %d is not 64, 128 or 256", c.dim);
+  if (c.kv_heads < 1 || c.n_pages < 0 || o.n < 0) return "a negative count, or no key head";
+  if (o.n > kMostRows) return text("more than 2^30 pages (%d)", o.n);
+  if (o.n == 0 || c.n_pages == 0) return "";
+  if (!c.k || !c.v || !c.k_scale || !c.v_scale || !o.pairs) return "NULL buffer";
+  if (!aligned_to(c.k, 16) || !aligned_to(c.v, 16)) return "k and v of the cache are not aligned to 16 bytes";
+  if (!aligned_to(c.k_scale, 4) || !aligned_to(c.v_scale, 4) || !aligned_to(o.pairs, 4)) return "a buffer is not aligned to 4 bytes";
+  return "";
+}
+
 // ---- launches -----------------------------------------------------------------------------------------------------------------
 
 template <typename A>
@@ -202,7 +294,7 @@ inline CacheArgs cache_args(const daris_cache& c, const int32_t* row_start, int 
 }
 inline int dim_index(int dim) { return dim == 64 ? 0 : dim == 128 ? 1 : 2; }
 
-inline std::string encode_append(const StepTable& t, const daris_append& o, StepLaunch* l) {
+inline std::string encode_append(const StepTable& t, const daris_append& o, StepLaunch* l, TreeMasks tree = {}) {
   AppendArgs a = {};
   a.c = cache_args(o.cache, o.row_start, o.n_rows);
   a.k = o.k; a.v = o.v; a.q = o.q; a.q_out = o.q_out; a.turn = o.turn;
@@ -214,11 +306,12 @@ inline std::string encode_append(const StepTable& t, const daris_append& o, Step
   if (items + q_items > 0x7fffffffll) return kTooMany;
   a.items = (int)items;
   a.q_items = (int)q_items;
-  set_args(l, a);
-  return set_grid(l, t.append[o.dtype == DARIS_BF16][dim_index(o.cache.dim)], (items + q_items + 3) / 4, 256, 0) ? "" : kTooMany;
+  if (tree.mask) set_args(l, TreeAppendArgs{a, tree});
+  else set_args(l, a);
+  return set_grid(l, (tree.mask ? t.tree_append : t.append)[o.dtype == DARIS_BF16][dim_index(o.cache.dim)], (items + q_items + 3) / 4, 256, 0) ? "" : kTooMany;
 }
 
-inline std::string encode_attend(const StepTable& t, const daris_attend& o, int n_cu, StepLaunch* l) {
+inline std::string encode_attend(const StepTable& t, const daris_attend& o, int n_cu, StepLaunch* l, TreeMasks tree = {}) {
   const int bf16 = o.dtype == DARIS_BF16, d = dim_index(o.cache.dim), vec = bf16 ? 8 : 4;
   AttendArgs a = {};
   a.c = cache_args(o.cache, o.row_start, o.n_rows);
@@ -235,7 +328,9 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   // 128: 16 x 24 (768) 41 and 43, 47 and 75; 8 x 64 (1024) 61 and 53, 71 and 100; 1 x 1024 (2048) 208 and 117, 240 and 243; 1 x 2048 444 and 203, 510 and 457; fp32's wide tiles have a CU for
   // themselves.  64 x 4 rows, which fill an eighth of wide tiles: 33 and 42.
   const int full = o.cache.dim == 64 ? 6 : bf16 ? 3 : 8;
-  const bool wide = columns * o.cache.dim >= 4096 * (int64_t)o.cache.n_seqs && columns * o.cache.kv_heads > (int64_t)full * kNarrowColumns * n_cu && t.wide[bf16][d];
+  const AqlKernel* const narrow_kernel = (tree.mask ? t.tree_narrow : t.narrow)[bf16][d];
+  const AqlKernel* const wide_kernel = (tree.mask ? t.tree_wide : t.wide)[bf16][d];
+  const bool wide = columns * o.cache.dim >= 4096 * (int64_t)o.cache.n_seqs && columns * o.cache.kv_heads > (int64_t)full * kNarrowColumns * n_cu && wide_kernel;
   const int cols = wide ? kWideColumns : kNarrowColumns;
   const int64_t tiles = columns / cols + o.cache.n_seqs;  // at most: each sequence's last one may be part of a tile
   // Two workgroups for each CU; wide tiles that are that many by themselves are not cut.  With one, two and four a CU, us a call: a token for 8 streams of 2000
@@ -255,8 +350,9 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   l->count_at = offsetof(AttendArgs, count);
   l->counters = a.target ? (size_t)units * o.cache.kv_heads : 0;
   l->part_bytes = a.target ? (size_t)(units * o.cache.kv_heads * unit_floats(cols, o.cache.dim)) * sizeof(float) : 0;
-  set_args(l, a);
-  return set_grid(l, wide ? t.wide[bf16][d] : t.narrow[bf16][d], units * o.cache.kv_heads, 256, wide ? wide_lds(o.cache.dim) : narrow_lds(o.cache.dim)) ? "" : kTooMany;
+  if (tree.mask) set_args(l, TreeAttendArgs{a, tree});
+  else set_args(l, a);
+  return set_grid(l, wide ? wide_kernel : narrow_kernel, units * o.cache.kv_heads, 256, wide ? wide_lds(o.cache.dim) : narrow_lds(o.cache.dim)) ? "" : kTooMany;
 }
 
 inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int n_cu, StepLaunch* l) {
@@ -334,6 +430,50 @@ inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int 
   return set_grid(l, t.matvec[type][g], (int64_t)a.wgs * blocks * a.shares, waves * 64, lds(a.steps, 1 << a.across, a.share_steps)) ? "" : kTooMany;
 }
 
+inline std::string encode_sample(const StepTable& t, const daris_sample& o, StepLaunch* l) {
+  const int bf16 = o.dtype == DARIS_BF16, vec = bf16 ? 8 : 4;
+  SampleArgs a = {};
+  a.logits = o.logits; a.temperature = o.temperature; a.top_p = o.top_p; a.min_p = o.min_p; a.top_k = o.top_k;
+  a.random = o.random; a.word = o.word; a.chance = o.chance;
+  a.row = o.logits_row;
+  a.rows = o.rows; a.n = o.n;
+  a.vec = aligned_to(o.logits, 16) && (o.rows == 1 || o.logits_row % vec == 0);
+  a.chunks = (o.n + kSampleChunk - 1) / kSampleChunk;
+  set_args(l, a);
+  return set_grid(l, t.sample[bf16], o.rows, kSampleWaves * 64, kSampleLds) ? "" : kTooMany;
+}
+
+inline std::string encode_accept(const StepTable& t, const daris_accept& o, StepLaunch* l) {
+  AcceptArgs a = {};
+  a.tree = o.tree; a.words = o.words; a.answers = o.answers; a.row_start = o.row_start; a.before = o.before;
+  a.path = o.path; a.count = o.count; a.word = o.word; a.after = o.after;
+  a.n_rows = o.n_rows; a.n_seqs = o.n_seqs; a.tree_words = o.tree_words;
+  set_args(l, a);
+  return set_grid(l, t.accept, o.n_seqs, 64, 0) ? "" : kTooMany;
+}
+
+inline std::string encode_keep(const StepTable& t, const daris_keep& o, StepLaunch* l) {
+  KeepArgs a = {};
+  a.c = cache_args(o.cache, o.row_start, o.n_rows);
+  a.path = o.path; a.count = o.count;
+  const int64_t waves = 2 * (int64_t)o.cache.n_seqs * o.cache.kv_heads;
+  if (waves > 0x7fffffffll) return kTooMany;
+  set_args(l, a);
+  return set_grid(l, t.keep[dim_index(o.cache.dim)], (waves + 3) / 4, 256, 0) ? "" : kTooMany;
+}
+
+inline std::string encode_copy(const StepTable& t, const daris_copy& o, StepLaunch* l) {
+  CopyArgs a = {};
+  a.c = cache_args(o.cache, nullptr, 0);
+  a.pairs = o.pairs;
+  a.n = o.n;
+  const int64_t pieces = ((int64_t)o.cache.kv_heads * kPage * o.cache.dim + kCopyPiece - 1) / kCopyPiece;
+  if (2 * pieces * o.n > 0xffffff) return kTooMany;
+  a.pieces = (int)pieces;
+  set_args(l, a);
+  return set_grid(l, t.copy[dim_index(o.cache.dim)], 2 * pieces * o.n, 256, 0) ? "" : kTooMany;
+}
+
 // What is wrong with an operator, or "".
 inline std::string check_step(const daris_op& op) {
   switch (op.kind) {
@@ -341,6 +481,12 @@ inline std::string check_step(const daris_op& op) {
     case DARIS_STEP_APPEND: return check_append(op.u.append);
     case DARIS_STEP_ATTEND: return check_attend(op.u.attend);
     case DARIS_STEP_MATVEC: return check_matvec(op.u.matvec);
+    case DARIS_STEP_TREE_APPEND: return check_tree_append(op.u.tree_append);
+    case DARIS_STEP_TREE_ATTEND: return check_tree_attend(op.u.tree_attend);
+    case DARIS_STEP_SAMPLE: return check_sample(op.u.sample);
+    case DARIS_STEP_ACCEPT: return check_accept(op.u.accept);
+    case DARIS_STEP_KEEP: return check_keep(op.u.keep);
+    case DARIS_STEP_COPY: return check_copy(op.u.copy);
   }
   return text("kind %d is no operator", op.kind);
 }
@@ -354,6 +500,18 @@ inline std::string encode_step(const StepTable& t, const daris_op& op, int n_cu,
     case DARIS_STEP_APPEND: return op.u.append.n_rows && op.u.append.cache.n_seqs ? encode_append(t, op.u.append, l) : "";
     case DARIS_STEP_ATTEND: return op.u.attend.n_rows && op.u.attend.cache.n_seqs ? encode_attend(t, op.u.attend, n_cu, l) : "";
     case DARIS_STEP_MATVEC: return op.u.matvec.rows ? encode_matvec(t, op.u.matvec, n_cu, l) : "";
+    case DARIS_STEP_TREE_APPEND: {
+      const daris_tree_append& o = op.u.tree_append;
+      return o.n_rows && o.cache.n_seqs ? encode_append(t, plain_append(o), l, {o.tree, o.tree_words}) : "";
+    }
+    case DARIS_STEP_TREE_ATTEND: {
+      const daris_tree_attend& o = op.u.tree_attend;
+      return o.attend.n_rows && o.attend.cache.n_seqs ? encode_attend(t, o.attend, n_cu, l, {o.tree, o.tree_words}) : "";
+    }
+    case DARIS_STEP_SAMPLE: return op.u.sample.rows ? encode_sample(t, op.u.sample, l) : "";
+    case DARIS_STEP_ACCEPT: return op.u.accept.n_seqs ? encode_accept(t, op.u.accept, l) : "";
+    case DARIS_STEP_KEEP: return op.u.keep.n_rows && op.u.keep.cache.n_seqs ? encode_keep(t, op.u.keep, l) : "";
+    case DARIS_STEP_COPY: return op.u.copy.n && op.u.copy.cache.n_pages ? encode_copy(t, op.u.copy, l) : "";
   }
   return "";
 }

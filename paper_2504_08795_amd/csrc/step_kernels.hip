@@ -12,6 +12,10 @@ __global__ __launch_bounds__(T) void step_norm(NormArgs a) { norm_body<BF16, F8,
 template <bool BF16, int D>
 __global__ __launch_bounds__(256) void step_append(AppendArgs a) { append_body<BF16, D>(a); }
 
+// ... where rows are nodes of trees
+template <bool BF16, int D>
+__global__ __launch_bounds__(256) void step_append_tree(TreeAppendArgs a) { append_body<BF16, D, true>(a.append, a.tree); }
+
 template <int XT, int G, bool BF16_OUT>
 __global__ __launch_bounds__(kMatvecWaves * 64) void step_matvec(MatvecArgs a) { matvec_body<XT, G, BF16_OUT>(a); }
 
@@ -24,6 +28,9 @@ __global__ __launch_bounds__(kMatvecWaves * 64) void step_matvec(MatvecArgs a) {
   template __global__ void step_norm<B, F, A, 0, 1024>(NormArgs);
 NORM(false, false, false) NORM(false, false, true) NORM(false, true, false) NORM(false, true, true)
 NORM(true, false, false) NORM(true, false, true) NORM(true, true, false) NORM(true, true, true)
+
+#define APPEND_TREE(B) template __global__ void step_append_tree<B, 64>(TreeAppendArgs); template __global__ void step_append_tree<B, 128>(TreeAppendArgs); template __global__ void step_append_tree<B, 256>(TreeAppendArgs);
+APPEND_TREE(false) APPEND_TREE(true)
 
 #define APPEND(B) template __global__ void step_append<B, 64>(AppendArgs); template __global__ void step_append<B, 128>(AppendArgs); template __global__ void step_append<B, 256>(AppendArgs);
 APPEND(false) APPEND(true)
