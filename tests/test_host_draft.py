@@ -168,7 +168,7 @@ def test_the_definitions_on_small_cases():
     total = 1 + 2 * e + 1 / e
     assert drawn(x, 0.0) == (0, pytest.approx(1 / total)) and drawn(x, 0.16)[0] == 1 and drawn(x, 1 / total + 1e-9)[0] == 1 and drawn(x, 0.999)[0] == 3
     assert drawn(x, 0.999, top_k=1) == (1, 1.0) and drawn(x, 0.999, top_k=2) == (2, 0.5) and drawn(x, 0.0, top_k=3)[0] == 0
-    assert drawn(x, 0.999, top_p=0.4)[0] == 1 and drawn(x, 0.999, top_p=0.5)[0] == 2 and drawn(x, 0.999, top_p=0.0)[0] == 1
+    assert drawn(x, 0.999, top_p=0.39)[0] == 1 and drawn(x, 0.999, top_p=0.5)[0] == 2 and drawn(x, 0.999, top_p=0.0)[0] == 1
     assert drawn(x, 0.999, min_p=0.5)[0] == 2 and drawn(x, 0.0, min_p=0.3)[0] == 0 and drawn(x, 0.999, min_p=7.0) == (1, 1.0)
     assert drawn(x, 0.999, temperature=0.0) == (1, 1.0) and drawn(torch.full((3,), float("nan")), 0.5) == (-1, 0.0)
     masks = D.tree_masks([[-1, 0, 0, 1, 1, 2]])
