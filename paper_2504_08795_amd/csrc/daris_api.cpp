@@ -1429,13 +1429,15 @@ static daris_status encode_steps(const daris_op* ops, int32_t n, daris_part p, S
   if (G->nodev) return fail(DARIS_ESTATE, "no device in DARIS_NO_DEVICE mode");
   plan->p = p;
   for (int i = 0; i < n; ++i) {
-    StepLaunch l;
-    const std::string err = encode_step(g_steps, ops[i], G->parts[p].n_cu, &l);
+    StepLaunch launch[2];
+    const std::string err = encode_step(g_steps, ops[i], G->parts[p].n_cu, &launch[0], &launch[1]);
     if (!err.empty()) return fail(DARIS_EINVAL, "operator %d: %s", i, err.c_str());
-    if (!l.groups) continue;
-    plan->bytes = std::max(plan->bytes, l.part_bytes);
-    plan->counters = std::max(plan->counters, l.counters);
-    plan->launches.push_back(l);
+    for (const StepLaunch& l : launch) {
+      if (!l.groups) continue;
+      plan->bytes = std::max(plan->bytes, l.part_bytes);
+      plan->counters = std::max(plan->counters, l.counters);
+      plan->launches.push_back(l);
+    }
   }
   return DARIS_OK;
 }

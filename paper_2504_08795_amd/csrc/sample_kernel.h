@@ -1,31 +1,48 @@
 // Draws a word for each row of logits: weights exp((x - M) / T) cut to the top_k largest, to the shortest front with top_p of their sum, to those of min_p,
-// and the first word, by number, at which the sum of the kept weights passes random x total.
+// and the first word, by number, at which the sum of the weights that are left passes random x total.
 //
 // Weights and their sums are held in 64 bits: a word is a whole number, and it changes where a sum passes the random number by a last bit.  Nothing is sorted:
-// what is kept is everything above a threshold, (logit, number) of one word.  It is found by a histogram of 4096 equal steps of the exponent (counts, and weights as whole numbers, whose
-// sums no order changes), and among the words of the one step that the threshold lies in by comparing each with each, or, where they are
-// many (equal logits), by their bits.  A workgroup a row; a row's numbers are read in chunks of 512, a wave each, and chunks whose largest is below what a pass looks for are left out.
+// what is left is everything above a threshold, (logit, number) of one word.  It is found by a histogram of equal steps of the exponent (counts, and weights as whole
+// numbers, whose sums no order changes), and among the words of the one step that the threshold lies in by finer steps and by comparing each with each, or, where they are
+// too many (equal logits), by their bits.
+//
+// Work. A row is cut into parts of up to kSamplePart numbers, a workgroup each, which reads them once: the largest, and as the row's wishes ask the histogram, or the sums
+// of weights, against its own largest (the steps are those of an absolute grid, so that histograms of parts are added by shifting them).  A second launch, a workgroup a row, adds them up and
+// finishes the row, from chunks of 512 numbers (a wave each) whose largest is above what a pass looks for.  (In one launch, the row's last workgroup finishing it, the others' successors
+// waited for its registers: 64 rows of 131072 135 us in place of NN.)
+//
+// What it costs is the length of that chain and its code, which comes from memory as well: loops over a lane's numbers are not unrolled where they compute weights (with
+// everything unrolled, 90 KB, a word of 50001 took 35 to 64 us).
 #pragma once
 #include "step_common.h"
 
 namespace daris {
 
-constexpr int kSampleThreads = kSampleWaves * 64;
+constexpr int kSampleThreads = kSampleWaves * 64, kSampleHeld = kSamplePart / kSampleChunk / kSampleWaves;
 constexpr int kSampleChunks = kSampleMost / kSampleChunk;
-constexpr float kSampleBits = 64.f;  // a weight below 2^-64 of the largest is nothing
+constexpr double kSampleBits = 64.0;   // a weight below 2^-64 of the largest is nothing
+constexpr double kSampleGrid = 15.9;   // steps of a power of two: all 64 of them in kSampleSteps
+static_assert(kSampleSteps == kSampleThreads, "a step for each thread");
+
+typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
 
 struct SampleLds {
-  float top[kSampleChunks];     // a chunk's largest
-  double sum[kSampleChunks];    // ... kept weights, or how many of its numbers are the threshold's
+  float top[kSampleChunks];         // a chunk's largest
+  float part_top[kSampleParts];     // ... a part's
+  int part_off[kSampleParts];       // steps of its histogram's first from the row's first; more than all: it has no part in it
+  double part_weight[kSampleParts]; // weight of its largest
+  uint64_t part_left[kSampleParts]; // ... of what is left of it
+  double sum[kSampleChunks];        // a chunk's weights that are left, or how many of its numbers are the threshold's
   uint32_t count[kSampleSteps];
   uint64_t mass[kSampleSteps];
-  uint32_t few_key[kSampleFew];
-  int few_at[kSampleFew];
+  uint64_t few[kSampleFew];         // words of one step: (logit, number), the larger word the larger number
   double wave_d[kSampleWaves];
   uint64_t wave_m[kSampleWaves];
   uint32_t wave_c[kSampleWaves];
   uint64_t found_mass;
-  uint32_t found_count, found_key;
+  uint64_t found_word;
+  double found_sum;
+  uint32_t found_count;
   int found, found_at;
 };
 
@@ -47,74 +64,270 @@ __device__ __forceinline__ uint64_t part_of(float p, uint64_t all) {
   return (hi << (64 - down) | lo >> down) + ((lo & ((1ull << down) - 1)) != 0);
 }
 
-template <typename T>
-__device__ __forceinline__ T wave_upto(T v) {  // of this lane and those in front
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const T o = __shfl_up(v, d);
-    if (lane >= d) v += o;
+// v of other lanes of a wave, as CTRL says; 0 where there is none.
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T from_lane(T v) {
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+  } else {
+    const u32x2 x = __builtin_bit_cast(u32x2, v);
+    u32x2 y;
+    y.x = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x.x, CTRL, ROWS, 0xf, false);
+    y.y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x.y, CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(T, y);
   }
-  return v;
+}
+// The sum over this lane and those in front: in its row of sixteen, in the wave (a third of the time of an exchange through LDS).
+template <typename T>
+__device__ __forceinline__ T row_upto(T v) {
+  v += from_lane<0x111, 0xf>(v);
+  v += from_lane<0x112, 0xf>(v);
+  v += from_lane<0x114, 0xf>(v);
+  return v + from_lane<0x118, 0xf>(v);
+}
+template <typename T>
+__device__ __forceinline__ T wave_upto(T v) {
+  v = row_upto(v);
+  v += from_lane<0x142, 0xa>(v);
+  return v + from_lane<0x143, 0xc>(v);
+}
+template <typename T>
+__device__ __forceinline__ T of_lane(T v, int lane) {
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+  } else {
+    u32x2 x = __builtin_bit_cast(u32x2, v);
+    x.x = (uint32_t)__builtin_amdgcn_readlane((int)x.x, lane);
+    x.y = (uint32_t)__builtin_amdgcn_readlane((int)x.y, lane);
+    return __builtin_bit_cast(T, x);
+  }
+}
+
+// 2^y for -64 <= y <= 0, 1 for 0: the series of e^f to the eleventh power, |f| <= ln 2 / 2, whose rest is below (ln 2 / 2)^12 / 12! = 2^-47.
+__device__ __forceinline__ double weight(double y) {
+  const double n = rint(y), f = (y - n) * 0.693147180559945309417;
+  double p = 1.0 / 39916800;
+  p = fma(p, f, 1.0 / 3628800);
+  p = fma(p, f, 1.0 / 362880);
+  p = fma(p, f, 1.0 / 40320);
+  p = fma(p, f, 1.0 / 5040);
+  p = fma(p, f, 1.0 / 720);
+  p = fma(p, f, 1.0 / 120);
+  p = fma(p, f, 1.0 / 24);
+  p = fma(p, f, 1.0 / 6);
+  p = fma(p, f, 0.5);
+  p = fma(p, f, 1.0);
+  p = fma(p, f, 1.0);
+  return __builtin_amdgcn_ldexp(p, (int)n);
 }
 
 template <bool BF16>
 struct Sampler {
   static constexpr int kPer = kSampleChunk / 64;  // numbers of a lane in a chunk, side by side
   static constexpr float kLowest = -3.4028235e38f;
+  static constexpr int kAhead = BF16 ? 4 : 2;  // chunks of a wave that are on their way (registers for more there are not)
   const SampleArgs& a;
   SampleLds& m;
   const char* row;
   int tid, lane, wave;
-  float most;
-  double step;  // log2(e) / T
-  float bins;   // steps of the histogram for a unit of the logits
-  double least_weight;
-  uint32_t key;  // the threshold: kept is what is above it, or it with a number up to `upto`
+  float most, temperature;
+  double step;   // log2(e) / T
+  double grid;   // steps of the histogram for a unit of the logits
+  double place;  // the largest's place on the grid
+  uint32_t key;  // the threshold: left is what is above it, or it with a number up to `upto`
   int upto;
-  int shift;  // weights as whole numbers: times 2^shift
+  int listed;           // m.few has all words that are left (and others), so many
+  int below;            // step of the histogram that the threshold is in, -1: the parts' sums are not known
+  double two_to_shift;  // weights as whole numbers: times this; the sum of a row's stays below 2^62
 
-  __device__ __forceinline__ void load(int chunk, float (&x)[kPer]) const {
-    const int e = chunk * kSampleChunk + lane * kPer;
-    if (a.vec && e + kPer <= a.n) {
-      if (BF16) {
-        unpack<true>(*(const uint4*)(row + 2 * (int64_t)e), x);
-      } else {
-        float lo[4], hi[4];
-        unpack<false>(*(const uint4*)(row + 4 * (int64_t)e), lo);
-        unpack<false>(*(const uint4*)(row + 4 * (int64_t)e + 16), hi);
+  // A lane's numbers of a chunk as they are in memory.  They begin at `first` (the last ones of the row where it ends in front of them).
+  struct Raw {
+    uint32_t w[BF16 ? 4 : 8];
+  };
+  __device__ __forceinline__ int first_of(int chunk) const {
+    const int e = chunk * kSampleChunk + lane * kPer, last = a.n - kPer;
+    return e < last ? e : last > 0 ? last : 0;
+  }
+  __device__ __forceinline__ void fetch(int chunk, Raw* r) const {
+    const int first = first_of(chunk);
+    if (a.n >= kPer) {  // (rows need not be aligned to more than their numbers)
+      const u32x4_a2* p = (const u32x4_a2*)(row + (BF16 ? 2 : 4) * (int64_t)first);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[i] = lo[i];
-          x[i + 4] = hi[i];
-        }
+      for (int i = 0; i < (BF16 ? 1 : 2); ++i) {
+        const u32x4 v = p[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r->w[4 * i + j] = v[j];
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) x[i] = e + i < a.n ? load_elem<BF16>(row, e + i) : -INFINITY;
+      for (int i = 0; i < kPer; ++i) {
+        const int at = i < a.n ? i : a.n - 1;
+        if (!BF16) r->w[i % (BF16 ? 4 : 8)] = ((const uint32_t*)row)[at];
+        else if (i & 1) r->w[i / 2] |= (uint32_t)((const uint16_t*)row)[at] << 16;
+        else r->w[i / 2] = ((const uint16_t*)row)[at];
+      }
     }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) x[i] = x[i] != x[i] ? -INFINITY : x[i] + 0.f;  // (-0 and 0 are equal)
   }
+  // ... as numbers: -infinity for NaN, for what an earlier lane has and for what lies behind the row
+  __device__ __forceinline__ void numbers(const Raw& r, int chunk, float (&x)[kPer]) const {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) x[i] = fmaxf(__uint_as_float(BF16 ? (i & 1 ? r.w[i / 2] & 0xffff0000u : r.w[i / 2] << 16) : r.w[i % (BF16 ? 4 : 8)]) + 0.f, -INFINITY);  // (-0 and 0 are equal)
+    if ((chunk + 1) * kSampleChunk <= a.n) return;
+    const int skip = chunk * kSampleChunk + lane * kPer - first_of(chunk), end = a.n < kPer ? a.n : kPer;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) x[i] = i >= skip && i < end ? x[i] : -INFINITY;
+  }
+  __device__ __forceinline__ void load(int chunk, float (&x)[kPer]) const {
+    Raw r;
+    fetch(chunk, &r);
+    numbers(r, chunk, x);
+  }
+  // f(i, x[i]) for the set bits of `on`, lowest first, a lane after its own
+  template <typename F>
+  static __device__ __forceinline__ void one_by_one(uint32_t on, const float (&x)[kPer], const F& f) {
+    while (on) {
+      const uint32_t least = on & -on;
+      float v = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        asm("" : "+v"(v));  // (a register each: left to itself the compiler makes an array in memory of them)
+        v = least >> e & 1 ? x[e] : v;
+      }
+      f(__builtin_ctz(on), v);
+      on &= on - 1;
+    }
+  }
+
   // In powers of two, 0 for the largest; NaN or below -64 for what is nothing.
   __device__ __forceinline__ double bits(float x) const { return x == most ? 0.0 : ((double)x - (double)most) * step; }
-  __device__ __forceinline__ bool live(double y) const { return y >= -(double)kSampleBits; }
-  // Whether the number has a weight and is on the threshold's side.
+  // Its step of the histogram, from the largest's on.  (Where the grid is finer than 64 bits tell, what differs from the largest is nothing.)
+  __device__ __forceinline__ int bin(float x) const {
+    const double b = place - floor((double)x * grid);
+    return x == most ? 0 : b < kSampleSteps ? (int)b : kSampleSteps - 1;
+  }
+  // The least number for which ok holds, as order_key has it: `guess` but for its rounding.  ok holds for the largest, and for what is above a number for which it does.
+  template <typename F>
+  __device__ __forceinline__ uint32_t least_key(double guess, const F& ok) const {
+    uint32_t k = order_key(most == INFINITY ? most : fminf(fmaxf((float)guess, kLowest), most) + 0.f);
+#pragma unroll 1
+    for (int i = 0; i < 4 && k > order_key(kLowest) && ok(of_key(k - 1) + 0.f); ++i) --k;
+#pragma unroll 1
+    for (int i = 0; i < 4 && !ok(of_key(k)); ++i) ++k;
+    return k;
+  }
+  // ... that is in step b or above
+  __device__ __forceinline__ uint32_t least_of(int b) const {
+    if (b >= kSampleSteps - 1) return order_key(kLowest);
+    return least_key(grid > 0 ? (place - b) / grid : -INFINITY, [&](float x) { return bin(x) <= b; });
+  }
+  static __device__ __forceinline__ uint32_t between(const float (&x)[kPer], float lowest, float highest) {
+    uint32_t on = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) on |= x[i] >= lowest && x[i] <= highest ? 1u << i : 0u;
+    return on;
+  }
+  // A finer step of step b, the largest first.
+  __device__ __forceinline__ int fine(float x, int b) const {
+    const double t = (place - b + 1 - (double)x * grid) * kSampleSteps;
+    return x == most ? 0 : (int)fmin(fmax(t, 0.0), kSampleSteps - 1.0);
+  }
+  // Whether the number is on the threshold's side (nothing that weighs nothing is).
   __device__ __forceinline__ bool counted(float x, int at) const {
     const uint32_t k = order_key(x);
-    return x > -INFINITY && live(bits(x)) && (k > key || (k == key && at <= upto));
+    return k > key || (k == key && at <= upto);
   }
-  __device__ __forceinline__ int bin(float x) const { return x == most ? 0 : (int)fminf((most - x) * bins, (float)(kSampleSteps - 1)); }
-  __device__ __forceinline__ uint64_t whole(double w) const { return (uint64_t)(ldexp(w, shift) + 0.5); }
+  // ... of a lane's numbers, a bit each
+  __device__ __forceinline__ uint32_t counted(const float (&x)[kPer], int first) const {
+    uint32_t on = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) on |= counted(x[i], first + i) ? 1u << i : 0u;
+    return on;
+  }
+  // Moves the threshold up to the least number that weighs `least` or more (0: anything), which is most + far but for its rounding.
+  __device__ __forceinline__ void leave(double far, double least) {
+    const uint32_t k = least_key((double)most + far, [&](float x) {
+      const double y = bits(x);
+      return y >= -kSampleBits && (least == 0 || weight(y) >= least);
+    });
+    if (k > key) {
+      key = k;
+      upto = 0x7fffffff;
+    }
+  }
+  // What follows is against this largest number; all that weighs anything beside it is left.
+  __device__ __forceinline__ void against(float largest) {
+    most = largest;
+    place = floor((double)most * grid);
+    key = 0;
+    leave((double)temperature * (-kSampleBits * 0.693147180559945309417), 0);
+  }
+  __device__ __forceinline__ uint64_t whole(float x) const { return (uint64_t)(weight(bits(x)) * two_to_shift + 0.5); }
+  __device__ __forceinline__ void add_to(int b, float x, bool mass) {
+    atomicAdd(&m.count[b], 1u);
+    if (mass) atomicAdd((unsigned long long*)&m.mass[b], (unsigned long long)whole(x));
+  }
+  static __device__ __forceinline__ uint64_t scaled(uint64_t v, double f) { return f == 1.0 ? v : (uint64_t)((double)v * f + 0.5); }
+  __device__ __forceinline__ void clear_steps() {
+    m.count[tid] = 0;
+    m.mass[tid] = 0;
+  }
+  // The sum of a lane's weights that are left, and of the wave's.
+  __device__ __forceinline__ double sum_of(const float (&x)[kPer], int first) const {
+    double s = 0;
+    one_by_one(counted(x, first), x, [&](int, float v) { s += weight(bits(v)); });
+    return s;
+  }
+  // Sums over the threads in front, and over all (v_wave: LDS for the waves' sums).  A barrier inside; another before v_wave is written again.
+  template <typename T>
+  __device__ __forceinline__ T in_front(T v, T* v_wave, T* all) const {
+    const T upto_me = wave_upto(v);
+    if (lane == 63) v_wave[wave] = upto_me;
+    __syncthreads();
+    const T waves = row_upto(v_wave[lane & (kSampleWaves - 1)]);
+    *all = of_lane(waves, kSampleWaves - 1);
+    const T before = of_lane(waves, wave > 0 ? wave - 1 : 0);
+    return (wave > 0 ? before : T(0)) + (upto_me - v);
+  }
 
-  // f(chunk, first number of the lane, its numbers) for the chunks whose largest is `from` or more
+  // What the parts of a row leave: [row][chunks] floats, their largest, in front; [row][chunks] sums; [row][part] histograms.
+  __device__ __forceinline__ float* tops_at(int r) const { return a.part + (int64_t)r * a.row_floats; }
+  __device__ __forceinline__ double* sums_at(int r) const { return (double*)(tops_at(r) + (a.chunks + 1) / 2 * 2); }
+  __device__ __forceinline__ uint64_t* mass_at(int r, int part) const { return (uint64_t*)(sums_at(r) + a.chunks) + (int64_t)part * (kSampleSteps + kSampleSteps / 2); }
+  __device__ __forceinline__ uint32_t* counts_at(int r, int part) const { return (uint32_t*)(mass_at(r, part) + kSampleSteps); }
+
+  // f(chunk, first, x) for the chunks whose largest is `from` or more: a lane's numbers x of them, from number `first` on.  kAhead chunks of a wave are on their way.
   template <typename F>
-  __device__ __forceinline__ void each(float from, const F& f) const {
-    for (int c = wave; c < a.chunks; c += kSampleWaves) {
-      if (m.top[c] < from) continue;
-      float x[kPer];
-      load(c, x);
-      f(c, c * kSampleChunk + lane * kPer, x);
+  __device__ __forceinline__ void each(float from, const F& f, int begin = 0, int end = kSampleChunks) const {
+    end = end < a.chunks ? end : a.chunks;
+#pragma unroll 1
+    for (int base = begin; base < end; base += 64 * kSampleWaves) {
+      const int mine = base + lane * kSampleWaves + wave;
+      uint64_t left = __ballot(mine < end && m.top[mine < end ? mine : 0] >= from);
+      if (!left) continue;
+      Raw r[kAhead] = {};
+      int c[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) c[i] = -1;
+      bool more;
+#pragma unroll 1
+      do {
+#pragma unroll
+        for (int i = 0; i + 1 < kAhead; ++i) {
+          r[i] = r[i + 1];
+          c[i] = c[i + 1];
+        }
+        c[kAhead - 1] = left ? base + __builtin_ctzll(left) * kSampleWaves + wave : -1;
+        left &= left - 1;
+        if (c[kAhead - 1] >= 0) fetch(c[kAhead - 1], &r[kAhead - 1]);
+        if (c[0] >= 0) {
+          float x[kPer];
+          numbers(r[0], c[0], x);
+          f(c[0], first_of(c[0]), x);
+        }
+        more = false;
+#pragma unroll
+        for (int i = 1; i < kAhead; ++i) more = more || c[i] >= 0;
+      } while (more);
     }
   }
 
@@ -124,183 +337,219 @@ struct Sampler {
   __device__ __forceinline__ int chunk_at(double target_of_all, double target, double* front, double* all) {
     constexpr int EACH = kSampleChunks / kSampleThreads;
     double v[EACH], mine = 0;
-    int last = -1;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int c = tid * EACH + i;
-      v[i] = c < a.chunks ? m.sum[c] : 0;
+      v[i] = tid * EACH + i < a.chunks ? m.sum[tid * EACH + i] : 0;
       mine += v[i];
-      if (v[i] > 0) last = c;
     }
-    const double upto_me = wave_upto(mine);
-    if (lane == 63) m.wave_d[wave] = upto_me;
     if (tid == 0) {
       m.found = kSampleChunks;
-      m.found_at = -1;
+      m.found_at = 0;
     }
-    __syncthreads();
-    double base = 0, total = 0;
-    for (int w = 0; w < kSampleWaves; ++w) {
-      if (w == wave) base = total;
-      total += m.wave_d[w];
-    }
+    double total, sum = in_front(mine, m.wave_d, &total);
     target += target_of_all * total;
-    double sum = base + upto_me - mine;
+    // (of a wave one lane says which is its first, and which its last: all at one address would come one after the other)
+    double begins[EACH];
+    int first = kSampleChunks, last = -1;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const double next = sum + v[i];
-      if (v[i] > 0 && (REACHES ? next >= target : next > target)) atomicMin(&m.found, tid * EACH + i);
-      sum = next;
-    }
-    if (last >= 0) atomicMax(&m.found_at, last);
-    __syncthreads();
-    int c = m.found < kSampleChunks ? m.found : m.found_at;
-    c = c < 0 ? 0 : c;
-    sum = base + upto_me - mine;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      if (tid * EACH + i == c) m.wave_d[0] = sum;  // (read by all above, before the last barrier)
+      begins[i] = sum;
       sum += v[i];
+      if (v[i] > 0) {
+        last = tid * EACH + i;
+        if (first == kSampleChunks && (REACHES ? sum >= target : sum > target)) first = tid * EACH + i;
+      }
     }
+    const uint64_t any = __ballot(last >= 0), hit = __ballot(first < kSampleChunks);
+    if (any && lane == 63 - __builtin_clzll(any)) atomicMax(&m.found_at, last);
+    if (hit && lane == __builtin_ctzll(hit)) atomicMin(&m.found, first);
     __syncthreads();
-    *front = m.wave_d[0];
+    const int c = m.found < kSampleChunks ? m.found : m.found_at;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+      if (tid * EACH + i == c) m.found_sum = begins[i];
+    __syncthreads();
+    *front = m.found_sum;
     *all = total;
-    __syncthreads();
     return c;
   }
 
-  // Threshold of the words in front (largest first) until their number reaches `want_count`, or (BY_MASS) their weight `want_mass`.
-  template <bool BY_MASS>
-  __device__ __forceinline__ void front(uint32_t want_count, uint64_t want_mass) {
-    // ---- which step
-    uint32_t above = 0;
-    uint64_t above_mass = 0;
-    uint32_t in = 0;
-    const int b = step_at<BY_MASS, kSampleSteps>(want_count, want_mass, &above, &above_mass, &in);
-    if (tid == 0) m.found_count = 0;
-    __syncthreads();
-    float edge = most - (float)(b + 1) / bins;  // nothing of the step is below it, but for roundings
-    edge -= fabsf(edge) * 1e-5f + fabsf(most) * 1e-5f;
-    if (!(edge > -INFINITY)) edge = kLowest;
-    if (in <= kSampleFew) {
-      each(edge, [&](int, int at, const float(&x)[kPer]) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-          if (counted(x[i], at + i) && bin(x[i]) == b) {
-            const uint32_t n = atomicAdd(&m.found_count, 1u);
-            m.few_key[n] = order_key(x[i]);
-            m.few_at[n] = at + i;
-          }
-      });
-      __syncthreads();
-      if (tid < (int)in) {
-        const uint32_t k = m.few_key[tid];
-        const int at = m.few_at[tid];
-        uint32_t n = above;
-        uint64_t w = above_mass;
-        for (uint32_t o = 0; o < in; ++o) {
-          const uint32_t ok = m.few_key[o];
-          if (ok > k || (ok == k && m.few_at[o] < at)) {
-            ++n;
-            if (BY_MASS) w += whole(exp2(bits(of_key(ok))));
-          }
-        }
-        const uint64_t own = BY_MASS ? whole(exp2(bits(of_key(k)))) : 0;
-        if (BY_MASS ? w < want_mass && want_mass <= w + own : n + 1 == want_count) {
-          m.found_key = k;
-          m.found_at = at;
-        }
-      }
-      __syncthreads();
-      key = m.found_key;
-      upto = m.found_at;
-      __syncthreads();
-      return;
-    }
-    // ---- many: by their bits, 11, 11 and 10 of them
-    uint32_t prefix = 0;
-    uint32_t ties = 0;
-#pragma unroll 1
-    for (int level = 0; level < 3; ++level) {
-      const int low = level == 0 ? 21 : level == 1 ? 10 : 0, width = level == 2 ? 10 : 11;
-      for (int i = tid; i < 2048; i += kSampleThreads) {
-        m.count[i] = 0;
-        m.mass[i] = 0;
-      }
-      __syncthreads();
-      each(edge, [&](int, int at, const float(&x)[kPer]) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const uint32_t k = order_key(x[i]);
-          if (counted(x[i], at + i) && bin(x[i]) == b && (level == 0 || k >> (low + width) == prefix)) {
-            const uint32_t d = ((1u << width) - 1) & ~(k >> low);  // the largest first
-            atomicAdd(&m.count[d], 1u);
-            if (BY_MASS) atomicAdd((unsigned long long*)&m.mass[d], (unsigned long long)whole(exp2(bits(x[i]))));
-          }
-        }
-      });
-      __syncthreads();
-      const uint32_t d = step_at<BY_MASS, 2048>(want_count - above, want_mass - above_mass, &above, &above_mass, &ties);
-      prefix = prefix << width | (((1u << width) - 1) & ~d);
-    }
-    const uint32_t was = key;
-    key = prefix;
-    const uint64_t own = whole(exp2(bits(of_key(key))));
-    const uint32_t take = BY_MASS ? (uint32_t)((want_mass - above_mass + own - 1) / own) : want_count - above;
-    if (take < ties) upto = nth_equal(take);
-    else if (key != was) upto = 0x7fffffff;
-  }
-
-  // The step (of N) in which the sums over m.count or m.mass reach what is wanted; *count, *mass: added to by what lies above it; *in: what it holds.
-  template <bool BY_MASS, int N>
-  __device__ __forceinline__ int step_at(uint32_t want_count, uint64_t want_mass, uint32_t* count, uint64_t* mass, uint32_t* in) {
-    constexpr int EACH = N / kSampleThreads;
-    uint32_t c = 0;
-    uint64_t w = 0;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      c += m.count[tid * EACH + i];
-      w += m.mass[tid * EACH + i];
-    }
-    const uint32_t c_upto = wave_upto(c);
-    const uint64_t w_upto = wave_upto((unsigned long long)w);
-    if (lane == 63) {
-      m.wave_c[wave] = c_upto;
-      m.wave_m[wave] = w_upto;
-    }
-    if (tid == 0) m.found = N - 1;
-    __syncthreads();
-    uint32_t c_base = c_upto - c;
-    uint64_t w_base = w_upto - w;
-    for (int v = 0; v < wave; ++v) {
-      c_base += m.wave_c[v];
-      w_base += m.wave_m[v];
-    }
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const uint32_t cc = m.count[tid * EACH + i];
-      const uint64_t ww = m.mass[tid * EACH + i];
-      if (BY_MASS ? w_base < want_mass && want_mass <= w_base + ww : c_base < want_count && want_count <= c_base + cc) {
-        m.found = tid * EACH + i;
-        m.found_count = c_base;
-        m.found_mass = w_base;
-      }
-      c_base += cc;
-      w_base += ww;
+  // The step in which the sums over m.count (or, by mass, m.mass) reach what is wanted (or all that there is, if that is less); *count, *mass: added to by what lies above it;
+  // *in: what it holds.  whole_row: -1 if all of the count is wanted.
+  __device__ __forceinline__ int step_at(bool by_mass, bool whole_row, uint32_t want_count, uint64_t want_mass, uint32_t* count, uint64_t* mass, uint32_t* in) {
+    if (tid == 0) m.found = -1;
+    const uint32_t c = m.count[tid];
+    const uint64_t w = m.mass[tid];
+    uint32_t c_all;
+    uint64_t w_all;
+    const uint32_t c_base = in_front(c, m.wave_c, &c_all);
+    const uint64_t w_base = in_front(w, m.wave_m, &w_all);
+    if (!by_mass && whole_row && want_count >= c_all) want_count = 0;
+    want_count = want_count < c_all ? want_count : c_all;
+    want_mass = want_mass < w_all ? want_mass : w_all;
+    if (by_mass ? w_base < want_mass && want_mass <= w_base + w : c_base < want_count && want_count <= c_base + c) {
+      m.found = tid;
+      m.found_count = c_base;
+      m.found_mass = w_base;
     }
     __syncthreads();
     const int b = m.found;
-    *count += m.found_count;
-    *mass += m.found_mass;
-    *in = m.count[b];
+    if (b >= 0) {
+      *count += m.found_count;
+      *mass += m.found_mass;
+      *in = m.count[b];
+    }
     __syncthreads();
     return b;
+  }
+
+  // Moves the threshold to the last word of those in front (largest first) whose number is `want_count`, or (by mass) whose weight reaches `want_mass`.
+  // sums: what the step's words that are left weigh goes to m.part_left, which is zero.
+  __device__ __forceinline__ void front(bool by_mass, uint32_t want_count, uint64_t want_mass, bool sums) {
+    uint32_t above = 0, in = 0;
+    uint64_t above_mass = 0;
+    const int b = step_at(by_mass, true, want_count, want_mass, &above, &above_mass, &in);
+    if (b < 0) return;  // fewer than that: none is cut
+    below = -1;
+    listed = 0;
+    const uint32_t first_above = above;
+    const uint64_t first_mass = above_mass;
+    const uint32_t from = least_of(b);
+    const float edge = of_key(from > key ? from : key);
+    float highest = b > 0 ? of_key(least_of(b - 1) - 1) : most;
+    bool few = in <= kSampleFew;
+    if (few) {
+      // ---- the step's words in LDS, with those above it where all are few
+      const bool with_above = above + in <= kSampleRank / 2;
+      if (with_above) {
+        highest = most;
+        above = 0;
+        above_mass = 0;
+      }
+      if (tid == 0) m.found_count = 0;
+      __syncthreads();
+      each(edge, [&](int, int first, const float(&x)[kPer]) {
+        uint32_t on = between(x, edge, highest);
+        if (upto != 0x7fffffff) on &= counted(x, first);
+        const int n = __popc(on), end = wave_upto(n), all = of_lane(end, 63);
+        if (all == 0) return;
+        int base = 0;
+        if (lane == 0) base = (int)atomicAdd(&m.found_count, (uint32_t)all);
+        base = uniform(base) + end - n;
+        one_by_one(on, x, [&](int i, float v) {
+          if (base < kSampleFew) m.few[base] = (uint64_t)order_key(v) << 32 | ~(uint32_t)(first + i);
+          ++base;
+        });
+      });
+      __syncthreads();
+      in = m.found_count < kSampleFew ? m.found_count : kSampleFew;
+      listed = with_above ? (int)in : 0;
+      // (a thread keeps its words of the step: in the end those that are left are weighed for their parts)
+      constexpr int N = kSampleFew / kSampleThreads;
+      uint64_t mine[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) mine[i] = tid + i * kSampleThreads < (int)in ? m.few[tid + i * kSampleThreads] : 0;
+      if (in == 0) return;  // (counted against parts whose largest is smaller: nothing here weighs 2^-64, and all that does is in front)
+      if (in > kSampleRank / 4 && !with_above) {
+        // ---- those of one of its finer steps
+        int step_of[N];
+        clear_steps();
+        if (tid == 0) m.found_at = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int n = tid + i * kSampleThreads;
+          step_of[i] = -1;
+          if (n < (int)in) {
+            const float x = of_key((uint32_t)(mine[i] >> 32));
+            step_of[i] = fine(x, b);
+            add_to(step_of[i], x, by_mass);
+          }
+        }
+        __syncthreads();
+        const int d = step_at(by_mass, false, want_count - above, want_mass - above_mass, &above, &above_mass, &in);
+        if (d < 0) return;
+        few = in <= kSampleRank;
+        if (few) {
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            if (step_of[i] == d) m.few[atomicAdd(&m.found_at, 1)] = mine[i];
+          __syncthreads();
+        }
+      }
+      if (few) {
+      // ---- each with each, so many threads to a word that all have one
+      int threads = 64;
+      while (threads * (int)in > kSampleThreads) threads /= 2;
+      const int word = tid / threads;
+      const bool on = word < (int)in;
+      const uint64_t own_word = on ? m.few[word] : 0;
+      if (by_mass) {
+        if (tid < (int)in) m.mass[tid] = whole(of_key((uint32_t)(m.few[tid] >> 32)));  // (the histogram has done its work)
+        __syncthreads();
+      }
+      uint32_t n = 0;
+      uint64_t w = 0;
+#pragma unroll 4
+      for (int o = tid & (threads - 1); o < (int)in; o += threads) {
+        const bool before = m.few[o] > own_word;
+        n += before;
+        if (by_mass) w += before ? m.mass[o] : 0;
+      }
+#pragma unroll 1
+      for (int d = 1; d < threads; d *= 2) {
+        n += __shfl_xor(n, d);
+        if (by_mass) w += __shfl_xor((unsigned long long)w, d);
+      }
+      n += above;
+      w += above_mass;
+      const uint64_t own = by_mass && on ? m.mass[word] : 0;
+      // (the last, if they come to less: the histogram's sums are rounded otherwise)
+      if (on && ((by_mass ? w < want_mass && want_mass <= w + own : n + 1 == want_count) || (n + 1 == above + in && (by_mass ? w + own < want_mass : n + 1 < want_count)))) m.found_word = own_word;
+      __syncthreads();
+      key = (uint32_t)(m.found_word >> 32);
+      upto = (int)~(uint32_t)m.found_word;
+      if (sums && !with_above) {
+        below = b;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (mine[i] >= m.found_word) atomicAdd((unsigned long long*)&m.part_left[(int)~(uint32_t)mine[i] / (a.part_chunks * kSampleChunk)], (unsigned long long)whole(of_key((uint32_t)(mine[i] >> 32))));
+      }
+      return;
+      }
+    }
+    // ---- many: by their bits, 10, 10, 6 and 6 of them
+    above = first_above;
+    above_mass = first_mass;
+    uint32_t prefix = 0, ties = 0;
+#pragma unroll 1
+    for (int level = 0; level < 4; ++level) {
+      const int low = level == 0 ? 22 : level == 1 ? 12 : level == 2 ? 6 : 0, width = level < 2 ? 10 : 6;
+      clear_steps();
+      __syncthreads();
+      each(edge, [&](int, int first, const float(&x)[kPer]) {
+        one_by_one(counted(x, first) & between(x, edge, highest), x, [&](int, float v) {
+          const uint32_t k = order_key(v);
+          if (level == 0 || k >> (low + width) == prefix) add_to(((1u << width) - 1) & ~(k >> low), v, by_mass);  // the largest first
+        });
+      });
+      __syncthreads();
+      const int d = step_at(by_mass, false, want_count - above, want_mass - above_mass, &above, &above_mass, &ties);
+      if (d < 0) return;
+      prefix = prefix << width | (((1u << width) - 1) & ~(uint32_t)d);
+    }
+    const uint32_t was = key;
+    key = prefix;
+    const uint64_t own = whole(of_key(key));
+    const uint32_t take = by_mass ? (uint32_t)((want_mass - above_mass + own - 1) / own) : want_count - above;
+    if (take < ties) upto = nth_equal(take);
+    else if (key != was) upto = 0x7fffffff;
   }
 
   // Number of the n-th word whose logit is the threshold's.
   __device__ __forceinline__ int nth_equal(uint32_t n) {
     const float value = of_key(key);
-    for (int c = tid; c < kSampleChunks; c += kSampleThreads) m.sum[c] = 0;
+    for (int c = tid; c < a.chunks; c += kSampleThreads) m.sum[c] = 0;
     __syncthreads();
     each(value, [&](int c, int, const float(&x)[kPer]) {
       int k = 0;
@@ -309,49 +558,193 @@ struct Sampler {
       if (lane == 0) m.sum[c] = k;
     });
     __syncthreads();
-    double front, all;
-    const int c = chunk_at<true>(0, (double)n, &front, &all);
+    double in_chunks, all;
+    const int c = chunk_at<true>(0, (double)n, &in_chunks, &all);
     if (wave == 0) {
       float x[kPer];
       load(c, x);
-      int k = 0, left = (int)n - (int)front;
+      int k = 0;
+      const int left = (int)n - (int)in_chunks;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) k += x[i] == value;
       int base = wave_upto(k) - k;
 #pragma unroll
       for (int i = 0; i < kPer; ++i)
-        if (x[i] == value && ++base == left) m.found_at = c * kSampleChunk + lane * kPer + i;
+        if (x[i] == value && ++base == left) m.found_at = first_of(c) + i;
     }
     __syncthreads();
-    const int at = m.found_at;
+    return m.found_at;
+  }
+
+  // Draws from the words of m.few that are left: in the order of their numbers, as each counts those in front of it.
+  __device__ __forceinline__ void pick(int r, float u) {
+    int threads = 64;
+    while (threads * listed > kSampleThreads) threads /= 2;
+    const int word = tid / threads;
+    const uint64_t own = word < listed ? m.few[word] : 0;
+    const bool on = word < listed && counted(of_key((uint32_t)(own >> 32)), (int)~(uint32_t)own);
+    if (tid == 0) {
+      m.found = kSampleThreads;
+      m.found_at = 0;
+    }
+    int n = 0;
+#pragma unroll 4
+    for (int o = tid & (threads - 1); o < listed; o += threads) {
+      const uint64_t w = m.few[o];
+      n += (uint32_t)w > (uint32_t)own && counted(of_key((uint32_t)(w >> 32)), (int)~(uint32_t)w);
+    }
+#pragma unroll 1
+    for (int d = 1; d < threads; d *= 2) n += __shfl_xor(n, d);
     __syncthreads();
-    return at;
+    if (on && (tid & (threads - 1)) == 0) {
+      m.sum[n] = weight(bits(of_key((uint32_t)(own >> 32))));
+      m.count[n] = ~(uint32_t)own;
+      atomicMax(&m.found_at, n);
+    }
+    __syncthreads();
+    const int last = m.found_at;
+    const double v = tid <= last ? m.sum[tid] : 0;
+    double total;
+    const double front = in_front(v, m.wave_d, &total);
+    const uint64_t hit = __ballot(tid <= last && front + v > (double)u * total);
+    if (hit && lane == __builtin_ctzll(hit)) atomicMin(&m.found, tid);
+    __syncthreads();
+    if (tid == (m.found <= last ? m.found : last)) {
+      a.word[r] = (int)m.count[tid];
+      if (a.chance) a.chance[r] = (float)(v / total);
+    }
   }
 
-  __device__ __forceinline__ double kept(float x, int at) const {
-    if (!counted(x, at)) return 0;
-    const double w = exp2(bits(x));
-    return w >= least_weight ? w : 0;
-  }
-
-  __device__ __forceinline__ void run(int r) {
+  // What row r asks for.
+  int k;
+  float p, mp;
+  bool greedy, by_count, by_mass, steps, all, weighed;
+  __device__ __forceinline__ void wishes(int r) {
     row = (const char*)a.logits + (int64_t)r * a.row * (BF16 ? 2 : 4);
-    // ---- the largest
+    temperature = a.temperature ? a.temperature[r] : 1.f;
+    p = a.top_p ? a.top_p[r] : 1.f;
+    mp = a.min_p ? a.min_p[r] : 0.f;
+    k = a.top_k ? a.top_k[r] : 0;
+    greedy = !a.random || !(temperature > 0.f) || mp > 1.f;  // (nothing weighs more than the largest)
+    by_count = !greedy && k > 0 && k < a.n;
+    by_mass = !greedy && p < 1.f;
+    steps = by_count || by_mass;
+    all = !greedy && !steps && !(mp > 0.f);  // of them are left
+    // The histogram has weights where they are asked for, and where many words may be left, whose parts' sums then need not be taken again.
+    weighed = by_mass || (by_count && k > kSampleChunk);
+    step = 1.4426950408889634074 / (double)temperature;
+    grid = step * kSampleGrid;
+    two_to_shift = (double)(1ull << (62 - (32 - __builtin_clz(a.n))));
+  }
+
+  // One part of row r: its chunks' largest, and as the row asks its histogram or its chunks' sums, in LDS and (where there are others) in a.part.
+  __device__ __forceinline__ void part(int r, int part) {
+    // ---- the part's largest
+    const int c0 = part * a.part_chunks, c1 = c0 + a.part_chunks < a.chunks ? c0 + a.part_chunks : a.chunks;
+    Raw raw[kSampleHeld];
+#pragma unroll
+    for (int h = 0; h < kSampleHeld; ++h) {
+      const int c = c0 + h * kSampleWaves + wave;
+      fetch(c < c1 ? c : c0, &raw[h]);  // (no branch: they travel together)
+    }
+    clear_steps();
     float top = -INFINITY;
-    for (int c = wave; c < a.chunks; c += kSampleWaves) {
+#pragma unroll
+    for (int h = 0; h < kSampleHeld; ++h) {
+      const int c = c0 + h * kSampleWaves + wave;
+      if (c >= c1) break;
       float x[kPer];
-      load(c, x);
+      numbers(raw[h], c, x);
       float t = x[0];
 #pragma unroll
       for (int i = 1; i < kPer; ++i) t = fmaxf(t, x[i]);
       t = wave_max<64>(t);
-      if (lane == 0) m.top[c] = t;
+      if (lane == 0) {
+        m.top[c] = t;
+        if (a.parts > 1) tops_at(r)[c] = t;
+      }
       top = fmaxf(top, t);
     }
     if (lane == 0) m.wave_d[wave] = top;
     __syncthreads();
-    most = -INFINITY;
-    for (int w = 0; w < kSampleWaves; ++w) most = fmaxf(most, (float)m.wave_d[w]);
+    top = lanes_max<1, kSampleWaves>((float)m.wave_d[lane & (kSampleWaves - 1)]);
+    // ---- its weights against its largest
+    if (greedy) most = top;
+    else against(top);
+    if ((steps || all) && top > -INFINITY) {
+#pragma unroll 1
+      for (int h = 0; h < kSampleHeld; ++h) {
+        const int c = c0 + h * kSampleWaves + wave;
+        if (c >= c1) break;
+        float x[kPer];
+        numbers(raw[0], c, x);
+#pragma unroll
+        for (int i = 1; i < kSampleHeld; ++i) raw[i - 1] = raw[i];
+        if (steps) {
+          one_by_one(counted(x, 0), x, [&](int, float v) { add_to(bin(v), v, weighed); });
+        } else {
+          const double s = of_lane(wave_upto(sum_of(x, 0)), 63);
+          if (lane == 0) {
+            m.sum[c] = s;
+            if (a.parts > 1) sums_at(r)[c] = s;
+          }
+        }
+      }
+    }
+    if (steps && a.parts > 1) {
+      __syncthreads();
+      if (weighed) mass_at(r, part)[tid] = m.mass[tid];
+      counts_at(r, part)[tid] = m.count[tid];
+    }
+  }
+
+  // Row r, whose parts are known.
+  __device__ __forceinline__ void finish(int r) {
+    if (a.parts > 1) {
+      for (int c = tid; c < a.chunks; c += kSampleThreads) m.top[c] = tops_at(r)[c];
+      if (tid < kSampleParts) {
+        m.part_top[tid] = -INFINITY;
+        m.part_left[tid] = 0;
+      }
+      __syncthreads();
+      if (tid < a.parts) {
+        float t = -INFINITY;
+#pragma unroll 8
+        for (int i = 0; i < a.part_chunks; ++i) t = fmaxf(t, tid * a.part_chunks + i < a.chunks ? m.top[tid * a.part_chunks + i] : -INFINITY);
+        m.part_top[tid] = t;
+      }
+      __syncthreads();
+      const float top = wave_max<64>(fmaxf(m.part_top[lane], m.part_top[lane + 64]));
+      if (greedy) most = top;
+      else against(top);
+      if (tid < a.parts && !greedy) {
+        const float t = m.part_top[tid];
+        const double off = t == top ? 0.0 : place - floor((double)t * grid), y = bits(t);  // (NaN beside an infinity: none of it)
+        m.part_off[tid] = t > -INFINITY && off < kSampleSteps ? (int)off : kSampleSteps;
+        m.part_weight[tid] = t > -INFINITY && y >= -kSampleBits ? weight(y) : 0.0;
+      }
+      __syncthreads();
+      if (steps) {
+        uint32_t n = 0;
+        uint64_t w = 0;
+#pragma unroll 8
+        for (int q = 0; q < a.parts; ++q) {
+          const int at = tid - m.part_off[q];
+          const uint32_t c = counts_at(r, q)[at > 0 ? at : 0];
+          const uint64_t v = weighed ? mass_at(r, q)[at > 0 ? at : 0] : 0;
+          n += at >= 0 ? c : 0;
+          w += at >= 0 ? scaled(v, m.part_weight[q]) : 0;
+        }
+        m.count[tid] = n;
+        m.mass[tid] = w;
+      } else if (all) {
+        for (int c = tid; c < a.chunks; c += kSampleThreads) {
+          // (a chunk whose largest is nothing beside the row's has no part in it, nor is its sum weighed)
+          const double s = sums_at(r)[c];
+          m.sum[c] = counted(m.top[c], 0) ? s * m.part_weight[c / a.part_chunks] : 0.0;
+        }
+      }
+    }
     __syncthreads();
     if (!(most > -INFINITY)) {
       if (tid == 0) {
@@ -360,153 +753,143 @@ struct Sampler {
       }
       return;
     }
-    const float temperature = a.temperature ? a.temperature[r] : 1.f;
-    const float mp = a.min_p ? a.min_p[r] : 0.f;
-    const bool greedy = !a.random || !(temperature > 0.f) || mp > 1.f;  // (nothing weighs more than the largest)
-    key = 0;
-    upto = 0x7fffffff;
-    least_weight = 0;
-    step = 1.4426950408889634074 / (double)temperature;
-    bins = fminf((float)(step * ((kSampleSteps - 1) / kSampleBits)), -kLowest);
     if (greedy) {
-      key = order_key(most);
-      step = 1;
-      bins = 1.f;
-      upto = nth_equal(1);
-    } else {
-      const int k = a.top_k ? a.top_k[r] : 0;
-      const float p = a.top_p ? a.top_p[r] : 1.f;
-      if (mp > 0.f) least_weight = (double)mp;
-      const bool by_count = k > 0 && k < a.n, by_mass = p < 1.f;
-      shift = 62 - (32 - __builtin_clz(a.n));
-      if (by_count || by_mass) {
-        for (int i = tid; i < kSampleSteps; i += kSampleThreads) {
-          m.count[i] = 0;
-          m.mass[i] = 0;
-        }
-        __syncthreads();
-        uint32_t n = 0;
-        uint64_t all = 0;
-        each(kLowest, [&](int, int at, const float(&x)[kPer]) {
+      if (tid == 0) m.found = kSampleChunks;
+      __syncthreads();
+      for (int c = tid; c < a.chunks; c += kSampleThreads)
+        if (m.top[c] == most) atomicMin(&m.found, c);
+      __syncthreads();
+      if (wave != 0) return;
+      const int c = m.found;
+      float y[kPer];
+      load(c, y);
+      int at = kPer;
 #pragma unroll
-          for (int i = 0; i < kPer; ++i) {
-            const double y = bits(x[i]);
-            if (counted(x[i], at + i)) {
-              const int b = bin(x[i]);
-              ++n;
-              atomicAdd(&m.count[b], 1u);
-              if (by_mass) {
-                const uint64_t w = whole(exp2(y));
-                all += w;
-                atomicAdd((unsigned long long*)&m.mass[b], (unsigned long long)w);
-              }
-            }
-          }
-        });
-        n = wave_upto(n);
-        all = wave_upto((unsigned long long)all);
-        if (lane == 63) {
-          m.wave_c[wave] = n;
-          m.wave_m[wave] = all;
+      for (int i = kPer - 1; i >= 0; --i) at = y[i] == most ? i : at;
+      const uint64_t lanes = __ballot(at < kPer);
+      if (lane == __builtin_ctzll(lanes)) {
+        a.word[r] = first_of(c) + at;
+        if (a.chance) a.chance[r] = 1.f;
+      }
+      return;
+    }
+    // ---- the threshold: of the count, then of the weight
+    const uint32_t lowest = key;
+    below = kSampleSteps;
+    listed = 0;
+#pragma unroll 1
+    for (int turn = 0; turn < 2; ++turn) {
+      if (!(turn ? by_mass : by_count)) continue;
+      uint64_t want = 0;
+      if (turn) {
+        if (key != lowest || upto != 0x7fffffff) {
+          // the k largest by themselves
+          __syncthreads();
+          clear_steps();
+          __syncthreads();
+          each(of_key(key), [&](int, int first, const float(&x)[kPer]) { one_by_one(counted(x, first), x, [&](int, float v) { add_to(bin(v), v, true); }); });
+          __syncthreads();
         }
+        uint64_t sum;
+        (void)in_front(m.mass[tid], m.wave_m, &sum);
         __syncthreads();
-        n = 0;
-        all = 0;
-        for (int w = 0; w < kSampleWaves; ++w) {
-          n += m.wave_c[w];
-          all += m.wave_m[w];
+        want = part_of(p, sum);
+      }
+      front(turn, k, want, weighed && a.parts > 1 && (turn || !by_mass));
+    }
+    if (mp > 0.f) leave((double)temperature * log((double)mp), (double)mp);
+    float u = a.random[r];
+    u = u >= 0.f ? u : 0.f;
+    // ---- the weights that are left, and where their sum passes the random number
+    if (listed) {
+      pick(r, u);
+      return;
+    }
+    double skipped = 0, more = 0;  // weights of the parts in front of the one that is looked at, and of all others
+    int c0_left = 0, c1_left = a.chunks;
+    if (weighed && a.parts > 1 && below >= 0 && !(mp > 0.f) && u >= 0x1p-40f) {
+      // The histograms say what is left of each part (weights below 2^-46 as nothing, which the random number is not), and so in which part the sum passes.
+      for (int q = wave; q < a.parts; q += kSampleWaves) {
+        const int off = m.part_off[q], end = below - off;
+        const double f = m.part_weight[q];
+        uint64_t w = 0;
+#pragma unroll 8
+        for (int i = 0; i < kSampleSteps / 64; ++i) {
+          const uint64_t v = mass_at(r, q)[i * 64 + lane];
+          w += i * 64 + lane < end ? scaled(v, f) : 0;
         }
-        __syncthreads();
-        const bool fewer = by_count && k < (int)n;
-        if (fewer) front<false>(k, 0);
-        if (by_mass) {
-          if (fewer) {
-            // the k largest by themselves (the search by bits may have taken the histogram's place, too)
-            all = 0;
-            for (int i = tid; i < kSampleSteps; i += kSampleThreads) {
-              m.count[i] = 0;
-              m.mass[i] = 0;
-            }
-            __syncthreads();
-            each(of_key(key), [&](int, int at, const float(&x)[kPer]) {
-#pragma unroll
-              for (int i = 0; i < kPer; ++i) {
-                if (counted(x[i], at + i)) {
-                  const uint64_t w = whole(exp2(bits(x[i])));
-                  all += w;
-                  atomicAdd(&m.count[bin(x[i])], 1u);
-                  atomicAdd((unsigned long long*)&m.mass[bin(x[i])], (unsigned long long)w);
-                }
-              }
-            });
-            all = wave_upto((unsigned long long)all);
-            if (lane == 63) m.wave_m[wave] = all;
-            __syncthreads();
-            all = 0;
-            for (int w = 0; w < kSampleWaves; ++w) all += m.wave_m[w];
-            __syncthreads();
-          }
-          front<true>(0, part_of(p, all));
-        }
+        w = of_lane(wave_upto(w), 63);
+        if (lane == 0) atomicAdd((unsigned long long*)&m.part_left[q], (unsigned long long)w);
+      }
+      __syncthreads();
+      const double per = 1.0 / two_to_shift;
+      const uint64_t left0 = lane < a.parts ? m.part_left[lane] : 0, left1 = lane + 64 < a.parts ? m.part_left[lane + 64] : 0;
+      const uint64_t upto0 = wave_upto(left0), all0 = of_lane(upto0, 63), upto1 = all0 + wave_upto(left1), sum = of_lane(upto1, 63);
+      const double target = (double)u * (double)sum;
+      const uint64_t hit0 = __ballot((double)upto0 > target && left0), hit1 = __ballot((double)upto1 > target && left1);
+      const int q = hit0 ? __builtin_ctzll(hit0) : hit1 ? 64 + __builtin_ctzll(hit1) : -1;
+      if (q >= 0) {
+        const uint64_t upto_q = q < 64 ? of_lane(upto0, q) : of_lane(upto1, q - 64), left_q = q < 64 ? of_lane(left0, q) : of_lane(left1, q - 64);
+        skipped = (double)(upto_q - left_q) * per;
+        more = (double)(sum - left_q) * per;
+        c0_left = q * a.part_chunks;
+        c1_left = c0_left + a.part_chunks < a.chunks ? c0_left + a.part_chunks : a.chunks;
       }
     }
-    // ---- the kept weights, and where their sum passes the random number
-    for (int c = tid; c < kSampleChunks; c += kSampleThreads) m.sum[c] = 0;
-    __syncthreads();
-    each(key ? of_key(key) : kLowest, [&](int c, int at, const float(&x)[kPer]) {
-      double s = 0;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) s += kept(x[i], at + i);
-      s = __shfl(wave_upto(s), 63);
-      if (lane == 0) m.sum[c] = s;
-    });
-    __syncthreads();
-    float u = a.random ? a.random[r] : 0.f;
-    u = u >= 0.f ? u : 0.f;
+    if (!all) {
+      __syncthreads();
+      for (int c = tid; c < a.chunks; c += kSampleThreads) m.sum[c] = 0;
+      __syncthreads();
+      each(of_key(key), [&](int c, int first, const float(&x)[kPer]) {
+        const double s = of_lane(wave_upto(sum_of(x, first)), 63);
+        if (lane == 0) m.sum[c] = s;
+      }, c0_left, c1_left);
+      __syncthreads();
+    }
     double before, total;
-    const int c = chunk_at<false>((double)u, 0, &before, &total);
+    const int c = chunk_at<false>((double)u, skipped * -1.0 + (double)u * more, &before, &total);
+    total += more;
     if (wave == 0) {
       float x[kPer];
       load(c, x);
-      double w[kPer], mine = 0;
-      int last = -1;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        w[i] = kept(x[i], c * kSampleChunk + lane * kPer + i);
-        mine += w[i];
-        if (w[i] > 0) last = i;
-      }
-      double sum = before + (wave_upto(mine) - mine);
-      int hit = -1;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        sum += w[i];
-        if (hit < 0 && w[i] > 0 && sum > (double)u * total) hit = i;
-      }
-      uint64_t lanes = __ballot(hit >= 0);
-      // (none, where roundings of the two sums differ, or the random number is 1: the last that is kept)
+      const int first = first_of(c);
+      const double mine = sum_of(x, first), target = (double)u * total;
+      double sum = skipped + before + (wave_upto(mine) - mine), hit_weight = 0, last_weight = 0;
+      int hit = -1, last = -1;
+      one_by_one(counted(x, first), x, [&](int i, float v) {
+        last = i;
+        last_weight = weight(bits(v));
+        sum += last_weight;
+        if (hit < 0 && sum > target) {
+          hit = i;
+          hit_weight = last_weight;
+        }
+      });
+      // (none, where roundings of the two sums differ, or the random number is 1: the last that is left)
+      const uint64_t lanes = __ballot(hit >= 0);
       const int l = lanes ? __builtin_ctzll(lanes) : 63 - __builtin_clzll(__ballot(last >= 0));
       if (lane == l) {
-        const int i = lanes ? hit : last;
-        a.word[r] = c * kSampleChunk + lane * kPer + i;
-        double weight = 0;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) weight = e == i ? w[e] : weight;
-        if (a.chance) a.chance[r] = (float)(weight / total);
+        a.word[r] = first + (lanes ? hit : last);
+        if (a.chance) a.chance[r] = (float)((lanes ? hit_weight : last_weight) / total);
       }
     }
   }
 };
 
 static_assert(sizeof(SampleLds) == kSampleLds, "what the host asks for");
-template <bool BF16>
+// FINISH: a workgroup a row, whose parts other workgroups have looked at (or which is its only part itself); else a workgroup a part.
+template <bool BF16, bool FINISH>
 __device__ __forceinline__ void sample_body(const SampleArgs& a) {
   extern __shared__ double smem_sample[];
   Sampler<BF16> s{a, *(SampleLds*)smem_sample};
   s.tid = threadIdx.x;
   s.lane = threadIdx.x & 63;
   s.wave = uniform(threadIdx.x >> 6);
-  s.run(blockIdx.x);
+  const int r = FINISH ? blockIdx.x : blockIdx.x / a.parts;
+  s.wishes(r);
+  if (!FINISH) s.part(r, blockIdx.x - r * a.parts);
+  else if (a.parts == 1) s.part(r, 0);
+  if (FINISH) s.finish(r);
 }
 
 }  // namespace daris

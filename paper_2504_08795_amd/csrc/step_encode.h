@@ -35,7 +35,8 @@ struct StepTable {
   const AqlKernel* tree_append[2][3] = {};
   const AqlKernel* tree_narrow[2][3] = {};
   const AqlKernel* tree_wide[2][3] = {};
-  const AqlKernel* sample[2] = {};  // [bf16]
+  const AqlKernel* sample[2] = {};        // [bf16]
+  const AqlKernel* sample_parts[2] = {};  // what runs in front of it for long rows
   const AqlKernel* accept = nullptr;
   const AqlKernel* keep[3] = {};    // [dim 64, 128, 256]
   const AqlKernel* copy[3] = {};
@@ -72,6 +73,7 @@ inline std::string StepTable::resolve(const AqlRuntime& rt) {
       if (d < 2) tree_wide[b][d] = find("daris::step_attend_tree_wide<%s, %d>", tf[b], 64 << d);
     }
     sample[b] = find("daris::step_sample<%s>", tf[b]);
+    sample_parts[b] = find("daris::step_sample_parts<%s>", tf[b]);
   }
   accept = find("%s", "daris::step_accept");
   for (int d = 0; d < 3; ++d) {
@@ -430,16 +432,29 @@ inline std::string encode_matvec(const StepTable& t, const daris_matvec& o, int 
   return set_grid(l, t.matvec[type][g], (int64_t)a.wgs * blocks * a.shares, waves * 64, lds(a.steps, 1 << a.across, a.share_steps)) ? "" : kTooMany;
 }
 
-inline std::string encode_sample(const StepTable& t, const daris_sample& o, StepLaunch* l) {
-  const int bf16 = o.dtype == DARIS_BF16, vec = bf16 ? 8 : 4;
+inline std::string encode_sample(const StepTable& t, const daris_sample& o, int n_cu, StepLaunch* first, StepLaunch* l) {
+  const int bf16 = o.dtype == DARIS_BF16;
   SampleArgs a = {};
   a.logits = o.logits; a.temperature = o.temperature; a.top_p = o.top_p; a.min_p = o.min_p; a.top_k = o.top_k;
   a.random = o.random; a.word = o.word; a.chance = o.chance;
   a.row = o.logits_row;
   a.rows = o.rows; a.n = o.n;
-  a.vec = aligned_to(o.logits, 16) && (o.rows == 1 || o.logits_row % vec == 0);
   a.chunks = (o.n + kSampleChunk - 1) / kSampleChunk;
+  // A chunk for each wave of a part, two where that makes more workgroups than the CUs hold.
+  a.part_chunks = (int64_t)o.rows * ((a.chunks + kSampleWaves - 1) / kSampleWaves) > 2 * n_cu ? 2 * kSampleWaves : kSampleWaves;
+  a.parts = (a.chunks + a.part_chunks - 1) / a.part_chunks;
+  if (a.parts > 1) {
+    a.row_floats = sample_floats(a.chunks, a.parts);
+    l->part_at = offsetof(SampleArgs, part);
+    l->part_bytes = (size_t)(o.rows * a.row_floats) * sizeof(float);
+  }
+  const int64_t groups = (int64_t)o.rows * a.parts;
+  if (groups > 0xffffff) return kTooMany;
   set_args(l, a);
+  if (a.parts > 1) {
+    *first = *l;
+    if (!set_grid(first, t.sample_parts[bf16], groups, kSampleWaves * 64, kSampleLds)) return kTooMany;
+  }
   return set_grid(l, t.sample[bf16], o.rows, kSampleWaves * 64, kSampleLds) ? "" : kTooMany;
 }
 
@@ -491,9 +506,10 @@ inline std::string check_step(const daris_op& op) {
   return text("kind %d is no operator", op.kind);
 }
 
-// An operator that check_step takes, as a launch on a partition of n_cu CUs: "" (l->groups == 0: it has no rows) or why it cannot be.
-inline std::string encode_step(const StepTable& t, const daris_op& op, int n_cu, StepLaunch* l) {
-  l->groups = 0;
+// An operator that check_step takes, as a launch on a partition of n_cu CUs: "" (l->groups == 0: it has no rows) or why it cannot be.  first: one that runs in front of
+// it (first->groups == 0: none does).
+inline std::string encode_step(const StepTable& t, const daris_op& op, int n_cu, StepLaunch* first, StepLaunch* l) {
+  first->groups = l->groups = 0;
   l->part_bytes = l->counters = 0;
   switch (op.kind) {
     case DARIS_STEP_NORM: return op.u.norm.rows ? encode_norm(t, op.u.norm, l) : "";
@@ -508,7 +524,7 @@ inline std::string encode_step(const StepTable& t, const daris_op& op, int n_cu,
       const daris_tree_attend& o = op.u.tree_attend;
       return o.attend.n_rows && o.attend.cache.n_seqs ? encode_attend(t, o.attend, n_cu, l, {o.tree, o.tree_words}) : "";
     }
-    case DARIS_STEP_SAMPLE: return op.u.sample.rows ? encode_sample(t, op.u.sample, l) : "";
+    case DARIS_STEP_SAMPLE: return op.u.sample.rows ? encode_sample(t, op.u.sample, n_cu, first, l) : "";
     case DARIS_STEP_ACCEPT: return op.u.accept.n_seqs ? encode_accept(t, op.u.accept, l) : "";
     case DARIS_STEP_KEEP: return op.u.keep.n_rows && op.u.keep.cache.n_seqs ? encode_keep(t, op.u.keep, l) : "";
     case DARIS_STEP_COPY: return op.u.copy.n && op.u.copy.cache.n_pages ? encode_copy(t, op.u.copy, l) : "";
@@ -516,11 +532,15 @@ inline std::string encode_step(const StepTable& t, const daris_op& op, int n_cu,
   return "";
 }
 
+inline std::string encode_step(const StepTable& t, const daris_op& op, int n_cu, StepLaunch* l) {
+  StepLaunch first;
+  return encode_step(t, op, n_cu, &first, l);
+}
+
 // The launch's places in the workspace.
 inline void place_step(StepLaunch* l, void* part, uint32_t* counters) {
-  if (!l->counters) return;
-  std::memcpy(l->args + l->part_at, &part, sizeof part);
-  std::memcpy(l->args + l->count_at, &counters, sizeof counters);
+  if (l->part_bytes) std::memcpy(l->args + l->part_at, &part, sizeof part);
+  if (l->counters) std::memcpy(l->args + l->count_at, &counters, sizeof counters);
 }
 
 }  // namespace daris

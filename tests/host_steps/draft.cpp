@@ -25,6 +25,7 @@ int main() {
       t.copy[d] = &kernels[6];
     }
     t.sample[b] = &kernels[4];
+    t.sample_parts[b] = &kernels[0];
   }
   t.accept = &kernels[7];
   char* const some = reinterpret_cast<char*>(uintptr_t(1) << 20);  // an address that nothing reads
@@ -91,8 +92,8 @@ int main() {
       o.tree = reinterpret_cast<uint64_t*>(some);
     }
     std::string e = check_step(op);
-    StepLaunch l;
-    if (e.empty()) e = encode_step(t, op, n_cu, &l);
+    StepLaunch first, l;
+    if (e.empty()) e = encode_step(t, op, n_cu, &first, &l);
     if (!e.empty()) {
       printf("error %s\n", e.c_str());
       continue;
@@ -102,7 +103,7 @@ int main() {
     } else if (what == "sample") {
       SampleArgs a;
       std::memcpy(&a, l.args, sizeof a);
-      printf(" %d %d", a.vec, a.chunks);
+      printf(" %u %d %d %d", first.groups, a.parts, a.part_chunks, a.chunks);
     } else if (what == "copy") {
       CopyArgs a;
       std::memcpy(&a, l.args, sizeof a);

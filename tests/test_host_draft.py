@@ -35,9 +35,11 @@ def test_descriptors_are_laid_out_as_in_c(encode):
 
 
 def test_launches_cover_their_work(encode):
-    for rows, n, dtype, offset, row, vec in ((1, 50001, 0, 0, 50001, 1), (2, 50001, 0, 0, 50001, 0), (64, 131072, 1, 0, 131072, 1), (3, 7, 1, 2, 8, 0), (5, 512, 0, 16, 516, 1), (1, 1 << 20, 1, 0, 0, 1)):
-        p = encode(("sample", rows, n, dtype, offset, row))[0]
-        assert p[0] == 4 and p[1] * 1 >= rows and p[3] <= 160 * 1024 and p[-2] == vec and p[-1] == -(-n // 512), p
+    for rows, n, dtype, offset, row in ((1, 50001, 0, 0, 50001), (2, 50001, 0, 0, 50001), (64, 131072, 1, 0, 131072), (3, 7, 1, 2, 8), (5, 512, 0, 16, 516), (1, 1 << 20, 1, 0, 0), (5000, 30000, 1, 0, 30000), (9, 16384, 0, 4, 16385)):
+        kernel, groups, threads, lds, part, counters, first, parts, part_chunks, chunks = encode(("sample", rows, n, dtype, offset, row))[0]
+        assert kernel == 4 and groups == rows and threads == 1024 and lds <= 80 * 1024 and counters == 0, "two workgroups a CU"
+        assert chunks == -(-n // 512) and (parts - 1) * part_chunks < chunks <= parts * part_chunks and part_chunks in (16, 32) and parts <= 128
+        assert (first, part) == ((0, 0) if parts == 1 else (rows * parts, rows * 4 * ((chunks + 1) // 2 * 2 + 2 * chunks + 3 * 1024 * parts)))
     for rows, seqs, words in ((26, 1, 1), (3000, 512, 4), (0, 3, 16)):
         assert encode(("accept", rows, seqs, words))[0][:3] == [7, seqs, 64]
     for rows, seqs, kv, dim in ((26, 1, 8, 128), (200, 7, 3, 64), (9, 9, 1, 256)):
