@@ -182,6 +182,16 @@ struct Sampler {
     fetch(chunk, &r);
     numbers(r, chunk, x);
   }
+  // f(x[i]) for all of them, in a loop that is one (the constants of eight weights at once leave half of the waves without registers)
+  template <typename F>
+  static __device__ __forceinline__ void in_turn(float (&x)[kPer], const F& f) {
+#pragma unroll 1
+    for (int i = 0; i < kPer; ++i) {
+      f(x[0]);
+#pragma unroll
+      for (int e = 1; e < kPer; ++e) x[e - 1] = x[e];
+    }
+  }
   // f(i, x[i]) for the set bits of `on`, lowest first, a lane after its own
   template <typename F>
   static __device__ __forceinline__ void one_by_one(uint32_t on, const float (&x)[kPer], const F& f) {
@@ -681,9 +691,13 @@ struct Sampler {
 #pragma unroll
         for (int i = 1; i < kSampleHeld; ++i) raw[i - 1] = raw[i];
         if (steps) {
-          one_by_one(counted(x, 0), x, [&](int, float v) { add_to(bin(v), v, weighed); });
+          in_turn(x, [&](float v) {
+            if (counted(v, 0)) add_to(bin(v), v, weighed);
+          });
         } else {
-          const double s = of_lane(wave_upto(sum_of(x, 0)), 63);
+          double s = 0;
+          in_turn(x, [&](float v) { s += counted(v, 0) ? weight(bits(v)) : 0.0; });
+          s = of_lane(wave_upto(s), 63);
           if (lane == 0) {
             m.sum[c] = s;
             if (a.parts > 1) sums_at(r)[c] = s;
@@ -727,13 +741,23 @@ struct Sampler {
       if (steps) {
         uint32_t n = 0;
         uint64_t w = 0;
-#pragma unroll 8
-        for (int q = 0; q < a.parts; ++q) {
-          const int at = tid - m.part_off[q];
-          const uint32_t c = counts_at(r, q)[at > 0 ? at : 0];
-          const uint64_t v = weighed ? mass_at(r, q)[at > 0 ? at : 0] : 0;
-          n += at >= 0 ? c : 0;
-          w += at >= 0 ? scaled(v, m.part_weight[q]) : 0;
+        constexpr int TOGETHER = 8;  // (parts whose numbers travel together, those behind the last repeating it)
+        for (int q0 = 0; q0 < a.parts; q0 += TOGETHER) {
+          uint32_t c[TOGETHER];
+          uint64_t v[TOGETHER];
+#pragma unroll
+          for (int i = 0; i < TOGETHER; ++i) {
+            const int q = q0 + i < a.parts ? q0 + i : a.parts - 1, at = tid - m.part_off[q];
+            c[i] = counts_at(r, q)[at > 0 ? at : 0];
+            v[i] = weighed ? mass_at(r, q)[at > 0 ? at : 0] : 0;
+          }
+#pragma unroll
+          for (int i = 0; i < TOGETHER; ++i) {
+            const int q = q0 + i < a.parts ? q0 + i : a.parts - 1;
+            const bool in = q0 + i < a.parts && tid >= m.part_off[q];
+            n += in ? c[i] : 0;
+            if (weighed) w += in ? scaled(v[i], m.part_weight[q]) : 0;
+          }
         }
         m.count[tid] = n;
         m.mass[tid] = w;
