@@ -19,11 +19,12 @@ __device__ __forceinline__ void keep_body(const KeepArgs& a) {
   end = end < rows ? end : rows;
   const int32_t* path = a.path + row0;
   // The first entry that moves a token, and the first that names none (it is not behind the one in front of it, or no row of the step).
-  int first = end;
+  int first = end, early = 0;  // (early: the lane's entry of the first 64)
   for (int j0 = 0; j0 < end; j0 += 64) {
     const int j = j0 + lane;
     const bool in = j < end;
     const int p = in ? path[j] : 0, q = in && j > 0 ? path[j - 1] : -1;
+    if (j0 == 0) early = p;
     const uint64_t wrong = __ballot(in && (p <= q || p >= rows));
     if (wrong) end = j0 + __builtin_ctzll(wrong);
     const uint64_t moves = __ballot(in && p != j);
@@ -40,7 +41,8 @@ __device__ __forceinline__ void keep_body(const KeepArgs& a) {
     const int part = (int)(t0 % kPage) / kScaleTokens, slot = lane & 15;
     const int64_t t = t0 + slot, j = t - before;
     bool move = j >= first && j < end;
-    const int64_t from = (int64_t)before + (move ? path[j] : 0);
+    const int entry = __shfl(early, (int)j & 63);
+    const int64_t from = (int64_t)before + (!move ? 0 : j < 64 ? entry : path[j]);
     int from_page = move ? page_of(a.c, s, (int)(from / kPage)) : -1, from_slot = (int)(from % kPage);
     move = from_page >= 0;
     const int64_t to_head = (int64_t)page * a.c.kv_heads + head;
@@ -119,14 +121,14 @@ __device__ __forceinline__ void copy_body(const CopyArgs& a) {
   const int64_t at = (int64_t)piece * kCopyPiece + tid * 16;
   u32x4 x[N];
 #pragma unroll
-  for (int j = 0; j < N; ++j) x[j] = *(const u32x4*)(src + (at + j * 4096 < bytes ? at + j * 4096 : tid * 16));  // (no branch: they travel together)
+  for (int j = 0; j < N; ++j) x[j] = __builtin_nontemporal_load((const u32x4*)(src + (at + j * 4096 < bytes ? at + j * 4096 : tid * 16)));  // (no branch: they travel together)
   const uint32_t* s_src = (const uint32_t*)(values ? a.c.v_scale : a.c.k_scale) + (int64_t)from * a.c.kv_heads;
   uint32_t* s_dst = (uint32_t*)(values ? a.c.v_scale : a.c.k_scale) + (int64_t)to * a.c.kv_heads;
   if (piece == 0)
     for (int h = tid; h < a.c.kv_heads; h += 256) s_dst[h] = s_src[h];
 #pragma unroll
   for (int j = 0; j < N; ++j)
-    if (at + j * 4096 < bytes) *(u32x4*)(dst + at + j * 4096) = x[j];
+    if (at + j * 4096 < bytes) __builtin_nontemporal_store(x[j], (u32x4*)(dst + at + j * 4096));
 }
 
 }  // namespace daris

@@ -34,7 +34,7 @@ struct StepTable {
   // ... where the step's rows are nodes of trees
   const AqlKernel* tree_append[2][3] = {};
   const AqlKernel* tree_narrow[2][3] = {};
-  const AqlKernel* tree_wide[2][3] = {};
+  const AqlKernel* tree_wide[2][3] = {};  // (none of 256, nor of 128 in fp32)
   const AqlKernel* sample[2] = {};        // [bf16]
   const AqlKernel* sample_parts[2] = {};  // what runs in front of it for long rows
   const AqlKernel* accept = nullptr;
@@ -70,7 +70,7 @@ inline std::string StepTable::resolve(const AqlRuntime& rt) {
       if (d < 2) wide[b][d] = find("daris::step_attend_wide<%s, %d>", tf[b], 64 << d);
       tree_append[b][d] = find("daris::step_append_tree<%s, %d>", tf[b], 64 << d);
       tree_narrow[b][d] = find("daris::step_attend_tree_narrow<%s, %d>", tf[b], 64 << d);
-      if (d < 2) tree_wide[b][d] = find("daris::step_attend_tree_wide<%s, %d>", tf[b], 64 << d);
+      if (d == 0 || (b && d == 1)) tree_wide[b][d] = find("daris::step_attend_tree_wide<%s, %d>", tf[b], 64 << d);
     }
     sample[b] = find("daris::step_sample<%s>", tf[b]);
     sample_parts[b] = find("daris::step_sample_parts<%s>", tf[b]);

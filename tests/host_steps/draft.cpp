@@ -20,7 +20,7 @@ int main() {
     for (int d = 0; d < 3; ++d) {
       t.tree_append[b][d] = &kernels[1];
       t.tree_narrow[b][d] = &kernels[2];
-      if (d < 2) t.tree_wide[b][d] = &kernels[3];
+      if (d == 0 || (b && d == 1)) t.tree_wide[b][d] = &kernels[3];
       t.keep[d] = &kernels[5];
       t.copy[d] = &kernels[6];
     }

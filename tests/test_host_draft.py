@@ -53,6 +53,8 @@ def test_launches_cover_their_work(encode):
     assert p[0] == 1 and p[-3] == (1000 // 16 + 40) * 3 and p[-2] == 2000 and p[-1] == 2
     narrow, wide = encode(("attend", 64, 4, 32, 8, 128, 1, 1, 256), ("attend", 64 * 32, 32, 32, 8, 128, 1, 4, 256))
     assert narrow[0] == 2 and wide[0] == 3 and wide[-1] == 4
+    for dtype, dim, kernel in ((D.FP32, 64, 3), (D.FP32, 128, 2), (D.BF16, 128, 3), (D.BF16, 256, 2)):
+        assert encode(("attend", 64 * 32, 32, 32, 8, dim, dtype, 1, 256))[0][0] == kernel
 
 
 def test_operators_without_rows_are_no_launches(encode):
