@@ -293,10 +293,14 @@ struct Sampler {
     const T upto_me = wave_upto(v);
     if (lane == 63) v_wave[wave] = upto_me;
     __syncthreads();
+    return waves_in_front(upto_me - v, v_wave, all);
+  }
+  template <typename T>
+  __device__ __forceinline__ T waves_in_front(T in_wave, const T* v_wave, T* all) const {
     const T waves = row_upto(v_wave[lane & (kSampleWaves - 1)]);
     *all = of_lane(waves, kSampleWaves - 1);
     const T before = of_lane(waves, wave > 0 ? wave - 1 : 0);
-    return (wave > 0 ? before : T(0)) + (upto_me - v);
+    return (wave > 0 ? before : T(0)) + in_wave;
   }
 
   // What the parts of a row leave: [row][chunks] floats, their largest, in front; [row][chunks] sums; [row][part] histograms.
@@ -390,10 +394,17 @@ struct Sampler {
     if (tid == 0) m.found = -1;
     const uint32_t c = m.count[tid];
     const uint64_t w = m.mass[tid];
+    const uint32_t c_upto = wave_upto(c);
+    const uint64_t w_upto = by_mass ? wave_upto(w) : 0;
+    if (lane == 63) {
+      m.wave_c[wave] = c_upto;
+      m.wave_m[wave] = w_upto;
+    }
+    __syncthreads();
     uint32_t c_all;
-    uint64_t w_all;
-    const uint32_t c_base = in_front(c, m.wave_c, &c_all);
-    const uint64_t w_base = in_front(w, m.wave_m, &w_all);
+    uint64_t w_all = 0, w_base = 0;
+    const uint32_t c_base = waves_in_front(c_upto - c, m.wave_c, &c_all);
+    if (by_mass) w_base = waves_in_front(w_upto - w, m.wave_m, &w_all);
     if (!by_mass && whole_row && want_count >= c_all) want_count = 0;
     want_count = want_count < c_all ? want_count : c_all;
     want_mass = want_mass < w_all ? want_mass : w_all;

@@ -329,7 +329,9 @@ inline std::string encode_attend(const StepTable& t, const daris_attend& o, int 
   // with narrow and with wide tiles, bf16 and fp32.  Heads of 64: 16 x 48 rows (1536 narrow tiles) 38 and 43, 53 and 59; 8 x 128 (2048) 53 and 49, 81 and 70.  Heads of
   // 128: 16 x 24 (768) 41 and 43, 47 and 75; 8 x 64 (1024) 61 and 53, 71 and 100; 1 x 1024 (2048) 208 and 117, 240 and 243; 1 x 2048 444 and 203, 510 and 457; fp32's wide tiles have a CU for
   // themselves.  64 x 4 rows, which fill an eighth of wide tiles: 33 and 42.
-  const int full = o.cache.dim == 64 ? 6 : bf16 ? 3 : 8;
+  // Of trees the last wide tile of each sequence is part empty: 16 of up to 100 nodes behind up to 4000 tokens, bf16 heads of 64 (1600 narrow tiles) 53 and 70, 32 of 128 behind 2500
+  // (4100) 78 and 68.
+  const int full = o.cache.dim == 64 ? (tree.mask ? 10 : 6) : bf16 ? 3 : 8;
   const AqlKernel* const narrow_kernel = (tree.mask ? t.tree_narrow : t.narrow)[bf16][d];
   const AqlKernel* const wide_kernel = (tree.mask ? t.tree_wide : t.wide)[bf16][d];
   const bool wide = columns * o.cache.dim >= 4096 * (int64_t)o.cache.n_seqs && columns * o.cache.kv_heads > (int64_t)full * kNarrowColumns * n_cu && wide_kernel;
