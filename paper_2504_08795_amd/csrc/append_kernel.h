@@ -68,7 +68,8 @@ __device__ __forceinline__ int position_of(const TreeMasks& tree, int row, int b
   return before + n;
 }
 
-template <bool BF16, int D, bool TREE>
+// KEYS, VALUES: what of the two this wave appends.
+template <bool BF16, int D, bool TREE, bool KEYS = true, bool VALUES = true>
 __device__ __forceinline__ void append_sixteenth(const AppendArgs& a, const TreeMasks& tree, int head, int row0, int page, int part, int lo, int hi, int pos0, int before) {
   // tokens lo .. hi - 1 of the sixteenth are rows row0 ... of the step, their places pos0 ... of the sequence
   constexpr int E = D / 64, Q = 4;  // channels of a lane; tokens that are read together
@@ -77,7 +78,7 @@ __device__ __forceinline__ void append_sixteenth(const AppendArgs& a, const Tree
   const int had_k = lo > 0 ? a.c.k_scale[ph * 4 + part] : kLeastScale, had_v = lo > 0 ? a.c.v_scale[ph * 4 + part] : kLeastScale;
 
   const int mine = lane < lo ? lo : lane < hi ? lane : hi - 1;  // (TREE: lane i has the position of token i)
-  const int position = position_of<TREE>(tree, row0 + mine - lo, before, 0);
+  const int position = KEYS ? position_of<TREE>(tree, row0 + mine - lo, before, 0) : 0;
   float xv[kScaleTokens][E];
   {  // ---- keys
     Turn t[E];
@@ -99,12 +100,12 @@ __device__ __forceinline__ void append_sixteenth(const AppendArgs& a, const Tree
         const int64_t kr = (int64_t)(row0 + in - lo) * a.k_row + head * a.k_head, vr = (int64_t)(row0 + in - lo) * a.v_row + head * a.v_head;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          own[i][e] = load_elem<BF16>(a.k, kr + lane * E + e);
-          other[i][e] = load_elem<BF16>(a.k, kr + t[e].with);
-          xv[tok][e] = load_elem<BF16>(a.v, vr + lane + 64 * e);
+          if constexpr (KEYS) own[i][e] = load_elem<BF16>(a.k, kr + lane * E + e);
+          if constexpr (KEYS) other[i][e] = load_elem<BF16>(a.k, kr + t[e].with);
+          if constexpr (VALUES) xv[tok][e] = load_elem<BF16>(a.v, vr + lane + 64 * e);
           c[i][e] = 1.f;
           s[i][e] = 0.f;
-          if (a.rot_dim) table_entry(a, t[e], TREE ? __builtin_amdgcn_readlane(position, in) : pos0 + in - lo, &c[i][e], &s[i][e]);
+          if (KEYS && a.rot_dim) table_entry(a, t[e], TREE ? __builtin_amdgcn_readlane(position, in) : pos0 + in - lo, &c[i][e], &s[i][e]);
         }
       }
 #pragma unroll
@@ -113,12 +114,13 @@ __device__ __forceinline__ void append_sixteenth(const AppendArgs& a, const Tree
         for (int e = 0; e < E; ++e) {
           const int tok = b * Q + i;
           const bool on = tok >= lo && tok < hi;
-          x[tok][e] = on ? turned(t[e], own[i][e], other[i][e], c[i][e], s[i][e]) : 0.f;
+          if constexpr (KEYS) x[tok][e] = on ? turned(t[e], own[i][e], other[i][e], c[i][e], s[i][e]) : 0.f;
           if (!on) xv[tok][e] = 0.f;
           most = fmaxf(most, size_of(x[tok][e]));
           most_v = fmaxf(most_v, size_of(xv[tok][e]));
         }
     }
+    if constexpr (KEYS) {
     const int need = scale_byte(wave_max<64>(most)), now = need > had_k ? need : had_k;
     const float inv = two_to(127 - now), shrink = two_to(had_k - now);
     uint8_t* k = a.c.k + (ph * kPage + part * kScaleTokens) * D + lane * E;
@@ -139,6 +141,8 @@ __device__ __forceinline__ void append_sixteenth(const AppendArgs& a, const Tree
       else *p = (uint8_t)w;
     }
     if (lane == 0) a.c.k_scale[ph * 4 + part] = (uint8_t)now;
+    }
+    if constexpr (!VALUES) return;
     // ---- values
     const int need_v = scale_byte(wave_max<64>(most_v)), now_v = need_v > had_v ? need_v : had_v;
     const float inv_v = two_to(127 - now_v), shrink_v = two_to(had_v - now_v);
@@ -222,7 +226,8 @@ template <bool BF16, int D, bool TREE = false>
 __device__ __forceinline__ void append_body(const AppendArgs& a, const TreeMasks& tree = {}) {
   const int wave = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (wave < a.items) {
-    const int item = wave / a.c.kv_heads, head = wave - item * a.c.kv_heads;
+    const int both = TREE ? wave >> 1 : wave;  // (of a tree, whose nodes fill sixteenths, two waves share one: see kTreeAppendWaves)
+    const int item = both / a.c.kv_heads, head = both - item * a.c.kv_heads;
     // Sequence s has the items from first_row(s) / 16 + 2 s on: n tokens lie in at most n / 16 + 2 sixteenths.
     int s = item, base = item;
     if (a.c.row_start) {
@@ -240,7 +245,13 @@ __device__ __forceinline__ void append_body(const AppendArgs& a, const TreeMasks
     const int page = page_of(a.c, s, (int)(t0 / kPage));
     if (page < 0) return;
     const int tok = (int)t0 + lo;
-    append_sixteenth<BF16, D, TREE>(a, tree, head, row0 + (tok - before), page, (int)(sixteenth % (kPage / kScaleTokens)), lo, hi, tok, before);
+    const int row = row0 + (tok - before), part = (int)(sixteenth % (kPage / kScaleTokens));
+    if constexpr (TREE) {
+      if (wave & 1) append_sixteenth<BF16, D, true, false, true>(a, tree, head, row, page, part, lo, hi, tok, before);
+      else append_sixteenth<BF16, D, true, true, false>(a, tree, head, row, page, part, lo, hi, tok, before);
+    } else {
+      append_sixteenth<BF16, D, false>(a, tree, head, row, page, part, lo, hi, tok, before);
+    }
   } else if (wave < a.items + a.q_items) {
     const int per_row = (a.q_heads + kTurnHeads - 1) / kTurnHeads;
     const int i = wave - a.items, row = i / per_row, head = (i - row * per_row) * kTurnHeads;

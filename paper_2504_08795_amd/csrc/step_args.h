@@ -49,8 +49,10 @@ struct AppendArgs {
   int items, q_items;  // sixteenths x key heads at most; (row, kTurnHeads query heads)
 };
 constexpr int kTurnHeads = 4;
+// Waves to a sixteenth of a tree's nodes: one for the keys, one for the values.
+constexpr int kTreeAppendWaves = 2;
 struct TreeAppendArgs {
-  AppendArgs append;
+  AppendArgs append;  // (items: times kTreeAppendWaves)
   TreeMasks tree;
 };
 

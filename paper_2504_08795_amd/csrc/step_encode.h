@@ -303,7 +303,7 @@ inline std::string encode_append(const StepTable& t, const daris_append& o, Step
   a.k_row = o.k_row; a.k_head = o.k_head; a.v_row = o.v_row; a.v_head = o.v_head;
   a.q_row = o.q_row; a.q_head = o.q_head; a.qo_row = o.qo_row; a.qo_head = o.qo_head;
   a.q_heads = o.q ? o.q_heads : 0; a.turn_rows = o.turn_rows; a.rot_dim = o.rot_dim; a.pairs = o.pairs;
-  const int64_t items = (o.row_start ? (int64_t)o.n_rows / kScaleTokens + 2 * (int64_t)o.cache.n_seqs : o.n_rows) * o.cache.kv_heads;
+  const int64_t items = (o.row_start ? (int64_t)o.n_rows / kScaleTokens + 2 * (int64_t)o.cache.n_seqs : o.n_rows) * o.cache.kv_heads * (tree.mask ? kTreeAppendWaves : 1);
   const int64_t q_items = (int64_t)o.n_rows * ((a.q_heads + kTurnHeads - 1) / kTurnHeads);
   if (items + q_items > 0x7fffffffll) return kTooMany;
   a.items = (int)items;

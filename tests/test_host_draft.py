@@ -50,7 +50,7 @@ def test_launches_cover_their_work(encode):
         assert p[0] == 6 and p[-1] * 16384 >= kv * 64 * dim > (p[-1] - 1) * 16384 and p[1] == 2 * n * p[-1]
     assert "workgroups" in encode(("copy", 1 << 29, 1 << 30, 8, 128))[0]
     p = encode(("append", 1000, 20, 3, 5, 128, 2))[0]
-    assert p[0] == 1 and p[-3] == (1000 // 16 + 40) * 3 and p[-2] == 2000 and p[-1] == 2
+    assert p[0] == 1 and p[-3] == (1000 // 16 + 40) * 3 * 2 and p[-2] == 2000 and p[-1] == 2
     narrow, wide = encode(("attend", 64, 4, 32, 8, 128, 1, 1, 256), ("attend", 64 * 32, 32, 32, 8, 128, 1, 4, 256))
     assert narrow[0] == 2 and wide[0] == 3 and wide[-1] == 4
     for dtype, dim, kernel in ((D.FP32, 64, 3), (D.FP32, 128, 2), (D.BF16, 128, 3), (D.BF16, 256, 2)):
