@@ -186,10 +186,11 @@ struct Sampler {
   template <typename F>
   static __device__ __forceinline__ void in_turn(float (&x)[kPer], const F& f) {
 #pragma unroll 1
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < kPer; i += 2) {
       f(x[0]);
+      f(x[1]);
 #pragma unroll
-      for (int e = 1; e < kPer; ++e) x[e - 1] = x[e];
+      for (int e = 2; e < kPer; ++e) x[e - 2] = x[e];
     }
   }
   // f(i, x[i]) for the set bits of `on`, lowest first, a lane after its own
@@ -693,6 +694,7 @@ struct Sampler {
     if (greedy) most = top;
     else against(top);
     if ((steps || all) && top > -INFINITY) {
+      const float least = of_key(key);
 #pragma unroll 1
       for (int h = 0; h < kSampleHeld; ++h) {
         const int c = c0 + h * kSampleWaves + wave;
@@ -703,11 +705,11 @@ struct Sampler {
         for (int i = 1; i < kSampleHeld; ++i) raw[i - 1] = raw[i];
         if (steps) {
           in_turn(x, [&](float v) {
-            if (counted(v, 0)) add_to(bin(v), v, weighed);
+            if (v >= least) add_to(bin(v), v, weighed);
           });
         } else {
           double s = 0;
-          in_turn(x, [&](float v) { s += counted(v, 0) ? weight(bits(v)) : 0.0; });
+          in_turn(x, [&](float v) { s += v >= least ? weight(bits(v)) : 0.0; });
           s = of_lane(wave_upto(s), 63);
           if (lane == 0) {
             m.sum[c] = s;
