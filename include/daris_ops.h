@@ -215,7 +215,8 @@ typedef struct daris_accept {
  * Keeps the tokens of some of the step's rows: token before[s] + path[row_start[s] + j] of the cache becomes token before[s] + j, for j < count[s] (at most the
  * sequence's rows; path as daris_accept leaves it).  Entries increase and name rows of the sequence; the first that does not ends the list.  before is what it was for the
  * step's append.  A sixteenth that gets tokens has the largest scale of the tokens that it then holds, and its codes are rounded again where theirs was smaller; one that gets
- * none, and what lies behind the last kept token, stays as it is.  A token whose old or new page is not there is not moved.
+ * none, and what lies behind the last kept token, stays as it is.  A token whose old or new page is not there is not moved.  No page that gets tokens may belong to two
+ * places of the table.
  */
 typedef struct daris_keep {
   daris_cache cache;
@@ -259,7 +260,7 @@ typedef int32_t daris_plan; /* handle of a planned list of operators; <0 is an e
  * wrote.  The caller's streams are synchronised first (as daris_forward does), and the results are visible to every HIP
  * stream and the host on return.  All descriptors are checked before anything is launched: DARIS_EINVAL names the first operator that is
  * wrong, and nothing has run.  Operators without rows do nothing.  Tasks may have active jobs, which go on meanwhile (those
- * that share the queue wait in line).  Attention and products keep partial results in a workspace of the partition, which grows when a call
+ * that share the queue wait in line).  Attention, products and sampling (12 KB for every 8192 or 16384 logits of a row) keep partial results in a workspace of the partition, which grows when a call
  * needs more (DARIS_ENOMEM: nothing has run) and lives until daris_shutdown. */
 daris_status daris_run_ops(const daris_op* ops, int32_t n, daris_part p);
 /* The same in two parts, for a program that runs the same list step after step: daris_plan_ops checks the descriptors and keeps

@@ -539,7 +539,7 @@ def make_append(cache, k, v, row_start=None, q=None, q_out=None, turn=None, rot_
     if tree is None:
         return _made(STEP_APPEND, a, cache, k, v, q, q_out, turn, row_start)
     _tree(tree, k.shape[0])
-    _need(k.stride()[:2] == v.stride()[:2], f"with a tree, k and v lie alike: their distances are {k.stride()[:2]} and {v.stride()[:2]}")
+    _need(all(k.shape[d] <= 1 or k.stride(d) == v.stride(d) for d in (0, 1)), f"with a tree, k and v lie alike: their distances are {k.stride()[:2]} and {v.stride()[:2]}")
     t = daris_tree_append(cache, a.k, a.v, a.q, a.q_out, a.turn, a.row_start, _at(tree), a.k_row, a.k_head, a.q_row, a.q_head, a.qo_row, a.qo_head,
                           a.n_rows, a.q_heads, a.dtype, a.turn_rows, a.rot_dim, a.pairs, tree.shape[1])
     return _made(STEP_TREE_APPEND, t, cache, k, v, q, q_out, turn, row_start, tree)

@@ -309,6 +309,24 @@ def test_equal_logits_go_by_number(part, dtype, n):
     sample_case(part, x, [0.1] * 3, temperature=[0.0] * 3)
 
 
+@pytest.mark.parametrize("dtype,n,skew", [("bf16", 131073, 1), ("fp32", 50001, 3), ("bf16", 8193, 0)])
+def test_rows_of_many_parts_at_the_ends_of_the_random_numbers(part, dtype, n, skew):
+    """A flat row and a steep one, whose words that are left are many and few; random numbers that only the smallest weights answer to."""
+    x = torch.cat([logits(2, n, dtype, 12, 0.7), logits(2, n, dtype, 13, 6.0)])
+    x[0, :20000] -= 30.0                                    # words of almost no weight in front
+    x[1] = x[1].sort().values
+    for u in (0.0, 1e-30, 2.0 ** -24, 0.5, 1 - 2.0 ** -24, 1.0):
+        for more in (dict(), dict(top_k=[n - 1] * 4), dict(top_k=[600] * 4), dict(top_k=[9000] * 4, top_p=[0.8] * 4), dict(top_p=[0.999] * 4), dict(top_p=[0.9] * 4, min_p=[1e-4] * 4), dict(min_p=[1e-6] * 4)):
+            sample_case(part, x, [u] * 4, skew=skew, **{k: [min(v, n) for v in w] for k, w in more.items()})
+
+
+def test_many_short_rows_and_none(part):
+    sample_case(part, logits(3000, 40, "bf16", 14), uniform(3000, 15), top_k=[7] * 3000)
+    sample_case(part, logits(9, 8, "fp32", 16), uniform(9, 17), top_p=[0.5] * 9)
+    word = torch.full((0,), 1, dtype=torch.int32, device="cuda")
+    run(part, D.make_sample(torch.zeros((0, 30), device="cuda"), word, torch.zeros(0, device="cuda")))
+
+
 def test_random_numbers_at_their_ends_and_between(part):
     x = torch.tensor([[0.0, 0.0, -math.inf, 0.0, 0.0, -100.0]]).repeat(9, 1)
     u = [0.0, 0.2499999, 0.25, 0.5, 0.75, 1 - 2.0 ** -24, 1.0, 7.0, float("nan")]
@@ -564,6 +582,46 @@ def test_a_drafted_step_in_one_list(part):
         for name, a, b, scales in (("k", got[0], want[0], c.k_scale), ("v", got[1], want[1], c.v_scale)):
             # scales may be larger than those of the kept tokens alone (a rejected one's): two roundings on either side
             close(a, b, 4 * e4m3_slack(b, two_to(scales)[c.pages[s][c.pages[s] >= 0].long()].max()), name)
+
+
+def test_keys_and_values_that_lie_apart(part):
+    """With a tree, k and v have the same distances; of one row or one head the distance does not count."""
+    c = Cache(95, [3], [1], 2, 64)
+    cache, tree = c.gpu(D), torch.ones((1, 1), dtype=torch.int64, device="cuda")
+    k, v = torch.randn((1, 2, 64), device="cuda"), torch.randn((1, 4, 64), device="cuda")[:, :2]
+    run(part, D.make_append(cache, k, v, row_start=c.start.cuda(), tree=tree))
+    back = [t.cpu() for t in c.on_gpu[:4]]
+    page, s = int(c.pages[0, 0]), two_to(back[3])
+    close(back[1][page, :, :, 3].double() * s[page, :, 0, None], v[0].cpu().double(), e4m3_slack(v[0].cpu().double(), s[page, :, 0, None]), "values")
+    with pytest.raises(D.DarisError):
+        D.make_append(cache, torch.zeros((2, 2, 64), device="cuda"), torch.zeros((2, 4, 64), device="cuda")[:, :2], row_start=c.start.cuda(), tree=torch.ones((2, 1), dtype=torch.int64, device="cuda"))
+    for wrong in (lambda: D.make_attend(cache, k.repeat(1, 2, 1), k.repeat(1, 2, 1), tree=tree[:, :0]), lambda: D.make_attend(cache, k, torch.empty_like(k), tree=tree.repeat(2, 1)),
+                  lambda: D.make_attend(cache, k, torch.empty_like(k), tree=tree.int()), lambda: D.make_sample(k[0], torch.zeros(2, device="cuda")), lambda: D.make_copy(cache, tree.int()),
+                  lambda: D.make_keep(cache, tree.int()[0], torch.zeros(3, dtype=torch.int32, device="cuda")), lambda: D.make_sample(k[0], torch.zeros(2, dtype=torch.int32, device="cuda"), top_k=torch.zeros(2, device="cuda"))):
+        with pytest.raises(D.DarisError) as e:
+            wrong()
+        assert e.value.code == D.EINVAL
+
+
+def test_plans_of_two_partitions_take_turns(part):
+    """Sampling of long rows and cut attention share a partition's workspace with each other, and none with another partition's."""
+    x, u = logits(6, 40000, "bf16", 96).cuda(), torch.tensor(uniform(6, 97), device="cuda")
+    words = [torch.full((6,), -5, dtype=torch.int32, device="cuda") for _ in range(2)]
+    c = Cache(98, [3000, 100], [30, 9], 1, 64).filled(99)
+    masks, q = trees(98, [30, 9]), rand((39, 4, 64), torch.bfloat16, 100, 0.3).cuda()
+    outs = [torch.zeros_like(q) for _ in range(2)]
+    cache = c.gpu(D)
+    lists = [D.make_ops([D.make_sample(x, words[i], u, top_p=torch.full((6,), 0.9, device="cuda")), D.make_attend(cache, q, outs[i], row_start=c.start.cuda(), scale=0.02, tree=masks.cuda()),
+                         D.make_sample(x, words[i], u, top_p=torch.full((6,), 0.9, device="cuda"))]) for i in range(2)]
+    want = [drawn(x[i].cpu(), float(u[i]), top_p=float(np.float32(0.9)))[0] for i in range(6)]
+    ref, slack = attend_tree(c, masks, q, 0.02, 0, "bf16")
+    for _ in range(3):
+        for i, place in ((0, part), (1, SMALL)):
+            words[i].fill_(-5)
+            outs[i].zero_()
+            D.daris_run_ops(lists[i], place)
+            assert words[i].tolist() == want
+            close(outs[i], ref, slack, "attention")
 
 
 def test_lists_that_are_not_planned_give_the_same(part):
