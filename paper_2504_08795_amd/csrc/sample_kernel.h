@@ -253,8 +253,14 @@ struct Sampler {
   // ... of a lane's numbers, a bit each
   __device__ __forceinline__ uint32_t counted(const float (&x)[kPer], int first) const {
     uint32_t on = 0;
+    const float least = of_key(key);
+    if (upto == 0x7fffffff) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) on |= counted(x[i], first + i) ? 1u << i : 0u;
+      for (int i = 0; i < kPer; ++i) on |= x[i] >= least ? 1u << i : 0u;
+      return on;
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) on |= x[i] > least || (x[i] == least && first + i <= upto) ? 1u << i : 0u;
     return on;
   }
   // Moves the threshold up to the least number that weighs `least` or more (0: anything), which is most + far but for its rounding.
