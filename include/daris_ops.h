@@ -4,6 +4,8 @@
  *
  *     norm -> product -> append -> attend -> product -> norm -> gated product -> product
  *
+ * and, behind its last product, the words that come of it: drawn from given random numbers, and accepted from trees of drafted ones (see daris_tree_append and on).
+ *
  * An operator is a descriptor that names buffers of the caller; daris_run_ops runs a list of them.  The general rules of
  * daris.h apply (status codes, nothing throws or aborts, one API thread).  In addition:
  *   - Every pointer is HIP memory of the library's GPU, aligned to its element, and stays valid until the call returns.  Channels
@@ -32,7 +34,7 @@ extern "C" {
 #endif
 
 enum { DARIS_STEP_NORM = 0, DARIS_STEP_APPEND = 1, DARIS_STEP_ATTEND = 2, DARIS_STEP_MATVEC = 3 };
-/* ... of a step whose words are drafted (see daris_tree_append and on) */
+/* ... of a step whose words are drafted (see daris_tree_append and on; 7 is none) */
 enum { DARIS_STEP_TREE_APPEND = 4, DARIS_STEP_TREE_ATTEND = 5, DARIS_STEP_SAMPLE = 6, DARIS_STEP_ACCEPT = 8, DARIS_STEP_KEEP = 9, DARIS_STEP_COPY = 10 };
 enum { DARIS_PAGE_TOKENS = 64, DARIS_SCALE_TOKENS = 16, DARIS_TREE_WORDS = 16, DARIS_SAMPLE_WORDS = 1 << 20 };
 

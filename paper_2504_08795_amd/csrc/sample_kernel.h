@@ -509,44 +509,44 @@ struct Sampler {
         }
       }
       if (few) {
-      // ---- each with each, so many threads to a word that all have one
-      int threads = 64;
-      while (threads * (int)in > kSampleThreads) threads /= 2;
-      const int word = tid / threads;
-      const bool on = word < (int)in;
-      const uint64_t own_word = on ? m.few[word] : 0;
-      if (by_mass) {
-        if (tid < (int)in) m.mass[tid] = whole(of_key((uint32_t)(m.few[tid] >> 32)));  // (the histogram has done its work)
-        __syncthreads();
-      }
-      uint32_t n = 0;
-      uint64_t w = 0;
+        // ---- each with each, so many threads to a word that all have one
+        int threads = 64;
+        while (threads * (int)in > kSampleThreads) threads /= 2;
+        const int word = tid / threads;
+        const bool on = word < (int)in;
+        const uint64_t own_word = on ? m.few[word] : 0;
+        if (by_mass) {
+          if (tid < (int)in) m.mass[tid] = whole(of_key((uint32_t)(m.few[tid] >> 32)));  // (the histogram has done its work)
+          __syncthreads();
+        }
+        uint32_t n = 0;
+        uint64_t w = 0;
 #pragma unroll 4
-      for (int o = tid & (threads - 1); o < (int)in; o += threads) {
-        const bool before = m.few[o] > own_word;
-        n += before;
-        if (by_mass) w += before ? m.mass[o] : 0;
-      }
+        for (int o = tid & (threads - 1); o < (int)in; o += threads) {
+          const bool before = m.few[o] > own_word;
+          n += before;
+          if (by_mass) w += before ? m.mass[o] : 0;
+        }
 #pragma unroll 1
-      for (int d = 1; d < threads; d *= 2) {
-        n += __shfl_xor(n, d);
-        if (by_mass) w += __shfl_xor((unsigned long long)w, d);
-      }
-      n += above;
-      w += above_mass;
-      const uint64_t own = by_mass && on ? m.mass[word] : 0;
-      // (the last, if they come to less: the histogram's sums are rounded otherwise)
-      if (on && ((by_mass ? w < want_mass && want_mass <= w + own : n + 1 == want_count) || (n + 1 == above + in && (by_mass ? w + own < want_mass : n + 1 < want_count)))) m.found_word = own_word;
-      __syncthreads();
-      key = (uint32_t)(m.found_word >> 32);
-      upto = (int)~(uint32_t)m.found_word;
-      if (sums && !with_above) {
-        below = b;
+        for (int d = 1; d < threads; d *= 2) {
+          n += __shfl_xor(n, d);
+          if (by_mass) w += __shfl_xor((unsigned long long)w, d);
+        }
+        n += above;
+        w += above_mass;
+        const uint64_t own = by_mass && on ? m.mass[word] : 0;
+        // (the last, if they come to less: the histogram's sums are rounded otherwise)
+        if (on && ((by_mass ? w < want_mass && want_mass <= w + own : n + 1 == want_count) || (n + 1 == above + in && (by_mass ? w + own < want_mass : n + 1 < want_count)))) m.found_word = own_word;
+        __syncthreads();
+        key = (uint32_t)(m.found_word >> 32);
+        upto = (int)~(uint32_t)m.found_word;
+        if (sums && !with_above) {
+          below = b;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (mine[i] >= m.found_word) atomicAdd((unsigned long long*)&m.part_left[(int)~(uint32_t)mine[i] / (a.part_chunks * kSampleChunk)], (unsigned long long)whole(of_key((uint32_t)(mine[i] >> 32))));
-      }
-      return;
+          for (int i = 0; i < N; ++i)
+            if (mine[i] >= m.found_word) atomicAdd((unsigned long long*)&m.part_left[(int)~(uint32_t)mine[i] / (a.part_chunks * kSampleChunk)], (unsigned long long)whole(of_key((uint32_t)(mine[i] >> 32))));
+        }
+        return;
       }
     }
     // ---- many: by their bits, 10, 10, 6 and 6 of them
@@ -893,7 +893,7 @@ struct Sampler {
       __syncthreads();
     }
     double before, total;
-    const int c = chunk_at<false>((double)u, skipped * -1.0 + (double)u * more, &before, &total);
+    const int c = chunk_at<false>((double)u, (double)u * more - skipped, &before, &total);
     total += more;
     if (wave == 0) {
       float x[kPer];

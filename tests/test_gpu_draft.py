@@ -650,3 +650,30 @@ def test_lists_that_are_not_planned_give_the_same(part):
     for r in results[1:]:
         for a, b in zip(results[0], r):
             assert torch.equal(a, b) or (a.dtype == torch.float32 and float((a - b).abs().max()) < 1e-4)
+
+
+def test_pages_behind_four_gigabytes(part):
+    """The last pages of a cache of 70000: what each operator does there is what it does in a small cache."""
+    kv, dim, n = 8, 128, 70000
+    c = Cache(111, [70, 130], [26, 40], kv, dim).filled(112)
+    small = c.gpu(D)
+    few = c.k.shape[0]
+    big = []
+    for t in c.on_gpu[:4]:
+        b = torch.zeros((n,) + tuple(t.shape[1:]), dtype=torch.uint8, device="cuda")
+        b[n - few:] = t.view(torch.uint8)
+        big.append(b.view(t.dtype))
+    assert big[0].numel() > 1 << 32
+    large = D.make_cache(*big, torch.where(c.pages >= 0, c.pages + n - few, c.pages).cuda(), c.on_gpu[5])
+    rows, start, masks = 66, c.start.cuda(), trees(113, [26, 40]).cuda()
+    qkv = rand((rows, 4 * kv, dim), torch.bfloat16, 114).cuda()
+    path, count = torch.tensor(some_path(np.random.default_rng(115), [26, 40], [6, 9]), dtype=torch.int32, device="cuda"), torch.tensor([6, 9], dtype=torch.int32, device="cuda")
+    outs = []
+    for cache, base, held in ((small, 0, c.on_gpu), (large, n - few, big)):
+        out = torch.empty((rows, 2 * kv, dim), dtype=torch.bfloat16, device="cuda")
+        run(part, D.make_append(cache, qkv[:, 2 * kv:3 * kv], qkv[:, 3 * kv:], row_start=start, tree=masks), D.make_attend(cache, qkv[:, :2 * kv], out, row_start=start, scale=0.05, tree=masks),
+            D.make_keep(cache, path, count, row_start=start), D.make_copy(cache, torch.tensor([[base, base + few - 1]], dtype=torch.int32, device="cuda")))
+        outs.append([out] + [t.view(torch.uint8)[base:] for t in held[:4]])
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+    assert not bool(big[0].view(torch.uint8)[:n - few].any()) and not bool(big[1].view(torch.uint8)[:n - few].any())
