@@ -141,6 +141,7 @@ struct Sampler {
   int upto;
   int listed;           // m.few has all words that are left (and others), so many
   int below;            // step of the histogram that the threshold is in, -1: the parts' sums are not known
+  bool spent;           // the row's histogram has made room for a finer one
   double two_to_shift;  // weights as whole numbers: times this; the sum of a row's stays below 2^62
 
   // A lane's numbers of a chunk as they are in memory.  They begin at `first` (the last ones of the row where it ends in front of them).
@@ -484,6 +485,7 @@ struct Sampler {
       if (in > kSampleRank / 4 && !with_above) {
         // ---- those of one of its finer steps
         int step_of[N];
+        spent = true;
         clear_steps();
         if (tid == 0) m.found_at = 0;
         __syncthreads();
@@ -553,6 +555,7 @@ struct Sampler {
     above = first_above;
     above_mass = first_mass;
     uint32_t prefix = 0, ties = 0;
+    spent = true;
 #pragma unroll 1
     for (int level = 0; level < 4; ++level) {
       const int low = level == 0 ? 22 : level == 1 ? 12 : level == 2 ? 6 : 0, width = level < 2 ? 10 : 6;
@@ -566,7 +569,7 @@ struct Sampler {
       });
       __syncthreads();
       const int d = step_at(by_mass, false, want_count - above, want_mass - above_mass, &above, &above_mass, &ties);
-      if (d < 0) return;
+      if (d < 0) return;  // (as above, of more words)
       prefix = prefix << width | (((1u << width) - 1) & ~(uint32_t)d);
     }
     const uint32_t was = key;
@@ -823,13 +826,14 @@ struct Sampler {
     const uint32_t lowest = key;
     below = kSampleSteps;
     listed = 0;
+    spent = false;
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
       if (!(turn ? by_mass : by_count)) continue;
       uint64_t want = 0;
       if (turn) {
-        if (key != lowest || upto != 0x7fffffff) {
-          // the k largest by themselves
+        if (key != lowest || upto != 0x7fffffff || spent) {
+          // the k largest by themselves (or all, where the k-th weighs nothing)
           __syncthreads();
           clear_steps();
           __syncthreads();

@@ -1,0 +1,39 @@
+"""Words of long rows whose weights lie far apart (daris_sample), against the definition in whole numbers (draft_helpers.drawn)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2504_08795_amd as D
+from draft_helpers import drawn
+from step_helpers import DT
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def part():
+    D.daris_init(0, 0, 0)
+    yield D.daris_create_partition(256)
+    D.daris_shutdown()
+
+
+def words(part, x, u, **more):
+    """The words of rows x [rows][n] by the lists u, top_k, ..., and those of the definition."""
+    f = lambda v, t=torch.float32: torch.tensor(v, dtype=t, device="cuda")  # noqa: E731
+    word = torch.full((len(x),), -7, dtype=torch.int32, device="cuda")
+    D.daris_run_ops(D.make_ops([D.make_sample(x.cuda(), word, f(u), **{k: f(v, torch.int32 if k == "top_k" else torch.float32) for k, v in more.items()})]), part)
+    single = lambda v, i: float(np.float32(v[i]))  # noqa: E731
+    return word.tolist(), [drawn(x[i], single(u, i), **{k: v[i] if k == "top_k" else single(v, i) for k, v in more.items()})[0] for i in range(len(x))]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("far", [44.375, 44.5, 44.75])
+def test_top_p_counts_where_top_k_ends_among_words_of_no_weight(part, dtype, far):
+    """Three heavy words in a row's first numbers and 2^-64 or less of them everywhere else: the top_k likeliest reach into those, top_p does not."""
+    x = torch.zeros((4, 50001))
+    x[:, 5], x[:, 900], x[:, 7000] = far, far - 0.25, far - 0.5
+    x[3, 30000:] = -1.0
+    got, want = words(part, x.to(DT[dtype]), [0.0, 0.7, 0.999, 0.999], top_k=[10000, 10000, 49000, 20000], top_p=[0.3, 0.3, 0.3, 0.6])
+    assert got == want
