@@ -849,7 +849,7 @@ struct Sampler {
     }
     if (mp > 0.f) leave((double)temperature * log((double)mp), (double)mp);
     float u = a.random[r];
-    u = u >= 0.f ? u : 0.f;
+    u = u >= 1.f ? INFINITY : u >= 0.f ? u : 0.f;  // (no sum passes it: 1 x the whole sum, added up another way, may be passed by less than all)
     // ---- the weights that are left, and where their sum passes the random number
     if (listed) {
       pick(r, u);
@@ -915,7 +915,7 @@ struct Sampler {
           hit_weight = last_weight;
         }
       });
-      // (none, where roundings of the two sums differ, or the random number is 1: the last that is left)
+      // (none, where roundings of the two sums differ, or the random number is 1 or more: the last that is left)
       const uint64_t lanes = __ballot(hit >= 0);
       const int l = lanes ? __builtin_ctzll(lanes) : 63 - __builtin_clzll(__ballot(last >= 0));
       if (lane == l) {

@@ -1,5 +1,4 @@
 """Words of long rows whose weights lie far apart (daris_sample), against the definition in whole numbers (draft_helpers.drawn)."""
-import math
 
 import numpy as np
 import pytest
@@ -37,3 +36,14 @@ def test_top_p_counts_where_top_k_ends_among_words_of_no_weight(part, dtype, far
     x[3, 30000:] = -1.0
     got, want = words(part, x.to(DT[dtype]), [0.0, 0.7, 0.999, 0.999], top_k=[10000, 10000, 49000, 20000], top_p=[0.3, 0.3, 0.3, 0.6])
     assert got == want
+
+
+@pytest.mark.parametrize("n,rows", [(40, 200), (3000, 40), (50001, 6)])
+def test_random_numbers_from_1_on_give_the_last_word_however_little_it_weighs(part, n, rows):
+    """The words behind two thirds of a row weigh less than the last bit of the sum in front of them."""
+    x = torch.randn((rows, n), generator=torch.Generator().manual_seed(n))
+    x[:, n - n // 3:] -= 40.0
+    for u in (1.0, 1.5, 1e30):
+        for more in (dict(), dict(top_k=[n - 1] * rows), dict(temperature=[0.95] * rows), dict(min_p=[1e-19] * rows)):
+            got, want = words(part, x, [u] * rows, **more)
+            assert got == want, (u, more)
