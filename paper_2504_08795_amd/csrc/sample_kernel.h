@@ -28,21 +28,23 @@ constexpr double kSampleGrid = 15.9;   // steps of a power of two: all 64 of the
 static_assert(kSampleSteps == kSampleThreads, "a step for each thread");
 
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
+typedef unsigned __int128 u128;
 
 struct SampleLds {
   float top[kSampleChunks];         // a chunk's largest
   float part_top[kSampleParts];     // ... a part's
   int part_off[kSampleParts];       // steps of its histogram's first from the row's first; more than all: it has no part in it
   double part_weight[kSampleParts]; // weight of its largest
-  uint64_t part_left[kSampleParts]; // ... of what is left of it
+  uint64_t part_left[kSampleParts]; // ... of its words of the threshold's step that are left, in this step's numbers
   double sum[kSampleChunks];        // a chunk's weights that are left, or how many of its numbers are the threshold's
   uint32_t count[kSampleSteps];
   uint64_t mass[kSampleSteps];
   uint64_t few[kSampleFew];         // words of one step: (logit, number), the larger word the larger number
   double wave_d[kSampleWaves];
+  u128 wave_w[kSampleWaves];
   uint64_t wave_m[kSampleWaves];
   uint32_t wave_c[kSampleWaves];
-  uint64_t found_mass;
+  u128 found_mass;
   uint64_t found_word;
   double found_sum;
   uint32_t found_count;
@@ -56,14 +58,24 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
 
-// The least whole number that is p x all or more, 1 at least (p < 1; all < 2^63): exact, so that equal weights are cut where their number says.
-__device__ __forceinline__ uint64_t part_of(float p, uint64_t all) {
+// Weights as whole numbers: those of step b of the histogram times 2^(b / 16), which leaves them between 0.37 and 1.05, and 2^SHIFT, which leaves the sum of a
+// row's below 2^63.  Each is so rounded by 2^-42 of itself at most (2^-45 in rows of 131072), however little it weighs.  Sums over steps have them in their places.
+__device__ __forceinline__ int up_of(int b) { return b >> 4; }
+__device__ __forceinline__ u128 placed(uint64_t mass, int b) { return (u128)mass << (64 - up_of(b)); }
+// What is to come of step b, in its own numbers: the least one that is v or more.
+__device__ __forceinline__ uint64_t taken_from(u128 v, int b) {
+  const int d = 64 - up_of(b);
+  return (uint64_t)(v >> d) + ((v & (((u128)1 << d) - 1)) != 0);
+}
+// The least whole number that is p x all or more, 1 at least (p < 1; all < 2^127): exact, so that equal weights are cut where their number says.
+__device__ __forceinline__ u128 part_of(float p, u128 all) {
   if (!(p > 0x1p-62f)) return 1;
   int e;
   const uint64_t m = (uint64_t)ldexpf(frexpf(p, &e), 24);  // p = m 2^(e - 24), e <= 0
-  const uint64_t hi = __umul64hi(all, m), lo = all * m;
+  const u128 low = (u128)(uint64_t)all * m, hi = (u128)(uint64_t)(all >> 64) * m + (low >> 64);
+  const uint64_t lo = (uint64_t)low;
   const int down = 24 - e;  // 24 to 85
-  if (down >= 64) return (down == 64 ? hi : hi >> (down - 64)) + ((lo | (down == 64 ? 0ull : hi & ((1ull << (down - 64)) - 1))) != 0);
+  if (down >= 64) return (hi >> (down - 64)) + ((lo | ((uint64_t)hi & ((1ull << (down - 64)) - 1))) != 0);
   return (hi << (64 - down) | lo >> down) + ((lo & ((1ull << down) - 1)) != 0);
 }
 
@@ -72,6 +84,8 @@ template <int CTRL, int ROWS, typename T>
 __device__ __forceinline__ T from_lane(T v) {
   if constexpr (sizeof(T) == 4) {
     return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+  } else if constexpr (sizeof(T) == 16) {
+    return (T)from_lane<CTRL, ROWS>((uint64_t)(v >> 64)) << 64 | from_lane<CTRL, ROWS>((uint64_t)v);
   } else {
     const u32x2 x = __builtin_bit_cast(u32x2, v);
     u32x2 y;
@@ -98,6 +112,8 @@ template <typename T>
 __device__ __forceinline__ T of_lane(T v, int lane) {
   if constexpr (sizeof(T) == 4) {
     return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+  } else if constexpr (sizeof(T) == 16) {
+    return (T)of_lane((uint64_t)(v >> 64), lane) << 64 | of_lane((uint64_t)v, lane);
   } else {
     u32x2 x = __builtin_bit_cast(u32x2, v);
     x.x = (uint32_t)__builtin_amdgcn_readlane((int)x.x, lane);
@@ -106,8 +122,8 @@ __device__ __forceinline__ T of_lane(T v, int lane) {
   }
 }
 
-// 2^y for -64 <= y <= 0, 1 for 0: the series of e^f to the eleventh power, |f| <= ln 2 / 2, whose rest is below (ln 2 / 2)^12 / 12! = 2^-47.
-__device__ __forceinline__ double weight(double y) {
+// 2^(y + up) for -64 <= y <= 0, 2^up for 0: the series of e^f to the eleventh power, |f| <= ln 2 / 2, whose rest is below (ln 2 / 2)^12 / 12! = 2^-47.
+__device__ __forceinline__ double weight(double y, int up = 0) {
   const double n = rint(y), f = (y - n) * 0.693147180559945309417;
   double p = 1.0 / 39916800;
   p = fma(p, f, 1.0 / 3628800);
@@ -121,7 +137,7 @@ __device__ __forceinline__ double weight(double y) {
   p = fma(p, f, 0.5);
   p = fma(p, f, 1.0);
   p = fma(p, f, 1.0);
-  return __builtin_amdgcn_ldexp(p, (int)n);
+  return __builtin_amdgcn_ldexp(p, (int)n + up);
 }
 
 template <bool BF16>
@@ -142,7 +158,7 @@ struct Sampler {
   int listed;           // m.few has all words that are left (and others), so many
   int below;            // step of the histogram that the threshold is in, -1: the parts' sums are not known
   bool spent;           // the row's histogram has made room for a finer one
-  double two_to_shift;  // weights as whole numbers: times this; the sum of a row's stays below 2^62
+  int shift;            // of weights as whole numbers
 
   // A lane's numbers of a chunk as they are in memory.  They begin at `first` (the last ones of the row where it ends in front of them).
   struct Raw {
@@ -282,11 +298,13 @@ struct Sampler {
     key = 0;
     leave((double)temperature * (-kSampleBits * 0.693147180559945309417), 0);
   }
-  __device__ __forceinline__ uint64_t whole(float x) const { return (uint64_t)(weight(bits(x)) * two_to_shift + 0.5); }
-  __device__ __forceinline__ void add_to(int b, float x, bool mass) {
-    atomicAdd(&m.count[b], 1u);
-    if (mass) atomicAdd((unsigned long long*)&m.mass[b], (unsigned long long)whole(x));
+  __device__ __forceinline__ uint64_t whole(float x, int b) const { return (uint64_t)(weight(bits(x), up_of(b) + shift) + 0.5); }
+  // One more in place `at`, of step b.
+  __device__ __forceinline__ void add_to(int at, float x, bool mass, int b) {
+    atomicAdd(&m.count[at], 1u);
+    if (mass) atomicAdd((unsigned long long*)&m.mass[at], (unsigned long long)whole(x, b));
   }
+  __device__ __forceinline__ void add_to(int b, float x, bool mass) { add_to(b, x, mass, b); }
   static __device__ __forceinline__ uint64_t scaled(uint64_t v, double f) { return f == 1.0 ? v : (uint64_t)((double)v * f + 0.5); }
   __device__ __forceinline__ void clear_steps() {
     m.count[tid] = 0;
@@ -400,22 +418,28 @@ struct Sampler {
   }
 
   // The step in which the sums over m.count (or, by mass, m.mass) reach what is wanted (or all that there is, if that is less); *count, *mass: added to by what lies above it;
-  // *in: what it holds.  whole_row: -1 if all of the count is wanted.
-  __device__ __forceinline__ int step_at(bool by_mass, bool whole_row, uint32_t want_count, uint64_t want_mass, uint32_t* count, uint64_t* mass, uint32_t* in) {
+  // *in: what it holds.  M is u128 for the row's histogram: its masses in their places, and -1 if all of the count is wanted; uint64_t for one step's.
+  template <typename M>
+  __device__ __forceinline__ int step_at(bool by_mass, uint32_t want_count, M want_mass, uint32_t* count, M* mass, uint32_t* in) {
+    constexpr bool whole_row = sizeof(M) == 16;
+    M* wave_m;
+    if constexpr (whole_row) wave_m = m.wave_w;
+    else wave_m = m.wave_m;
     if (tid == 0) m.found = -1;
     const uint32_t c = m.count[tid];
-    const uint64_t w = m.mass[tid];
+    M w = m.mass[tid];
+    if constexpr (whole_row) w = placed(m.mass[tid], tid);
     const uint32_t c_upto = wave_upto(c);
-    const uint64_t w_upto = by_mass ? wave_upto(w) : 0;
+    const M w_upto = by_mass ? wave_upto(w) : 0;
     if (lane == 63) {
       m.wave_c[wave] = c_upto;
-      m.wave_m[wave] = w_upto;
+      wave_m[wave] = w_upto;
     }
     __syncthreads();
     uint32_t c_all;
-    uint64_t w_all = 0, w_base = 0;
+    M w_all = 0, w_base = 0;
     const uint32_t c_base = waves_in_front(c_upto - c, m.wave_c, &c_all);
-    if (by_mass) w_base = waves_in_front(w_upto - w, m.wave_m, &w_all);
+    if (by_mass) w_base = waves_in_front(w_upto - w, wave_m, &w_all);
     if (!by_mass && whole_row && want_count >= c_all) want_count = 0;
     want_count = want_count < c_all ? want_count : c_all;
     want_mass = want_mass < w_all ? want_mass : w_all;
@@ -428,7 +452,7 @@ struct Sampler {
     const int b = m.found;
     if (b >= 0) {
       *count += m.found_count;
-      *mass += m.found_mass;
+      *mass += (M)m.found_mass;
       *in = m.count[b];
     }
     __syncthreads();
@@ -437,18 +461,20 @@ struct Sampler {
 
   // Moves the threshold to the last word of those in front (largest first) whose number is `want_count`, or (by mass) whose weight reaches `want_mass`.
   // sums: what the step's words that are left weigh goes to m.part_left, which is zero.
-  __device__ __forceinline__ void front(bool by_mass, uint32_t want_count, uint64_t want_mass, bool sums) {
+  __device__ __forceinline__ void front(bool by_mass, uint32_t want_count, u128 want, bool sums) {
     uint32_t above = 0, in = 0;
-    uint64_t above_mass = 0;
-    const int b = step_at(by_mass, true, want_count, want_mass, &above, &above_mass, &in);
+    u128 in_front_of = 0;
+    const int b = step_at(by_mass, want_count, want, &above, &in_front_of, &in);
     if (b < 0) return;  // fewer than that: none is cut
+    const uint64_t want_mass = by_mass ? taken_from(want - in_front_of, b) : 0;
+    uint64_t above_mass = 0;  // (of the step)
     below = -1;
     listed = 0;
     const uint32_t first_above = above;
-    const uint64_t first_mass = above_mass;
     const uint32_t from = least_of(b);
     const float edge = of_key(from > key ? from : key);
-    float highest = b > 0 ? of_key(least_of(b - 1) - 1) : most;
+    const float upper = b > 0 ? of_key(least_of(b - 1) - 1) : most;
+    float highest = upper;
     bool few = in <= kSampleFew;
     if (few) {
       // ---- the step's words in LDS, with those above it where all are few
@@ -456,7 +482,6 @@ struct Sampler {
       if (with_above) {
         highest = most;
         above = 0;
-        above_mass = 0;
       }
       if (tid == 0) m.found_count = 0;
       __syncthreads();
@@ -496,11 +521,11 @@ struct Sampler {
           if (n < (int)in) {
             const float x = of_key((uint32_t)(mine[i] >> 32));
             step_of[i] = fine(x, b);
-            add_to(step_of[i], x, by_mass);
+            add_to(step_of[i], x, by_mass, b);
           }
         }
         __syncthreads();
-        const int d = step_at(by_mass, false, want_count - above, want_mass - above_mass, &above, &above_mass, &in);
+        const int d = step_at<uint64_t>(by_mass, want_count - above, want_mass - above_mass, &above, &above_mass, &in);
         if (d < 0) return;
         few = in <= kSampleRank;
         if (few) {
@@ -518,7 +543,10 @@ struct Sampler {
         const bool on = word < (int)in;
         const uint64_t own_word = on ? m.few[word] : 0;
         if (by_mass) {
-          if (tid < (int)in) m.mass[tid] = whole(of_key((uint32_t)(m.few[tid] >> 32)));  // (the histogram has done its work)
+          if (tid < (int)in) {  // (the histogram has done its work; what is above the step has been taken off what is wanted)
+            const float x = of_key((uint32_t)(m.few[tid] >> 32));
+            m.mass[tid] = x <= upper ? whole(x, b) : 0;
+          }
           __syncthreads();
         }
         uint32_t n = 0;
@@ -546,14 +574,14 @@ struct Sampler {
           below = b;
 #pragma unroll
           for (int i = 0; i < N; ++i)
-            if (mine[i] >= m.found_word) atomicAdd((unsigned long long*)&m.part_left[(int)~(uint32_t)mine[i] / (a.part_chunks * kSampleChunk)], (unsigned long long)whole(of_key((uint32_t)(mine[i] >> 32))));
+            if (mine[i] >= m.found_word) atomicAdd((unsigned long long*)&m.part_left[(int)~(uint32_t)mine[i] / (a.part_chunks * kSampleChunk)], (unsigned long long)whole(of_key((uint32_t)(mine[i] >> 32)), b));
         }
         return;
       }
     }
     // ---- many: by their bits, 10, 10, 6 and 6 of them
     above = first_above;
-    above_mass = first_mass;
+    above_mass = 0;
     uint32_t prefix = 0, ties = 0;
     spent = true;
 #pragma unroll 1
@@ -564,17 +592,17 @@ struct Sampler {
       each(edge, [&](int, int first, const float(&x)[kPer]) {
         one_by_one(counted(x, first) & between(x, edge, highest), x, [&](int, float v) {
           const uint32_t k = order_key(v);
-          if (level == 0 || k >> (low + width) == prefix) add_to(((1u << width) - 1) & ~(k >> low), v, by_mass);  // the largest first
+          if (level == 0 || k >> (low + width) == prefix) add_to(((1u << width) - 1) & ~(k >> low), v, by_mass, b);  // the largest first
         });
       });
       __syncthreads();
-      const int d = step_at(by_mass, false, want_count - above, want_mass - above_mass, &above, &above_mass, &ties);
+      const int d = step_at<uint64_t>(by_mass, want_count - above, want_mass - above_mass, &above, &above_mass, &ties);
       if (d < 0) return;  // (as above, of more words)
       prefix = prefix << width | (((1u << width) - 1) & ~(uint32_t)d);
     }
     const uint32_t was = key;
     key = prefix;
-    const uint64_t own = whole(of_key(key));
+    const uint64_t own = whole(of_key(key), b);
     const uint32_t take = by_mass ? (uint32_t)((want_mass - above_mass + own - 1) / own) : want_count - above;
     if (take < ties) upto = nth_equal(take);
     else if (key != was) upto = 0x7fffffff;
@@ -668,7 +696,7 @@ struct Sampler {
     weighed = by_mass || (by_count && k > kSampleChunk);
     step = 1.4426950408889634074 / (double)temperature;
     grid = step * kSampleGrid;
-    two_to_shift = (double)(1ull << (62 - (32 - __builtin_clz(a.n))));
+    shift = 62 - (32 - __builtin_clz(a.n));
   }
 
   // One part of row r: its chunks' largest, and as the row asks its histogram or its chunks' sums, in LDS and (where there are others) in a.part.
@@ -781,7 +809,7 @@ struct Sampler {
             const int q = q0 + i < a.parts ? q0 + i : a.parts - 1;
             const bool in = q0 + i < a.parts && tid >= m.part_off[q];
             n += in ? c[i] : 0;
-            if (weighed) w += in ? scaled(v[i], m.part_weight[q]) : 0;
+            if (weighed) w += in ? scaled(v[i], __builtin_amdgcn_ldexp(m.part_weight[q], up_of(tid) - up_of(tid - m.part_off[q]))) : 0;
           }
         }
         m.count[tid] = n;
@@ -830,7 +858,7 @@ struct Sampler {
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
       if (!(turn ? by_mass : by_count)) continue;
-      uint64_t want = 0;
+      u128 want = 0;
       if (turn) {
         if (key != lowest || upto != 0x7fffffff || spent) {
           // the k largest by themselves (or all, where the k-th weighs nothing)
@@ -840,8 +868,8 @@ struct Sampler {
           each(of_key(key), [&](int, int first, const float(&x)[kPer]) { one_by_one(counted(x, first), x, [&](int, float v) { add_to(bin(v), v, true); }); });
           __syncthreads();
         }
-        uint64_t sum;
-        (void)in_front(m.mass[tid], m.wave_m, &sum);
+        u128 sum;
+        (void)in_front(placed(m.mass[tid], tid), m.wave_w, &sum);
         __syncthreads();
         want = part_of(p, sum);
       }
@@ -860,28 +888,28 @@ struct Sampler {
     if (weighed && a.parts > 1 && below >= 0 && !(mp > 0.f) && u >= 0x1p-40f) {
       // The histograms say what is left of each part (weights below 2^-46 as nothing, which the random number is not), and so in which part the sum passes.
       for (int q = wave; q < a.parts; q += kSampleWaves) {
-        const int off = m.part_off[q], end = below - off;
-        const double f = m.part_weight[q];
-        uint64_t w = 0;
+        const int end = below - m.part_off[q];
+        double w = 0;
 #pragma unroll 8
         for (int i = 0; i < kSampleSteps / 64; ++i) {
           const uint64_t v = mass_at(r, q)[i * 64 + lane];
-          w += i * 64 + lane < end ? scaled(v, f) : 0;
+          w += i * 64 + lane < end ? __builtin_amdgcn_ldexp((double)v, -up_of(i * 64 + lane)) : 0;
         }
-        w = of_lane(wave_upto(w), 63);
-        if (lane == 0) atomicAdd((unsigned long long*)&m.part_left[q], (unsigned long long)w);
+        w = of_lane(wave_upto(w), 63) * m.part_weight[q];
+        if (lane == 0) m.sum[q] = w;
       }
       __syncthreads();
-      const double per = 1.0 / two_to_shift;
-      const uint64_t left0 = lane < a.parts ? m.part_left[lane] : 0, left1 = lane + 64 < a.parts ? m.part_left[lane + 64] : 0;
-      const uint64_t upto0 = wave_upto(left0), all0 = of_lane(upto0, 63), upto1 = all0 + wave_upto(left1), sum = of_lane(upto1, 63);
-      const double target = (double)u * (double)sum;
-      const uint64_t hit0 = __ballot((double)upto0 > target && left0), hit1 = __ballot((double)upto1 > target && left1);
+      const double per = __builtin_amdgcn_ldexp(1.0, -shift);
+      auto left = [&](int q) { return q < a.parts ? m.sum[q] + __builtin_amdgcn_ldexp((double)m.part_left[q], -up_of(below)) : 0.0; };
+      const double left0 = left(lane), left1 = left(lane + 64);
+      const double upto0 = wave_upto(left0), all0 = of_lane(upto0, 63), upto1 = all0 + wave_upto(left1), sum = of_lane(upto1, 63);
+      const double target = (double)u * sum;
+      const uint64_t hit0 = __ballot(upto0 > target && left0 > 0), hit1 = __ballot(upto1 > target && left1 > 0);
       const int q = hit0 ? __builtin_ctzll(hit0) : hit1 ? 64 + __builtin_ctzll(hit1) : -1;
       if (q >= 0) {
-        const uint64_t upto_q = q < 64 ? of_lane(upto0, q) : of_lane(upto1, q - 64), left_q = q < 64 ? of_lane(left0, q) : of_lane(left1, q - 64);
-        skipped = (double)(upto_q - left_q) * per;
-        more = (double)(sum - left_q) * per;
+        const double upto_q = q < 64 ? of_lane(upto0, q) : of_lane(upto1, q - 64), left_q = q < 64 ? of_lane(left0, q) : of_lane(left1, q - 64);
+        skipped = (upto_q - left_q) * per;
+        more = (sum - left_q) * per;
         c0_left = q * a.part_chunks;
         c1_left = c0_left + a.part_chunks < a.chunks ? c0_left + a.part_chunks : a.chunks;
       }

@@ -135,7 +135,7 @@ struct SampleArgs {
 constexpr int kSampleChunk = 512, kSampleMost = 1 << 20;  // numbers that a wave reads at once; of a row, at most
 constexpr int kSampleWaves = 16, kSampleSteps = 1024, kSampleFew = 4096, kSampleRank = 512;
 constexpr int kSamplePart = 16384, kSampleParts = kSampleMost / (kSamplePart / 2);  // numbers of a part, at most; parts of a row
-constexpr int kSampleLds = kSampleMost / kSampleChunk * 12 + kSampleParts * 24 + kSampleSteps * 12 + kSampleFew * 8 + kSampleWaves * 20 + 40;
+constexpr int kSampleLds = kSampleMost / kSampleChunk * 12 + kSampleParts * 24 + kSampleSteps * 12 + kSampleFew * 8 + kSampleWaves * 36 + 48;
 // numbers of a row in SampleArgs::part: the chunks' largest, their sums, the parts' histograms
 constexpr int64_t sample_floats(int chunks, int parts) { return (chunks + 1) / 2 * 2 + 2 * (int64_t)chunks + (int64_t)parts * kSampleSteps * 3; }
 

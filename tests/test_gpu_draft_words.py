@@ -1,5 +1,7 @@
 """Words of long rows whose weights lie far apart (daris_sample), against the definition in whole numbers (draft_helpers.drawn)."""
 
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -47,3 +49,26 @@ def test_random_numbers_from_1_on_give_the_last_word_however_little_it_weighs(pa
         for more in (dict(), dict(top_k=[n - 1] * rows), dict(temperature=[0.95] * rows), dict(min_p=[1e-19] * rows)):
             got, want = words(part, x, [u] * rows, **more)
             assert got == want, (u, more)
+
+
+def test_top_p_among_a_million_words_that_together_weigh_a_thousandth_of_the_first(part):
+    """One word, and equal ones of 2^-30.3 of it: each of them has its part in the sums, to a last word that is told from its neighbours."""
+    n = 1 << 20
+    x = torch.full((3, n), -21.0)
+    x[0, 600000] = x[1, 0] = x[2, n - 1] = 0.0
+    last = 1 - 2.0 ** -24
+    got, want = words(part, x, [last] * 3, top_p=[0.9995, 0.9993, 0.9999])
+    assert got == want and 100 < abs(want[1] - want[0]) < n - 1000
+    got, want = words(part, x[:2], [1 - 2.0 ** -13, last], top_k=[n // 2, n - 7])
+    assert got == want
+
+
+@pytest.mark.parametrize("u", [2.0 ** -36, 2.0 ** -37, 1.3 * 2.0 ** -38])
+def test_many_parts_of_little_weight_come_to_what_a_random_number_asks(part, u):
+    """A word of 2^-42.5 in each 8192 numbers, and one of weight 1 behind them."""
+    n = 1 << 20
+    x = torch.full((1, n), -math.inf)
+    x[0, 17:n - 8192:8192] = -42.5 * math.log(2.0)
+    x[0, n - 5] = 0.0
+    got, want = words(part, x, [u], top_k=[n - 1])
+    assert got == want and want[0] < n - 8192
