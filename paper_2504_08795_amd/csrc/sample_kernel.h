@@ -885,8 +885,11 @@ struct Sampler {
     }
     double skipped = 0, more = 0;  // weights of the parts in front of the one that is looked at, and of all others
     int c0_left = 0, c1_left = a.chunks;
-    if (weighed && a.parts > 1 && below >= 0 && !(mp > 0.f) && u >= 0x1p-40f) {
-      // The histograms say what is left of each part (weights below 2^-46 as nothing, which the random number is not), and so in which part the sum passes.
+    // (What the parts leave may have words of no weight in it where none is cut, lighter than 2^-64 of the row's largest but not of their part's: 2^-44 in all, which is at most half of the
+    // distance to the next random number from 2^-20 on.  For smaller ones all weights are taken again.)
+    const bool by_parts = u >= 0x1p-20f;
+    if (weighed && a.parts > 1 && below >= 0 && !(mp > 0.f) && by_parts) {
+      // The histograms say what is left of each part, and so in which part the sum passes.
       for (int q = wave; q < a.parts; q += kSampleWaves) {
         const int end = below - m.part_off[q];
         double w = 0;
@@ -914,7 +917,7 @@ struct Sampler {
         c1_left = c0_left + a.part_chunks < a.chunks ? c0_left + a.part_chunks : a.chunks;
       }
     }
-    if (!all) {
+    if (!all || (a.parts > 1 && !by_parts)) {
       __syncthreads();
       for (int c = tid; c < a.chunks; c += kSampleThreads) m.sum[c] = 0;
       __syncthreads();

@@ -72,3 +72,15 @@ def test_many_parts_of_little_weight_come_to_what_a_random_number_asks(part, u):
     x[0, n - 5] = 0.0
     got, want = words(part, x, [u], top_k=[n - 1])
     assert got == want and want[0] < n - 8192
+
+
+def test_words_of_no_weight_have_no_part_in_the_sum_that_a_small_random_number_passes(part):
+    """Words of just under 2^-40, each among 8191 of less than 2^-64: eight of them do not pass 2^-37, for which 511 others beside each would be enough."""
+    n = 1 << 20
+    x = torch.full((1, n), -44.4)
+    x[0, 17:n - 8192:8192] = -40 * math.log(2.0) - 2.0 ** -16
+    x[0, n - 5] = 0.0
+    assert 8 * math.exp(float(x[0, 17])) < 2.0 ** -37 < 8 * math.exp(float(x[0, 17])) + 7 * 511 * math.exp(-44.4) and math.exp(-44.4) < 2.0 ** -64
+    for more in (dict(top_k=[n - 1]), dict()):
+        got, want = words(part, x, [2.0 ** -37], **more)
+        assert got == want == [17 + 8 * 8192], more
