@@ -144,11 +144,13 @@ typedef struct daris_matvec {
  *
  * tree [n_rows][tree_words] (dense, aligned to 8 bytes, 1 to DARIS_TREE_WORDS words a row): bit j mod 64 of word j / 64 of a row's mask is set if the row sees
  * node j of its sequence, which is the sequence's row j.  A node's own bit and those of the nodes above it make a tree, whose nodes are numbered from
- * the root on (a node behind the one that it hangs on); any other masks over the step's rows may stand there too.  Bits of rows that the sequence does not have are ignored.
+ * the root on (a node behind the one that it hangs on); any other masks over the step's rows may stand there too.  Bits of rows that the sequence does not have are ignored by attention and
+ * acceptance; a position counts all bits of the mask, these among them.
  *
  * Append and attend as above with these differences.  Node j lies in the cache as token before + j, but its position -- for the turning of keys and
  * queries -- is before + (the number of bits in its mask) - 1.  A row attends the cached tokens 0 .. before - 1 and the nodes of its mask, in this
- * order; window != 0: the last `window` of them.  k and v of an append have the same distances.
+ * order; window != 0: the last `window` of them.  k and v of an append have the same distances (a
+ * descriptor is as large as daris_append: lists that were laid out before there were trees stay right).
  */
 typedef struct daris_tree_append {
   daris_cache cache;
