@@ -75,6 +75,16 @@ class Rows:
             ]
 
 
+def checked(words, streams, vocabulary):
+    """words: a tensor with a word in 0 .. vocabulary - 1 for each stream, or a ValueError.  (-1 is what a row of logits without a number gives: it must not become an index.)"""
+    if words.shape != (streams,):
+        raise ValueError(f"{tuple(words.shape)} words for {streams} streams")
+    for s, w in enumerate(words.tolist()):
+        if not 0 <= w < vocabulary:
+            raise ValueError(f"stream {s}: word {w} is outside 0 .. {vocabulary - 1}")
+    return words
+
+
 class Decoder:
     """streams: texts that grow side by side, max_tokens each at most."""
 
@@ -166,8 +176,7 @@ class Decoder:
 
     def step(self, words):
         """Appends a word to every stream (a tensor, as prompt and step return them); the words that follow."""
-        if words.shape != (self.streams,):
-            raise ValueError(f"{tuple(words.shape)} words for {self.streams} streams")
+        checked(words, self.streams, len(self.words))
         self._grow([1] * self.streams)
         torch.index_select(self.words, 0, words, out=self.rows.x)
         D.daris_run_ops(self.step_ops, self.part)
@@ -178,8 +187,9 @@ class Decoder:
     def draft_step(self, words, drafts):
         """Appends a word to every stream with drafts[s] = (words, parents) behind it: parents[i] is the number of the drafted word that drafted word i follows, or -1 for the
         appended one.  The drafts that the model would have given stand.  Returns them (a list for every stream) and the words that follow."""
-        if words.shape != (self.streams,) or len(drafts) != self.streams:
-            raise ValueError(f"{tuple(words.shape)} words and {len(drafts)} drafts for {self.streams} streams")
+        checked(words, self.streams, len(self.words))
+        if len(drafts) != self.streams:
+            raise ValueError(f"{len(drafts)} drafts for {self.streams} streams")
         for texts, parents in drafts:
             if len(texts) != len(parents) or any(not 0 <= w < len(self.words) for w in texts):
                 raise ValueError(f"drafts of words in 0 .. {len(self.words) - 1}, each with its parent")

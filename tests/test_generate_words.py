@@ -1,0 +1,38 @@
+"""Which words the example decoder takes: those that its steps get are indices on the GPU.  No GPU for the check itself."""
+import pytest
+import torch
+
+import paper_2504_08795_amd as D
+from paper_2504_08795_amd.generate import Decoder, checked
+
+
+@pytest.mark.parametrize("words,named", [([3, -1], "stream 1"), ([320, 0], "stream 0"), ([2 ** 40, 0], "stream 0"), ([-2 ** 63, 1], "stream 0"), ([1], "for 2 streams"), ([1, 2, 3], "for 2 streams")])
+def test_words_that_are_none_are_refused(words, named):
+    with pytest.raises(ValueError, match=named):
+        checked(torch.tensor(words), 2, 320)
+
+
+@pytest.mark.parametrize("words", [[0, 319], [5, 5]])
+def test_words_are_given_back(words):
+    assert checked(torch.tensor(words), 2, 320).tolist() == words
+    assert checked(torch.tensor(words, dtype=torch.int32), 2, 320).tolist() == words
+
+
+@pytest.mark.gpu
+def test_a_stream_whose_logits_are_no_numbers_is_not_continued():
+    """Its word is -1, which neither kind of step takes; the other streams' texts stay as they are."""
+    D.daris_init(0, 0, 0)
+    try:
+        m = Decoder(2, 70, blocks=1, width=256, q_heads=4, kv_heads=1, dim=64, hidden=256, vocabulary=320, part=D.daris_create_partition(256))
+        m.words[7] = float("nan")
+        words, _ = m.prompt([[1, 2], [3, 7]])
+        assert words.tolist()[1] == -1 and 0 <= words.tolist()[0] < 320
+        for call in (lambda: m.step(words), lambda: m.draft_step(words, [([], []), ([], [])]), lambda: m.step(torch.full_like(words, 320)), lambda: m.draft_step(words[:1], [([], []), ([], [])])):
+            with pytest.raises(ValueError):
+                call()
+        assert m.lengths == [2, 2] and m.before.tolist() == [2, 2]
+        words[1] = 0
+        m.step(words)
+        assert m.lengths == [3, 3]
+    finally:
+        D.daris_shutdown()
