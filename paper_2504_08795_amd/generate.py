@@ -111,15 +111,18 @@ class Decoder:
         head = [D.make_norm(self.rows.add, self.last_norm, self.normed, self.eps, res=self.rows.x),
                 D.make_matvec(self.normed, self.classifier.codes, self.classifier.scales, self.logits)]
         self.step_ops, self.head_ops = D.make_ops(self.rows.ops + head), D.make_ops(head)
+        self.drawn = vocabulary <= D.SAMPLE_WORDS                       # longer rows are not drawn from: their words are the likeliest ones
         # what a stream's words are drawn with: by default the likeliest one
         self.temperature, self.top_p, self.min_p = torch.zeros(streams, device="cuda"), torch.ones(streams, device="cuda"), torch.zeros(streams, device="cuda")
         self.top_k, self.word = torch.zeros(streams, dtype=torch.int32, device="cuda"), torch.zeros(streams, dtype=torch.int32, device="cuda")
         self.random = torch.zeros(streams, device="cuda")
         self.numbers = torch.Generator(device="cuda").manual_seed(seed)
-        self.draw_ops = D.make_ops([self._sample(self.logits, self.word, self.random, slice(None))])
+        self.draw_ops = D.make_ops([self._sample(self.logits, self.word, self.random, slice(None))]) if self.drawn else None
 
     def wish(self, temperature=None, top_k=None, top_p=None, min_p=None):
         """What words are drawn with from now on: a number for all streams or one for each (see daris_sample); temperature 0 gives the likeliest."""
+        if not self.drawn and temperature is not None and bool((torch.as_tensor(temperature) > 0).any()):
+            raise ValueError(f"words are drawn from {D.SAMPLE_WORDS} at most, not from {len(self.words)}")
         for mine, value in ((self.temperature, temperature), (self.top_k, top_k), (self.top_p, top_p), (self.min_p, min_p)):
             if value is not None:
                 mine.copy_(torch.as_tensor(value, dtype=mine.dtype).expand(self.streams))
@@ -129,6 +132,8 @@ class Decoder:
         return D.make_sample(logits, word, random, temperature=self.temperature[which], top_k=self.top_k[which], top_p=self.top_p[which], min_p=self.min_p[which])
 
     def _draw(self):
+        if not self.drawn:
+            return self.logits.argmax(1)
         self.random.uniform_(generator=self.numbers)
         D.daris_run_ops(self.draw_ops, self.part)
         return self.word.long()
@@ -188,6 +193,8 @@ class Decoder:
         """Appends a word to every stream with drafts[s] = (words, parents) behind it: parents[i] is the number of the drafted word that drafted word i follows, or -1 for the
         appended one.  The drafts that the model would have given stand.  Returns them (a list for every stream) and the words that follow."""
         checked(words, self.streams, len(self.words))
+        if not self.drawn:
+            raise ValueError(f"drafts of up to {D.SAMPLE_WORDS} words, not {len(self.words)}")
         if len(drafts) != self.streams:
             raise ValueError(f"{len(drafts)} drafts for {self.streams} streams")
         for texts, parents in drafts:

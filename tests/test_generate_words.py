@@ -36,3 +36,21 @@ def test_a_stream_whose_logits_are_no_numbers_is_not_continued():
         assert m.lengths == [3, 3]
     finally:
         D.daris_shutdown()
+
+
+@pytest.mark.gpu
+def test_vocabularies_that_are_not_drawn_from_give_their_likeliest_words():
+    D.daris_init(0, 0, 0)
+    try:
+        m = Decoder(2, 70, blocks=1, width=128, q_heads=2, kv_heads=1, dim=64, hidden=128, vocabulary=D.SAMPLE_WORDS + 16, part=D.daris_create_partition(256))
+        words, _ = m.prompt([[1, D.SAMPLE_WORDS + 3], [3]])
+        for _ in range(2):
+            assert torch.equal(m.logits.gather(1, words[:, None])[:, 0], m.logits.amax(1))
+            words = m.step(words)
+        m.wish(temperature=0.0, top_k=3)
+        for call in (lambda: m.wish(temperature=[0.0, 0.5]), lambda: m.draft_step(words, [([], []), ([], [])])):
+            with pytest.raises(ValueError, match=str(D.SAMPLE_WORDS)):
+                call()
+        assert m.lengths == [4, 3] and m.temperature.tolist() == [0, 0]
+    finally:
+        D.daris_shutdown()
