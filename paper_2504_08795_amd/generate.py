@@ -108,16 +108,17 @@ class Decoder:
         self.last_norm, self.classifier = torch.ones(width, dtype=dtype, device="cuda"), Weights(vocabulary, width, group, rng)
         self.rows = Rows(self, streams)
         self.normed, self.logits = torch.zeros((streams, width), dtype=dtype, device="cuda"), torch.zeros((streams, vocabulary), dtype=dtype, device="cuda")
-        head = [D.make_norm(self.rows.add, self.last_norm, self.normed, self.eps, res=self.rows.x),
-                D.make_matvec(self.normed, self.classifier.codes, self.classifier.scales, self.logits)]
-        self.step_ops, self.head_ops = D.make_ops(self.rows.ops + head), D.make_ops(head)
-        self.drawn = vocabulary <= D.SAMPLE_WORDS                       # longer rows are not drawn from: their words are the likeliest ones
         # what a stream's words are drawn with: by default the likeliest one
         self.temperature, self.top_p, self.min_p = torch.zeros(streams, device="cuda"), torch.ones(streams, device="cuda"), torch.zeros(streams, device="cuda")
         self.top_k, self.word = torch.zeros(streams, dtype=torch.int32, device="cuda"), torch.zeros(streams, dtype=torch.int32, device="cuda")
         self.random = torch.zeros(streams, device="cuda")
         self.numbers = torch.Generator(device="cuda").manual_seed(seed)
-        self.draw_ops = D.make_ops([self._sample(self.logits, self.word, self.random, slice(None))]) if self.drawn else None
+        head = [D.make_norm(self.rows.add, self.last_norm, self.normed, self.eps, res=self.rows.x),
+                D.make_matvec(self.normed, self.classifier.codes, self.classifier.scales, self.logits)]
+        self.drawn = vocabulary <= D.SAMPLE_WORDS                       # longer rows are not drawn from: their words are the likeliest ones
+        if self.drawn:
+            head.append(self._sample(self.logits, self.word, self.random, slice(None)))
+        self.step_ops, self.head_ops = D.make_ops(self.rows.ops + head), D.make_ops(head)
 
     def wish(self, temperature=None, top_k=None, top_p=None, min_p=None):
         """What words are drawn with from now on: a number for all streams or one for each (see daris_sample); temperature 0 gives the likeliest."""
@@ -131,12 +132,12 @@ class Decoder:
         """Draws a word for each row of logits; which: the rows' streams."""
         return D.make_sample(logits, word, random, temperature=self.temperature[which], top_k=self.top_k[which], top_p=self.top_p[which], min_p=self.min_p[which])
 
-    def _draw(self):
-        if not self.drawn:
-            return self.logits.argmax(1)
-        self.random.uniform_(generator=self.numbers)
-        D.daris_run_ops(self.draw_ops, self.part)
-        return self.word.long()
+    def _run(self, ops):
+        """A list that ends with the streams' words."""
+        if self.drawn:
+            self.random.uniform_(generator=self.numbers)
+        D.daris_run_ops(ops, self.part)
+        return self.word.long() if self.drawn else self.logits.argmax(1)
 
     def _page(self):
         page = self.free.pop()
@@ -158,7 +159,7 @@ class Decoder:
 
     def _grown(self, counts):
         self.lengths = [a + n for a, n in zip(self.lengths, counts)]
-        self.before.copy_(torch.tensor(self.lengths, dtype=torch.int32))
+        self.before += torch.tensor(counts, dtype=torch.int32, device="cuda")
 
     def prompt(self, texts):
         """Appends a text (a list of words' numbers, not empty) to every stream; the words that follow.  Returns them and the rows' buffers."""
@@ -175,19 +176,19 @@ class Decoder:
         last = torch.tensor(ends[1:] - 1, device="cuda")
         torch.index_select(rows.x, 0, last, out=self.rows.x)
         torch.index_select(rows.add, 0, last, out=self.rows.add)
-        D.daris_run_ops(self.head_ops, self.part)
+        words = self._run(self.head_ops)
         self._grown(counts)
-        return self._draw(), rows
+        return words, rows
 
     def step(self, words):
         """Appends a word to every stream (a tensor, as prompt and step return them); the words that follow."""
         checked(words, self.streams, len(self.words))
         self._grow([1] * self.streams)
         torch.index_select(self.words, 0, words, out=self.rows.x)
-        D.daris_run_ops(self.step_ops, self.part)
-        self._grown([1] * self.streams)
-        return self._draw()
-
+        words = self._run(self.step_ops)
+        self.lengths = [n + 1 for n in self.lengths]
+        self.before += 1                                                # (nothing to copy, which would be waited for)
+        return words
 
     def draft_step(self, words, drafts):
         """Appends a word to every stream with drafts[s] = (words, parents) behind it: parents[i] is the number of the drafted word that drafted word i follows, or -1 for the
@@ -253,7 +254,7 @@ class Decoder:
 
     def _tell(self):
         self.pages.copy_(torch.from_numpy(self.table))
-        self._grown([0] * self.streams)
+        self.before.copy_(torch.tensor(self.lengths, dtype=torch.int32))
 
 
 def looked_up(text, most):

@@ -54,3 +54,23 @@ def test_vocabularies_that_are_not_drawn_from_give_their_likeliest_words():
         assert m.lengths == [4, 3] and m.temperature.tolist() == [0, 0]
     finally:
         D.daris_shutdown()
+
+
+@pytest.mark.gpu
+def test_a_step_is_one_list_that_ends_with_its_words(monkeypatch):
+    from paper_2504_08795_amd import generate
+    lists, run = [], D.daris_run_ops
+    monkeypatch.setattr(generate.D, "daris_run_ops", lambda ops, part: (lists.append(ops), run(ops, part))[1])
+    D.daris_init(0, 0, 0)
+    try:
+        m = Decoder(2, 200, blocks=1, width=256, q_heads=4, kv_heads=1, dim=64, hidden=256, vocabulary=320, part=D.daris_create_partition(256))
+        m.wish(temperature=0.8)
+        words, _ = m.prompt([[1, 2], [3] * 70])
+        for _ in range(3):
+            lists.clear()
+            words = m.step(words)
+            assert lists == [m.step_ops] and torch.equal(words, m.word.long()) and m.before.tolist() == m.lengths
+        m.fork(1, 0)
+        assert m.before.tolist() == m.lengths == [73, 73]
+    finally:
+        D.daris_shutdown()
