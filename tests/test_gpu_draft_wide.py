@@ -1,11 +1,11 @@
-"""Attention of trees in wide tiles, whole and cut into units that are merged, against 64 bits (see draft_wide_cases)."""
+"""Attention of trees in wide tiles, whole and cut into units that are merged, and in narrow ones that are cut, against 64 bits (see draft_wide_cases)."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2504_08795_amd as D
 from draft_helpers import bits_of
-from draft_wide_cases import CASES, CUS, WIDE
+from draft_wide_cases import CASES, CUS, NARROW, WIDE
 from step_helpers import DT, PAGE, Cache, close
 from test_gpu_draft import attend_case, rand, trees
 
@@ -15,8 +15,13 @@ pytestmark = pytest.mark.gpu
 @pytest.fixture(scope="module")
 def part():
     D.daris_init(0, 0, 0)
-    yield D.daris_create_partition(CUS)
+    p = D.daris_create_partition(CUS)
+    D.daris_create_partition(256)
+    yield p
     D.daris_shutdown()
+
+
+LARGE = 1      # the partition of 256 CUs
 
 
 @pytest.mark.parametrize("dtype,dim", WIDE)
@@ -95,3 +100,19 @@ def test_cut_tiles_are_merged_alike_each_time(part, dtype, dim):
         out.zero_()
         D.daris_run_ops(ops, part)
         assert torch.equal(out, first)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("name", NARROW)
+def test_narrow_tiles_that_are_cut(part, name, dim, dtype):
+    before, rows, kv, heads, window, _ = NARROW[name]
+    attend_case(LARGE, 250 + dim, before, rows, kv, dim, heads, dtype, window)
+
+    def bad(c):                                             # a NaN among the values of node 5
+        page, i = int(c.pages[0, (before[0] + 5) // PAGE]), (before[0] + 5) % PAGE
+        c.v.view(torch.uint8)[page, 0, 3, i] = 0x7F
+    masks = trees(251, rows)
+    seen = torch.tensor([i < rows[0] and 5 in bits_of(masks[i].tolist()) for i in range(sum(rows))])
+    got, _ = attend_case(LARGE, 252, before, rows, kv, dim, heads, dtype, window, masks, bad)
+    assert 1 <= int(seen.sum()) < rows[0] and bool(torch.isnan(got[seen][:, :heads // kv, 3]).all()) and int(torch.isnan(got).sum()) == int(seen.sum()) * (heads // kv)
