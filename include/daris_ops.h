@@ -178,7 +178,8 @@ typedef struct daris_tree_attend {
  *   top_p[row] < 1   leaves the shortest front of these, the largest first, whose weights come to top_p of the sum of them all (one word at least);
  *   min_p[row] > 0   leaves those of them that weigh min_p or more (and the largest).
  * Of equal logits the word of the lower number is the larger.  word[row] is the first word that is left, by number, at which the sum of the weights that
- * are left is more than random[row] times all of it (random in [0, 1); NaN and what is below 0 count as 0; from 1 on it is the last word).  Weights and sums have 64 bits.
+ * are left is more than random[row] times all of it (random in [0, 1); NaN and what is below 0 count as 0; from 1 on it is the last word).  Weights and sums are
+ * doubles, within 2^-46 of themselves; top_p, and where a long row's sum passes the random number, are found with weights rounded to whole numbers, within 2^-39 of each.
  * chance[row], if not NULL, is its weight divided by that sum.  T <= 0 or NaN, and random == NULL, give the largest (and 1); a row with nothing but NaN and
  * -infinity gives -1 (and 0).  A row with +infinity is drawn among those words.  temperature == NULL is 1, the others' NULL leaves everything.  All per row: float, top_k int32.
  */

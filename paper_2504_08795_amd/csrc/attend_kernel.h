@@ -109,7 +109,7 @@ __device__ __forceinline__ bool find_among(const AttendArgs& a, int unit, Unit* 
   }
   // Trees of a few tiles each, all as long as their sequence: to cut them pays where the longest takes clearly longer than a CU's even share, by what the sums of a cut tile
   // cost.  (us a call whole and cut, 32 query and 8 key heads of 128, bf16: 24 trees of up to 24 nodes behind up to 3000 tokens 43 and 57, 12 of 40 38 and 53, 8 of 64 behind 2000
-  // 35 and 43, 8 of 32 behind 8000 65 and 55; wide 32 of 64 behind 4096 120 and 111, 6 of 256 behind 4000 130 and 92.)
+  // 35 and 43, 8 of 32 behind 8000 65 and 55; wide 32 of 64 behind 4096 120 and 111, 6 of 256 behind 4000 130 and 92.  Fewer than six trees were not measured both ways.)
   if (TREE && a.target > 0 && most > (float)c && most <= work / (float)a.round + (TILE == kWideColumns ? 10.f : 30.f)) c = ((int)most + 3) / 4 * 4;
   int base = 0;
   for (int s0 = 0; s0 < ns; s0 += 64 * SETS) {

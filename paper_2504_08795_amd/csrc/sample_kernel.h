@@ -1,7 +1,8 @@
 // Draws a word for each row of logits: weights exp((x - M) / T) cut to the top_k largest, to the shortest front with top_p of their sum, to those of min_p,
 // and the first word, by number, at which the sum of the weights that are left passes random x total.
 //
-// Weights and their sums are held in 64 bits: a word is a whole number, and it changes where a sum passes the random number by a last bit.  Nothing is sorted:
+// Weights and their sums are held in 64 bits: a word is a whole number, and it changes where a sum passes the random number by a last bit.  (A weight is within 2^-46 of itself, by
+// the series that it comes of; as the whole numbers of top_p within 2^-39.  Random numbers are floats, 2^-24 apart where they are next to 1.)  Nothing is sorted:
 // what is left is everything above a threshold, (logit, number) of one word.  It is found by a histogram of equal steps of the exponent (counts, and weights as whole
 // numbers, whose sums no order changes), and among the words of the one step that the threshold lies in by finer steps and by comparing each with each, or, where they are
 // too many (equal logits), by their bits.
@@ -12,7 +13,7 @@
 // waited for its registers: 64 rows of 131072, bf16, top_p 0.5 to 0.95, 135 us a call and 85.)
 //
 // One row of 50001 (fp32, 40 likeliest): 28 us a call, the parts 6 of them and the end 16, which is a chain of barriers and fetches: histograms, the step, its words, their order.  64 rows
-// of 131072 (bf16, wishes of every kind), 16.8 MB: 78 us, the parts 20 (79 % of the SIMDs' cycles are vector instructions), the end 52 on 64 CUs, of which the
+// of 131072 (bf16, wishes of every kind), 16.8 MB: 81 us, the parts 19 (75 % of the SIMDs' cycles are vector instructions), the end 54 on 64 CUs, of which the
 // longest rows gather the words of their step from 256 chunks (18) and add up one part's weights (11).  Weights in 64 bits cost 20 instructions a number; a lane's numbers take
 // turns in one loop of them (unrolled, the constants of eight weights leave half of the waves without registers).  Kept weights are taken again in one part only, as the
 // histograms say what is left of the others (one row of 131072, flat: 48 us for all of it, 7 so).
@@ -59,7 +60,8 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
 
 // Weights as whole numbers: those of step b of the histogram times 2^(b / 16), which leaves them between 0.37 and 1.05, and 2^SHIFT, which leaves the sum of a
-// row's below 2^63.  Each is so rounded by 2^-42 of itself at most (2^-45 in rows of 131072), however little it weighs.  Sums over steps have them in their places.
+// row's below 2^63.  Each is so rounded by 2^-40 of itself at most (2^-43 in rows of 131072), however little it weighs, and a part's step once more where parts are added up.  Sums over
+// steps have them in their places.
 __device__ __forceinline__ int up_of(int b) { return b >> 4; }
 __device__ __forceinline__ u128 placed(uint64_t mass, int b) { return (u128)mass << (64 - up_of(b)); }
 // What is to come of step b, in its own numbers: the least one that is v or more.

@@ -442,7 +442,8 @@ inline std::string encode_sample(const StepTable& t, const daris_sample& o, int 
   a.row = o.logits_row;
   a.rows = o.rows; a.n = o.n;
   a.chunks = (o.n + kSampleChunk - 1) / kSampleChunk;
-  // A chunk for each wave of a part, two where that makes more workgroups than the CUs hold.
+  // A chunk for each wave of a part, two where that makes more than two workgroups for each CU (which is what a CU holds of bf16 rows at once; of fp32 ones, whose numbers take more registers, it holds
+  // one).
   a.part_chunks = (int64_t)o.rows * ((a.chunks + kSampleWaves - 1) / kSampleWaves) > 2 * n_cu ? 2 * kSampleWaves : kSampleWaves;
   a.parts = (a.chunks + a.part_chunks - 1) / a.part_chunks;
   if (a.parts > 1) {

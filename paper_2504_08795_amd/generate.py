@@ -5,7 +5,8 @@ along by the norms.  Prompts of several streams go through it as one ragged set 
 stream; a step is one list of operators, planned once.  Weights are random: this is an example and a measurement, not a model.
 
 Words are the likeliest ones or drawn (temperature, top_k, top_p, min_p).  A step may carry drafts: a tree of words behind every stream's last one, which goes
-through the blocks at once; the words that the model would have given itself stand, and the cache keeps their tokens only.  A stream can be continued twice
+through the blocks at once; the words that the model would have given itself stand, and the cache keeps their tokens only.  Such a step makes its buffers and its list
+anew, as its rows differ each time: 1.5 ms in place of 0.23 for four streams and four blocks, so it shows the calls and is no gain.  A stream can be continued twice
 (fork): full pages are shared and the last one is copied.
 
     python -m paper_2504_08795_amd.generate --streams 4 --prompt 100 --tokens 64 --check
