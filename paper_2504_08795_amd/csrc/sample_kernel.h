@@ -877,7 +877,7 @@ struct Sampler {
       }
       front(turn, k, want, weighed && a.parts > 1 && (turn || !by_mass));
     }
-    if (mp > 0.f) leave((double)temperature * log((double)mp), (double)mp);
+    if (mp > 0.f) leave((double)temperature * (mp < 1.f ? log((double)mp) : -0x1p-54), (double)mp);  // (what is nearer than that weighs 1 in 64 bits)
     float u = a.random[r];
     u = u >= 1.f ? INFINITY : u >= 0.f ? u : 0.f;  // (no sum passes it: 1 x the whole sum, added up another way, may be passed by less than all)
     // ---- the weights that are left, and where their sum passes the random number

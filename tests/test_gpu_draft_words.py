@@ -84,3 +84,17 @@ def test_words_of_no_weight_have_no_part_in_the_sum_that_a_small_random_number_p
     for more in (dict(top_k=[n - 1]), dict()):
         got, want = words(part, x, [2.0 ** -37], **more)
         assert got == want == [17 + 8 * 8192], more
+
+
+@pytest.mark.parametrize("n", [9, 700, 20001])
+def test_min_p_of_1_leaves_all_that_weigh_1(part, n):
+    """Logits so near each other, or a temperature so high, that their weights are 1 in 64 bits, and two that weigh less."""
+    x = torch.randn((4, n), generator=torch.Generator().manual_seed(n))
+    x[0] *= 1e-30
+    x[1] *= 1e-20
+    x[:, n // 3] = x[:, n // 2] = torch.tensor([-1.0, -1e-3, -3.0e38, -1e30])
+    for u in (0.0, 0.37, 0.9999, 1.0):
+        for more in (dict(), dict(top_k=[n - 2] * 4), dict(top_p=[0.7] * 4)):
+            got, want = words(part, x, [u] * 4, temperature=[1.0, 0.5, 1e30, math.inf], min_p=[1.0] * 4, **more)
+            assert got == want, (u, more)
+    assert got[0] not in (n // 3, n // 2)
