@@ -13,7 +13,7 @@
 // waited for its registers: 64 rows of 131072, bf16, top_p 0.5 to 0.95, 135 us a call and 85.)
 //
 // One row of 50001 (fp32, 40 likeliest): 28 us a call, the parts 6 of them and the end 16, which is a chain of barriers and fetches: histograms, the step, its words, their order.  64 rows
-// of 131072 (bf16, wishes of every kind), 16.8 MB: 81 us, the parts 19 (75 % of the SIMDs' cycles are vector instructions), the end 54 on 64 CUs, of which the
+// of 131072 (bf16, wishes of every kind), 16.8 MB: 77 to 83 us, the parts 19 (75 % of the SIMDs' cycles are vector instructions), the end 54 on 64 CUs, of which the
 // longest rows gather the words of their step from 256 chunks (18) and add up one part's weights (11).  Weights in 64 bits cost 20 instructions a number; a lane's numbers take
 // turns in one loop of them (unrolled, the constants of eight weights leave half of the waves without registers).  Kept weights are taken again in one part only, as the
 // histograms say what is left of the others (one row of 131072, flat: 48 us for all of it, 7 so).
